@@ -40,8 +40,8 @@ typedef enum {
     QNN_OK = 0,
     QNN_ERR_NULL = 1,        /* a required pointer is NULL */
     QNN_ERR_SHAPE = 2,       /* a size, leading dimension, plane count or mode is out of range */
-    QNN_ERR_ALIGN = 3,       /* a pointer is not 4-byte aligned */
-    QNN_ERR_OVERFLOW = 4,    /* (sum |coefA|) * (sum |coefW|) * K does not fit int32 */
+    QNN_ERR_ALIGN = 3,       /* a pointer is not 4-byte aligned (float matrices beside codes: not aligned to their element) */
+    QNN_ERR_OVERFLOW = 4,    /* (sum |coefA|) * (sum |coefW|) * K, or 128 * 128 * K of int8 codes, does not fit int32 */
     QNN_ERR_UNSUPPORTED = 5, /* requested variant cannot handle these arguments */
     QNN_ERR_WORKSPACE = 6,   /* workspace NULL, misaligned (256 B) or too small */
     QNN_ERR_HIP = 7          /* the HIP runtime reported an error at launch */
@@ -65,6 +65,9 @@ typedef enum {
                                plane counts 1, 2, 4 or 8, coefficients a common factor times 1, 2, 4, ...), or, for
                                large products with int32 output, per call in memory (see qnn_bitplane_gemm) */
 } qnn_engine;
+
+/* Element type of the float matrices of the calls on int8 codes. */
+typedef enum { QNN_F32 = 0, QNN_F16 = 1, QNN_BF16 = 2 } qnn_float_type;
 
 #define QNN_MAX_PLANES 8
 #define QNN_MAX_LAYERS 16
@@ -306,6 +309,59 @@ int qnn_conv2d_dedup(const uint32_t *A, int Pa, const int32_t *coefA, int64_t st
                      int64_t Wd, int64_t Cin, const uint32_t *W, int64_t Cout, int pad, int32_t *out,
                      uint32_t *unique_count, void *workspace, size_t workspace_bytes, void *stream);
 size_t qnn_conv2d_dedup_workspace_bytes(int64_t B, int64_t H, int64_t Wd, int64_t Cin, int64_t Cout, int pad);
+
+/* 8-bit integer feed-forward path.  Activations and weights are int8 CODES with one float32 scale a row (a token, an output channel); a code stands
+ * for code * scale.  Rows are quantized as scale = max|y| / 127, code = rint(y * 127 / max|y|), ties to even: no value is clipped, a row of zeros has
+ * scale 0.  A row with a value that is not finite has scale NaN and codes 0, so that everything formed from it is NaN.  Float matrices are float32,
+ * float16 or bfloat16 (qnn_float_type), pointers aligned to their element; codes may lie at any address.  Rows of whole 16-byte groups at 16-byte
+ * aligned addresses are fastest.  All arithmetic between reading and writing is float32 or wider, or exact integers. */
+
+/* Root-mean-square norm with the residual's addition, to codes: h = x + residual, y = h / sqrt(mean(h^2) + eps) * gamma, codes and scale of y.
+ * x, residual (NULL: none), sum (NULL: not written; receives h, rounded once; it may be x or residual itself): DEVICE [rows][ld] of `type`.
+ * gamma: DEVICE [K] of float32 or `type` (gamma_type).  codes: DEVICE int8 [rows][ld_codes]; scale: DEVICE float32 [rows].  eps >= 0, finite.
+ * The norm is formed from h before it is rounded.  A row whose mean square is beyond float32 counts as not finite. */
+int qnn_rms_norm_quant(const void *x, int64_t ldx, const void *residual, int64_t ld_residual, int type, const void *gamma, int gamma_type, float eps,
+                       int64_t rows, int64_t K, void *sum, int64_t ld_sum, int8_t *codes, int64_t ld_codes, float *scale, void *stream);
+
+/* Its gradient, the quantizer taken as the identity (straight through, as Sec. 2.3 takes the sign): with g = grad the gradient at y, r = 1 /
+ * sqrt(mean(h^2) + eps) and grad_sum (NULL: none) a gradient that reaches h along the residual path,
+ *   grad_h = r (gamma g - h r^2 mean(gamma g h)) + grad_sum,   grad_gamma = sum over the rows of g h r   (DEVICE float32 [K]).
+ * h: what the forward call wrote to `sum` (x, without a residual).  grad_h may be grad_sum itself.  rows >= 1; K <= 16384.  workspace: DEVICE,
+ * 256-byte aligned, qnn_rms_norm_backward_workspace_bytes(rows, K) bytes.  Sums are formed in a fixed order. */
+int qnn_rms_norm_backward(const void *grad, int64_t ld_grad, const void *h, int64_t ld_h, const void *grad_sum, int64_t ld_grad_sum, int type,
+                          const void *gamma, int gamma_type, float eps, int64_t rows, int64_t K, void *grad_h, int64_t ld_grad_h, float *grad_gamma,
+                          void *workspace, size_t workspace_bytes, void *stream);
+size_t qnn_rms_norm_backward_workspace_bytes(int64_t rows, int64_t K);
+
+/* Gated activation, to codes: y = up * gate / (1 + exp(-gate)).  gate, up: DEVICE [rows][ld] of `type` (e.g. the two halves of one product's rows). */
+int qnn_silu_gate_quant(const void *gate, int64_t ld_gate, const void *up, int64_t ld_up, int type, int64_t rows, int64_t F, int8_t *codes,
+                        int64_t ld_codes, float *scale, void *stream);
+
+/* Its gradient, the quantizer taken as the identity: with g = grad and s = 1 / (1 + exp(-gate)),
+ *   grad_gate = g up s (1 + gate (1 - s)),   grad_up = g gate s.   grad_gate may be gate itself, grad_up may be up itself. */
+int qnn_silu_gate_backward(const void *grad, int64_t ld_grad, const void *gate, int64_t ld_gate, const void *up, int64_t ld_up, int type, int64_t rows,
+                           int64_t F, void *grad_gate, int64_t ld_grad_gate, void *grad_up, int64_t ld_grad_up, void *stream);
+
+/* Product of codes: out[m][n] = scaleA[m] * scaleW[n] * sum_k A[m][k] W[n][k] + bias[n].  A: DEVICE int8 [M][lda], W: DEVICE int8 [N][ldw], out: DEVICE
+ * [M][ldo] of `type`; scaleA [M], scaleW [N], bias [N] (NULL: none): DEVICE float32.  The sums are exact int32, so K <= 131071 (QNN_ERR_OVERFLOW). */
+int qnn_int8_gemm(const int8_t *A, int64_t lda, const float *scaleA, const int8_t *W, int64_t ldw, const float *scaleW, const float *bias, void *out,
+                  int64_t ldo, int type, int64_t M, int64_t N, int64_t K, void *stream);
+
+/* Mixture-of-experts layer for a few tokens.  Token t goes to the `top` experts of the largest logits (ties: the lowest index), weighted with the softmax
+ * of these logits:  u = W1[e] x[t] (scaled as in qnn_int8_gemm), a = up * silu(gate) of u = [gate; up] quantized to codes, v = W2[e] a (scaled),
+ * out[t] = sum of the experts' weight * v.  An expert of weight 0 (a logit of -infinity, say) takes no part; a token with no logit above -infinity gets
+ * zeros; one with a logit that is NaN or +infinity gets NaN.
+ * x: DEVICE int8 [tokens][ldx] with scale_x [tokens]; logits: DEVICE float32 [tokens][ld_logits]; W1: DEVICE int8 [experts][2F][ld_w1] (rows of H) with
+ * scale1 [experts][2F]; W2: DEVICE int8 [experts][H][ld_w2] (rows of F) with scale2 [experts][H]; out: DEVICE [tokens][ldo] of `type`.
+ * tokens <= QNN_MOE_MAX_TOKENS, 1 <= top <= min(experts, QNN_MOE_MAX_TOP), experts <= QNN_MOE_MAX_EXPERTS (QNN_ERR_UNSUPPORTED beyond); H, F <= 131071.
+ * workspace: DEVICE, 256-byte aligned, qnn_int8_moe_workspace_bytes(...) bytes.  Sums are formed in a fixed order. */
+#define QNN_MOE_MAX_TOKENS 64
+#define QNN_MOE_MAX_TOP 8
+#define QNN_MOE_MAX_EXPERTS 256
+int qnn_int8_moe(const int8_t *x, int64_t ldx, const float *scale_x, const float *logits, int64_t ld_logits, int64_t tokens, int experts, int top,
+                 int64_t H, int64_t F, const int8_t *W1, int64_t ld_w1, const float *scale1, const int8_t *W2, int64_t ld_w2, const float *scale2, void *out,
+                 int64_t ldo, int type, void *workspace, size_t workspace_bytes, void *stream);
+size_t qnn_int8_moe_workspace_bytes(int64_t tokens, int top, int64_t F);
 
 /* Engine (QNN_ENGINE_VALU, QNN_ENGINE_MFMA, QNN_ENGINE_MFMA_FP4 or QNN_ENGINE_MFMA_LDS) that ran the calling thread's last successful
  * multiply call; 0 before any.  QNN_ENGINE_MFMA_FP4 covers every kernel on the FP4 matrix cores: with QNN_ENGINE_AUTO also those for

@@ -66,6 +66,13 @@ _SIGS = {
     "qnn_conv2d_dedup": [_vp, _int, _vp, _i64, _i64, _i64, _i64, _i64, _vp, _i64, _int, _vp, _vp, _vp, _sz, _vp],
     "qnn_bitplane_conv2d_ex": [_vp, _int, _vp, _int, _i64, _i64, _i64, _i64, _i64, _vp, _int, _vp, _int, _i64, _i64, _int,
                                _int, _int, _int, _vp, _int, _vp],
+    "qnn_rms_norm_quant": [_vp, _i64, _vp, _i64, _int, _vp, _int, C.c_float, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _vp],
+    "qnn_rms_norm_backward": [_vp, _i64, _vp, _i64, _vp, _i64, _int, _vp, _int, C.c_float, _i64, _i64, _vp, _i64, _vp, _vp, _sz, _vp],
+    "qnn_silu_gate_quant": [_vp, _i64, _vp, _i64, _int, _i64, _i64, _vp, _i64, _vp, _vp],
+    "qnn_silu_gate_backward": [_vp, _i64, _vp, _i64, _vp, _i64, _int, _i64, _i64, _vp, _i64, _vp, _i64, _vp],
+    "qnn_int8_gemm": [_vp, _i64, _vp, _vp, _i64, _vp, _vp, _vp, _i64, _int, _i64, _i64, _i64, _vp],
+    "qnn_int8_moe": [_vp, _i64, _vp, _vp, _i64, _i64, _int, _int, _i64, _i64, _vp, _i64, _vp, _vp, _i64, _vp, _vp, _i64, _int, _vp,
+                     _sz, _vp],
 }
 for _name, _args in _SIGS.items():
     _f = getattr(_lib, _name)
@@ -80,6 +87,10 @@ _lib.qnn_conv2d_dedup_workspace_bytes.argtypes = [_i64, _i64, _i64, _i64, _i64, 
 _lib.qnn_conv2d_dedup_workspace_bytes.restype = _sz
 _lib.qnn_binary_backward_workspace_bytes.argtypes = [_i64, _i64, _i64, _int]
 _lib.qnn_binary_backward_workspace_bytes.restype = _sz
+_lib.qnn_rms_norm_backward_workspace_bytes.argtypes = [_i64, _i64]
+_lib.qnn_rms_norm_backward_workspace_bytes.restype = _sz
+_lib.qnn_int8_moe_workspace_bytes.argtypes = [_i64, _int, _i64]
+_lib.qnn_int8_moe_workspace_bytes.restype = _sz
 _lib.qnn_last_engine.restype = C.c_int
 _lib.qnn_last_error.restype = C.c_char_p
 _lib.qnn_version.restype = C.c_char_p
@@ -111,7 +122,8 @@ _lib.qnn_last_engines.argtypes = [_vp, _int]
 _lib.qnn_last_engines.restype = C.c_int
 
 EXPORTS = sorted(list(_SIGS) + ["qnn_binary_mlp_workspace_bytes", "qnn_static_scratch_bytes", "qnn_binary_convnet_workspace_bytes",
-                               "qnn_binary_backward_workspace_bytes", "qnn_conv2d_dedup_workspace_bytes", "qnn_last_engine",
+                               "qnn_binary_backward_workspace_bytes", "qnn_conv2d_dedup_workspace_bytes", "qnn_rms_norm_backward_workspace_bytes",
+                               "qnn_int8_moe_workspace_bytes", "qnn_last_engine",
                                "qnn_last_engines", "qnn_last_error", "qnn_version"])
 
 
@@ -593,3 +605,171 @@ def qnn_binary_convnet_forward(x: torch.Tensor, in_bits: int, cout: Sequence[int
                                            fo, Wp, Tp, Fp, _dev(logits, torch.int32, "logits"), ldl,
                                            _dev(workspace, torch.uint8, "workspace"), workspace.numel(), engine, _stream()))
     return logits
+
+
+# ------------------------------------------------------------------------------------------- 8-bit integer feed-forward path
+_FLOAT_TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+
+
+def _float_type(t: torch.Tensor, name: str) -> int:
+    code = _FLOAT_TYPES.get(t.dtype)
+    if code is None:
+        raise ValueError(f"{name} must be float32, float16 or bfloat16, got {t.dtype}")
+    return code
+
+
+def _shaped(t: torch.Tensor, rows: int, cols: int, name: str) -> int:
+    """Leading dimension of a [rows][cols] tensor with contiguous rows."""
+    r, c, ld = _rows_ld(t, name)
+    if (r, c) != (rows, cols):
+        raise ValueError(f"{name} must be [{rows}][{cols}], got [{r}][{c}]")
+    return ld
+
+
+def _vector(t: torch.Tensor, n: int, name: str) -> torch.Tensor:
+    if t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
+        raise ValueError(f"{name} must be dense [{n}]")
+    return t
+
+
+def _new_codes(rows: int, cols: int, like: torch.Tensor) -> torch.Tensor:
+    """Codes whose rows start at multiples of 16 bytes, which the products read fastest."""
+    return torch.empty((rows, (cols + 15) // 16 * 16), dtype=torch.int8, device=like.device)[:, :cols]
+
+
+def qnn_rms_norm_quant(x: torch.Tensor, gamma: torch.Tensor, eps: float, residual: Optional[torch.Tensor] = None,
+                       codes: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
+                       total: Optional[torch.Tensor] = None):
+    """h = x + residual (x, without one); codes int8 [rows][K] and scale float32 [rows] of h / sqrt(mean(h^2) + eps) * gamma
+    -> (codes, scale, h).  h goes to `total` (a new tensor if None; x or residual themselves are fine); without a residual and a `total` it is x."""
+    rows, K, ldx = _rows_ld(x, "x")
+    kind = _float_type(x, "x")
+    ldr = 0 if residual is None else _shaped(residual, rows, K, "residual")
+    if codes is None:
+        codes = _new_codes(rows, K, x)
+    if scale is None:
+        scale = torch.empty(rows, dtype=torch.float32, device=x.device)
+    if total is None and residual is not None:
+        total = torch.empty((rows, K), dtype=x.dtype, device=x.device)
+    lds = 0 if total is None else _shaped(total, rows, K, "total")
+    _check(_lib.qnn_rms_norm_quant(_dev(x, x.dtype, "x"), ldx, _dev(residual, x.dtype, "residual"), ldr, kind,
+                                   _dev(_vector(gamma, K, "gamma"), gamma.dtype, "gamma"), _float_type(gamma, "gamma"), eps, rows, K,
+                                   _dev(total, x.dtype, "total"), lds, _dev(codes, torch.int8, "codes"), _shaped(codes, rows, K, "codes"),
+                                   _dev(_vector(scale, rows, "scale"), torch.float32, "scale"), _stream()))
+    return codes, scale, x if total is None else total
+
+
+def qnn_rms_norm_backward_workspace_bytes(rows: int, K: int) -> int:
+    return int(_lib.qnn_rms_norm_backward_workspace_bytes(rows, K))
+
+
+def qnn_rms_norm_backward(grad: torch.Tensor, h: torch.Tensor, gamma: torch.Tensor, eps: float,
+                          grad_sum: Optional[torch.Tensor] = None, grad_h: Optional[torch.Tensor] = None,
+                          grad_gamma: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """Gradient of qnn_rms_norm_quant, straight through the quantizer.  grad: at the normed values; h: the forward call's third result; grad_sum: a
+    gradient that reaches h along the residual path -> (grad_h [rows][K] of the type of h, grad_gamma float32 [K])."""
+    rows, K, ldh = _rows_ld(h, "h")
+    kind = _float_type(h, "h")
+    ldz = 0 if grad_sum is None else _shaped(grad_sum, rows, K, "grad_sum")
+    if grad_h is None:
+        grad_h = torch.empty((rows, K), dtype=h.dtype, device=h.device)
+    if grad_gamma is None:
+        grad_gamma = torch.empty(K, dtype=torch.float32, device=h.device)
+    if workspace is None:
+        workspace = torch.empty(max(qnn_rms_norm_backward_workspace_bytes(rows, K), 1), dtype=torch.uint8, device=h.device)
+    _check(_lib.qnn_rms_norm_backward(_dev(grad, h.dtype, "grad"), _shaped(grad, rows, K, "grad"), _dev(h, h.dtype, "h"), ldh,
+                                      _dev(grad_sum, h.dtype, "grad_sum"), ldz, kind,
+                                      _dev(_vector(gamma, K, "gamma"), gamma.dtype, "gamma"), _float_type(gamma, "gamma"), eps, rows, K,
+                                      _dev(grad_h, h.dtype, "grad_h"), _shaped(grad_h, rows, K, "grad_h"),
+                                      _dev(_vector(grad_gamma, K, "grad_gamma"), torch.float32, "grad_gamma"),
+                                      _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream()))
+    return grad_h, grad_gamma
+
+
+def qnn_silu_gate_quant(gate: torch.Tensor, up: torch.Tensor, codes: Optional[torch.Tensor] = None,
+                        scale: Optional[torch.Tensor] = None):
+    """Codes int8 [rows][F] and scale float32 [rows] of up * gate / (1 + exp(-gate)) -> (codes, scale).  gate and up may be the halves of one
+    product's rows: u[:, :F], u[:, F:]."""
+    rows, F, ldg = _rows_ld(gate, "gate")
+    kind = _float_type(gate, "gate")
+    if codes is None:
+        codes = _new_codes(rows, F, gate)
+    if scale is None:
+        scale = torch.empty(rows, dtype=torch.float32, device=gate.device)
+    _check(_lib.qnn_silu_gate_quant(_dev(gate, gate.dtype, "gate"), ldg, _dev(up, gate.dtype, "up"), _shaped(up, rows, F, "up"), kind, rows, F,
+                                    _dev(codes, torch.int8, "codes"), _shaped(codes, rows, F, "codes"),
+                                    _dev(_vector(scale, rows, "scale"), torch.float32, "scale"), _stream()))
+    return codes, scale
+
+
+def qnn_silu_gate_backward(grad: torch.Tensor, gate: torch.Tensor, up: torch.Tensor, grad_gate: Optional[torch.Tensor] = None,
+                           grad_up: Optional[torch.Tensor] = None):
+    """Gradient of qnn_silu_gate_quant, straight through the quantizer -> (grad_gate, grad_up), by default the halves of one tensor [rows][2F]."""
+    rows, F, ldg = _rows_ld(gate, "gate")
+    kind = _float_type(gate, "gate")
+    if grad_gate is None or grad_up is None:
+        both = torch.empty((rows, 2 * F), dtype=gate.dtype, device=gate.device)
+        grad_gate = both[:, :F] if grad_gate is None else grad_gate
+        grad_up = both[:, F:] if grad_up is None else grad_up
+    _check(_lib.qnn_silu_gate_backward(_dev(grad, gate.dtype, "grad"), _shaped(grad, rows, F, "grad"), _dev(gate, gate.dtype, "gate"), ldg,
+                                       _dev(up, gate.dtype, "up"), _shaped(up, rows, F, "up"), kind, rows, F,
+                                       _dev(grad_gate, gate.dtype, "grad_gate"), _shaped(grad_gate, rows, F, "grad_gate"),
+                                       _dev(grad_up, gate.dtype, "grad_up"), _shaped(grad_up, rows, F, "grad_up"), _stream()))
+    return grad_gate, grad_up
+
+
+def qnn_int8_gemm(A: torch.Tensor, scaleA: torch.Tensor, W: torch.Tensor, scaleW: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                  out: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
+    """scaleA[m] * scaleW[n] * sum_k A[m][k] W[n][k] + bias[n] on int8 codes, as `dtype` (that of `out`, if there is one)."""
+    M, K, lda = _rows_ld(A, "A")
+    N, Kw, ldw = _rows_ld(W, "W")
+    if Kw != K:
+        raise ValueError(f"rows of A have {K} codes, rows of W {Kw}")
+    if out is None:
+        out = torch.empty((M, N), dtype=dtype, device=A.device)
+    _check(_lib.qnn_int8_gemm(_dev(A, torch.int8, "A"), lda, _dev(_vector(scaleA, M, "scaleA"), torch.float32, "scaleA"),
+                              _dev(W, torch.int8, "W"), ldw, _dev(_vector(scaleW, N, "scaleW"), torch.float32, "scaleW"),
+                              None if bias is None else _dev(_vector(bias, N, "bias"), torch.float32, "bias"),
+                              _dev(out, out.dtype, "out"), _shaped(out, M, N, "out"), _float_type(out, "out"), M, N, K, _stream()))
+    return out
+
+
+def qnn_int8_moe_workspace_bytes(tokens: int, top: int, F: int) -> int:
+    return int(_lib.qnn_int8_moe_workspace_bytes(tokens, top, F))
+
+
+def _experts_ld(t: torch.Tensor, name: str):
+    """(experts, rows, cols, leading dimension) of a [experts][rows][cols] tensor whose experts follow each other without a gap."""
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or (shape[2] > 1 and stride[2] != 1):
+        raise ValueError(f"{name} must be [experts][rows][cols] with contiguous rows")
+    ld = stride[1] if shape[1] > 1 else (stride[0] if shape[0] > 1 else max(shape[2], 1))
+    if shape[0] > 1 and stride[0] != shape[1] * ld:
+        raise ValueError(f"the experts of {name} must follow each other without a gap")
+    return *shape, ld
+
+
+def qnn_int8_moe(x: torch.Tensor, scale_x: torch.Tensor, logits: torch.Tensor, top: int, W1: torch.Tensor, scale1: torch.Tensor,
+                 W2: torch.Tensor, scale2: torch.Tensor, out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                 dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
+    """Mixture-of-experts layer for a few tokens.  x: int8 codes [tokens][H] with scale_x; logits: float32 [tokens][experts]; W1: int8
+    [experts][2F][H] (gate, then up) with scale1 [experts][2F]; W2: int8 [experts][H][F] with scale2 [experts][H] -> [tokens][H] as `dtype` (that of
+    `out`, if there is one)."""
+    T, H, ldx = _rows_ld(x, "x")
+    E, F2, H1, ld1 = _experts_ld(W1, "W1")
+    F = F2 // 2
+    E2, H2, Fw, ld2 = _experts_ld(W2, "W2")
+    if F2 != 2 * Fw or E2 != E or H1 != H or H2 != H:
+        raise ValueError("W1 must be [experts][2F][H] and W2 [experts][H][F]")
+    if tuple(scale1.shape) != (E, F2) or not scale1.is_contiguous() or tuple(scale2.shape) != (E, H) or not scale2.is_contiguous():
+        raise ValueError("scale1 must be dense [experts][2F] and scale2 dense [experts][H]")
+    if out is None:
+        out = torch.empty((T, H), dtype=dtype, device=x.device)
+    if workspace is None:
+        workspace = torch.empty(max(qnn_int8_moe_workspace_bytes(T, top, F), 1), dtype=torch.uint8, device=x.device)
+    _check(_lib.qnn_int8_moe(_dev(x, torch.int8, "x"), ldx, _dev(_vector(scale_x, T, "scale_x"), torch.float32, "scale_x"),
+                             _dev(logits, torch.float32, "logits"), _shaped(logits, T, E, "logits"), T, E, top, H, F,
+                             _dev(W1, torch.int8, "W1"), ld1, _dev(scale1, torch.float32, "scale1"), _dev(W2, torch.int8, "W2"), ld2,
+                             _dev(scale2, torch.float32, "scale2"), _dev(out, out.dtype, "out"), _shaped(out, T, H, "out"),
+                             _float_type(out, "out"), _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream()))
+    return out
