@@ -98,7 +98,9 @@ _lib.qnn_version.restype = C.c_char_p
 # The calls made per layer or time step marshal their arguments in C++ where everything is as usual (status -1: it is not, see there).
 # Without that part, or with one that was built for another torch or Python, every call is marshalled here.
 _MARSHALLED = {"pack_sign": "qnn_pack_sign", "linear_quant_planes": "qnn_linear_quant_planes", "binary_gemm": "qnn_binary_gemm",
-               "binary_gemm_sign": "qnn_binary_gemm_sign", "bitplane_gemm": "qnn_bitplane_gemm", "bitplane_conv2d": "qnn_bitplane_conv2d"}
+               "binary_gemm_sign": "qnn_binary_gemm_sign", "bitplane_gemm": "qnn_bitplane_gemm", "bitplane_conv2d": "qnn_bitplane_conv2d",
+               "rms_norm_quant": "qnn_rms_norm_quant", "rms_norm_backward": "qnn_rms_norm_backward", "silu_gate_quant": "qnn_silu_gate_quant",
+               "silu_gate_backward": "qnn_silu_gate_backward", "int8_gemm": "qnn_int8_gemm", "int8_moe": "qnn_int8_moe"}
 
 
 def _load_native():
@@ -642,6 +644,11 @@ def qnn_rms_norm_quant(x: torch.Tensor, gamma: torch.Tensor, eps: float, residua
                        total: Optional[torch.Tensor] = None):
     """h = x + residual (x, without one); codes int8 [rows][K] and scale float32 [rows] of h / sqrt(mean(h^2) + eps) * gamma
     -> (codes, scale, h).  h goes to `total` (a new tensor if None; x or residual themselves are fine); without a residual and a `total` it is x."""
+    if codes is not None and (residual is None or total is not None):
+        status = _native.rms_norm_quant(x, gamma, eps, residual, codes, scale, total, _stream)
+        if status >= 0:
+            _check(status)
+            return codes, scale, x if total is None else total
     rows, K, ldx = _rows_ld(x, "x")
     kind = _float_type(x, "x")
     ldr = 0 if residual is None else _shaped(residual, rows, K, "residual")
@@ -668,6 +675,9 @@ def qnn_rms_norm_backward(grad: torch.Tensor, h: torch.Tensor, gamma: torch.Tens
                           grad_gamma: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
     """Gradient of qnn_rms_norm_quant, straight through the quantizer.  grad: at the normed values; h: the forward call's third result; grad_sum: a
     gradient that reaches h along the residual path -> (grad_h [rows][K] of the type of h, grad_gamma float32 [K])."""
+    if grad_h is not None and (status := _native.rms_norm_backward(grad, h, gamma, eps, grad_sum, grad_h, grad_gamma, workspace, _stream)) >= 0:
+        _check(status)
+        return grad_h, grad_gamma
     rows, K, ldh = _rows_ld(h, "h")
     kind = _float_type(h, "h")
     ldz = 0 if grad_sum is None else _shaped(grad_sum, rows, K, "grad_sum")
@@ -690,6 +700,9 @@ def qnn_silu_gate_quant(gate: torch.Tensor, up: torch.Tensor, codes: Optional[to
                         scale: Optional[torch.Tensor] = None):
     """Codes int8 [rows][F] and scale float32 [rows] of up * gate / (1 + exp(-gate)) -> (codes, scale).  gate and up may be the halves of one
     product's rows: u[:, :F], u[:, F:]."""
+    if codes is not None and (status := _native.silu_gate_quant(gate, up, codes, scale, _stream)) >= 0:
+        _check(status)
+        return codes, scale
     rows, F, ldg = _rows_ld(gate, "gate")
     kind = _float_type(gate, "gate")
     if codes is None:
@@ -705,6 +718,9 @@ def qnn_silu_gate_quant(gate: torch.Tensor, up: torch.Tensor, codes: Optional[to
 def qnn_silu_gate_backward(grad: torch.Tensor, gate: torch.Tensor, up: torch.Tensor, grad_gate: Optional[torch.Tensor] = None,
                            grad_up: Optional[torch.Tensor] = None):
     """Gradient of qnn_silu_gate_quant, straight through the quantizer -> (grad_gate, grad_up), by default the halves of one tensor [rows][2F]."""
+    if grad_gate is not None and (status := _native.silu_gate_backward(grad, gate, up, grad_gate, grad_up, _stream)) >= 0:
+        _check(status)
+        return grad_gate, grad_up
     rows, F, ldg = _rows_ld(gate, "gate")
     kind = _float_type(gate, "gate")
     if grad_gate is None or grad_up is None:
@@ -721,6 +737,9 @@ def qnn_silu_gate_backward(grad: torch.Tensor, gate: torch.Tensor, up: torch.Ten
 def qnn_int8_gemm(A: torch.Tensor, scaleA: torch.Tensor, W: torch.Tensor, scaleW: torch.Tensor, bias: Optional[torch.Tensor] = None,
                   out: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
     """scaleA[m] * scaleW[n] * sum_k A[m][k] W[n][k] + bias[n] on int8 codes, as `dtype` (that of `out`, if there is one)."""
+    if out is not None and (status := _native.int8_gemm(A, scaleA, W, scaleW, bias, out, _stream)) >= 0:
+        _check(status)
+        return out
     M, K, lda = _rows_ld(A, "A")
     N, Kw, ldw = _rows_ld(W, "W")
     if Kw != K:
@@ -755,6 +774,9 @@ def qnn_int8_moe(x: torch.Tensor, scale_x: torch.Tensor, logits: torch.Tensor, t
     """Mixture-of-experts layer for a few tokens.  x: int8 codes [tokens][H] with scale_x; logits: float32 [tokens][experts]; W1: int8
     [experts][2F][H] (gate, then up) with scale1 [experts][2F]; W2: int8 [experts][H][F] with scale2 [experts][H] -> [tokens][H] as `dtype` (that of
     `out`, if there is one)."""
+    if out is not None and (status := _native.int8_moe(x, scale_x, logits, top, W1, scale1, W2, scale2, out, workspace, _stream)) >= 0:
+        _check(status)
+        return out
     T, H, ldx = _rows_ld(x, "x")
     E, F2, H1, ld1 = _experts_ld(W1, "W1")
     F = F2 // 2

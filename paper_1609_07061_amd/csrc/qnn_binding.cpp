@@ -20,8 +20,16 @@ typedef int (*BitplaneGemm)(const uint32_t *, int, const int32_t *, int, int64_t
                             int32_t *, int64_t, int64_t, int64_t, int64_t, void *);
 typedef int (*Conv2d)(const uint32_t *, int, const int32_t *, int, int64_t, int64_t, int64_t, int64_t, int64_t, const uint32_t *, int, const int32_t *,
                       int, int64_t, int64_t, int, int, int, int, int32_t *, void *);
-void *g_entry[6];
-enum { kPackSign, kLinearQuant, kBinaryGemm, kBinaryGemmSign, kBitplaneGemm, kConv2d };
+typedef int (*RmsNormQuant)(const void *, int64_t, const void *, int64_t, int, const void *, int, float, int64_t, int64_t, void *, int64_t, int8_t *, int64_t, float *, void *);
+typedef int (*RmsNormBackward)(const void *, int64_t, const void *, int64_t, const void *, int64_t, int, const void *, int, float, int64_t, int64_t, void *, int64_t, float *,
+                               void *, size_t, void *);
+typedef int (*SiluGateQuant)(const void *, int64_t, const void *, int64_t, int, int64_t, int64_t, int8_t *, int64_t, float *, void *);
+typedef int (*SiluGateBackward)(const void *, int64_t, const void *, int64_t, const void *, int64_t, int, int64_t, int64_t, void *, int64_t, void *, int64_t, void *);
+typedef int (*Int8Gemm)(const int8_t *, int64_t, const float *, const int8_t *, int64_t, const float *, const float *, void *, int64_t, int, int64_t, int64_t, int64_t, void *);
+typedef int (*Int8Moe)(const int8_t *, int64_t, const float *, const float *, int64_t, int64_t, int, int, int64_t, int64_t, const int8_t *, int64_t, const float *,
+                       const int8_t *, int64_t, const float *, void *, int64_t, int, void *, size_t, void *);
+enum { kPackSign, kLinearQuant, kBinaryGemm, kBinaryGemmSign, kBitplaneGemm, kConv2d, kRmsNormQuant, kRmsNormBackward, kSiluGateQuant, kSiluGateBackward, kInt8Gemm, kInt8Moe, kEntries };
+void *g_entry[kEntries];
 
 constexpr int kMaxPlanes = 8;  // QNN_MAX_PLANES
 
@@ -90,6 +98,35 @@ void *stream_of(int64_t v) { return reinterpret_cast<void *>(v); }
 template <typename T>
 T *as(const Rows &r) {
     return static_cast<T *>(r.p);
+}
+
+// qnn_float_type of a type of numbers, -1 for others
+int float_type(at::ScalarType t) { return t == at::kFloat ? 0 : t == at::kHalf ? 1 : t == at::kBFloat16 ? 2 : -1; }
+// [rows][cols] of any of these types
+bool floats_of(PyObject *o, Rows &r, int &type) {
+    if (!THPVariable_CheckExact(o)) return false;
+    const at::ScalarType t = THPVariable_Unpack(o).scalar_type();
+    type = float_type(t);
+    return type >= 0 && rows_of(o, t, 2, r);
+}
+// ... of a given one and shape
+bool shaped_like(PyObject *o, int type, int64_t rows, int64_t cols, Rows &r) {
+    int t;
+    return floats_of(o, r, t) && t == type && r.rows == rows && r.cols == cols;
+}
+bool codes_like(PyObject *o, int64_t rows, int64_t cols, Rows &r) { return rows_of(o, at::kChar, 2, r) && r.rows == rows && r.cols == cols; }
+// dense [n]
+bool vector_of(PyObject *o, at::ScalarType type, int64_t n, void *&p) {
+    const at::Tensor *const t = tensor(o, type, 1);
+    if (!t || t->size(0) != n || (n > 1 && t->stride(0) != 1)) return false;
+    p = t->data_ptr();
+    return true;
+}
+bool floats_vector(PyObject *o, int64_t n, void *&p, int &type) {
+    if (!THPVariable_CheckExact(o)) return false;
+    const at::ScalarType t = THPVariable_Unpack(o).scalar_type();
+    type = float_type(t);
+    return type >= 0 && vector_of(o, t, n, p);
 }
 
 // x, out, stream
@@ -167,6 +204,107 @@ PyObject *bitplane_conv2d(PyObject *const *a) {
     });
 }
 
+// x, gamma, eps, residual, codes, scale, total, stream
+PyObject *rms_norm_quant(PyObject *const *a) {
+    Rows x, res = {}, c, total = {};
+    void *gamma, *scale;
+    int type, gamma_type;
+    int64_t s;
+    if (!PyFloat_CheckExact(a[2]) || !floats_of(a[0], x, type) || !floats_vector(a[1], x.cols, gamma, gamma_type) ||
+        (a[3] != Py_None && !shaped_like(a[3], type, x.rows, x.cols, res)) || !codes_like(a[4], x.rows, x.cols, c) || !vector_of(a[5], at::kFloat, x.rows, scale) ||
+        (a[6] != Py_None && !shaped_like(a[6], type, x.rows, x.cols, total)) || !stream(a[7], s))
+        return not_here();
+    const float eps = (float)PyFloat_AS_DOUBLE(a[2]);
+    return call([&] {
+        return reinterpret_cast<RmsNormQuant>(g_entry[kRmsNormQuant])(x.p, x.ld, res.p, res.ld, type, gamma, gamma_type, eps, x.rows, x.cols, total.p, total.ld, as<int8_t>(c), c.ld,
+                                                                      static_cast<float *>(scale), stream_of(s));
+    });
+}
+// grad, h, gamma, eps, grad_sum, grad_h, grad_gamma, workspace, stream
+PyObject *rms_norm_backward(PyObject *const *a) {
+    Rows g, h, z = {}, o;
+    void *gamma, *grad_gamma;
+    int type, gamma_type;
+    int64_t s;
+    const at::Tensor *const ws = tensor(a[7], at::kByte, 1);
+    if (!ws || !ws->is_contiguous() || !PyFloat_CheckExact(a[3]) || !floats_of(a[1], h, type) || !shaped_like(a[0], type, h.rows, h.cols, g) ||
+        !floats_vector(a[2], h.cols, gamma, gamma_type) || (a[4] != Py_None && !shaped_like(a[4], type, h.rows, h.cols, z)) ||
+        !shaped_like(a[5], type, h.rows, h.cols, o) || !vector_of(a[6], at::kFloat, h.cols, grad_gamma) || !stream(a[8], s))
+        return not_here();
+    const float eps = (float)PyFloat_AS_DOUBLE(a[3]);
+    void *const w = ws->data_ptr();
+    const size_t bytes = (size_t)ws->numel();
+    return call([&] {
+        return reinterpret_cast<RmsNormBackward>(g_entry[kRmsNormBackward])(g.p, g.ld, h.p, h.ld, z.p, z.ld, type, gamma, gamma_type, eps, h.rows, h.cols, o.p, o.ld,
+                                                                            static_cast<float *>(grad_gamma), w, bytes, stream_of(s));
+    });
+}
+// gate, up, codes, scale, stream
+PyObject *silu_gate_quant(PyObject *const *a) {
+    Rows g, u, c;
+    void *scale;
+    int type;
+    int64_t s;
+    if (!floats_of(a[0], g, type) || !shaped_like(a[1], type, g.rows, g.cols, u) || !codes_like(a[2], g.rows, g.cols, c) || !vector_of(a[3], at::kFloat, g.rows, scale) ||
+        !stream(a[4], s))
+        return not_here();
+    return call([&] {
+        return reinterpret_cast<SiluGateQuant>(g_entry[kSiluGateQuant])(g.p, g.ld, u.p, u.ld, type, g.rows, g.cols, as<int8_t>(c), c.ld, static_cast<float *>(scale), stream_of(s));
+    });
+}
+// grad, gate, up, grad_gate, grad_up, stream
+PyObject *silu_gate_backward(PyObject *const *a) {
+    Rows d, g, u, dg, du;
+    int type;
+    int64_t s;
+    if (!floats_of(a[1], g, type) || !shaped_like(a[0], type, g.rows, g.cols, d) || !shaped_like(a[2], type, g.rows, g.cols, u) || !shaped_like(a[3], type, g.rows, g.cols, dg) ||
+        !shaped_like(a[4], type, g.rows, g.cols, du) || !stream(a[5], s))
+        return not_here();
+    return call([&] {
+        return reinterpret_cast<SiluGateBackward>(g_entry[kSiluGateBackward])(d.p, d.ld, g.p, g.ld, u.p, u.ld, type, g.rows, g.cols, dg.p, dg.ld, du.p, du.ld, stream_of(s));
+    });
+}
+// A, scaleA, W, scaleW, bias, out, stream
+PyObject *int8_gemm(PyObject *const *a) {
+    Rows A, W, o;
+    void *sa, *sw, *bias = nullptr;
+    int type;
+    int64_t s;
+    if (!rows_of(a[0], at::kChar, 2, A) || !rows_of(a[2], at::kChar, 2, W) || A.cols != W.cols || !vector_of(a[1], at::kFloat, A.rows, sa) ||
+        !vector_of(a[3], at::kFloat, W.rows, sw) || (a[4] != Py_None && !vector_of(a[4], at::kFloat, W.rows, bias)) || !floats_of(a[5], o, type) || o.rows != A.rows ||
+        o.cols != W.rows || !stream(a[6], s))
+        return not_here();
+    return call([&] {
+        return reinterpret_cast<Int8Gemm>(g_entry[kInt8Gemm])(as<int8_t>(A), A.ld, static_cast<float *>(sa), as<int8_t>(W), W.ld, static_cast<float *>(sw),
+                                                              static_cast<float *>(bias), o.p, o.ld, type, A.rows, W.rows, A.cols, stream_of(s));
+    });
+}
+// x, scale_x, logits, top, W1, scale1, W2, scale2, out, workspace, stream
+PyObject *int8_moe(PyObject *const *a) {
+    Rows x, l, o;
+    void *sx;
+    int32_t top;
+    int type, type_l;
+    int64_t s;
+    const at::Tensor *const W1 = tensor(a[4], at::kChar, 3), *const s1 = tensor(a[5], at::kFloat, 2), *const W2 = tensor(a[6], at::kChar, 3), *const s2 = tensor(a[7], at::kFloat, 2),
+                            *const ws = tensor(a[9], at::kByte, 1);
+    // (dense weights: others go the general way)
+    if (!W1 || !s1 || !W2 || !s2 || !ws || !W1->is_contiguous() || !W2->is_contiguous() || !s1->is_contiguous() || !s2->is_contiguous() || !ws->is_contiguous()) return not_here();
+    const int64_t E = W1->size(0), F = W2->size(2);
+    if (!rows_of(a[0], at::kChar, 2, x) || !vector_of(a[1], at::kFloat, x.rows, sx) || !floats_of(a[2], l, type_l) || type_l != 0 || l.rows != x.rows || l.cols != E ||
+        E > INT32_MAX || !integer32(a[3], top) || W1->size(1) != 2 * F || W1->size(2) != x.cols || W2->size(0) != E || W2->size(1) != x.cols || s1->size(0) != E ||
+        s1->size(1) != 2 * F || s2->size(0) != E || s2->size(1) != x.cols || !floats_of(a[8], o, type) || o.rows != x.rows || o.cols != x.cols || !stream(a[10], s))
+        return not_here();
+    const int8_t *const w1 = static_cast<const int8_t *>(W1->data_ptr()), *const w2 = static_cast<const int8_t *>(W2->data_ptr());
+    const float *const f1 = static_cast<const float *>(s1->data_ptr()), *const f2 = static_cast<const float *>(s2->data_ptr());
+    void *const w = ws->data_ptr();
+    const size_t bytes = (size_t)ws->numel();
+    return call([&] {
+        return reinterpret_cast<Int8Moe>(g_entry[kInt8Moe])(as<int8_t>(x), x.ld, static_cast<float *>(sx), as<float>(l), l.ld, x.rows, (int)E, top, x.cols, F, w1, x.cols, f1, w2, F, f2,
+                                                            o.p, o.ld, type, w, bytes, stream_of(s));
+    });
+}
+
 // (C++ errors, of a tensor that has no memory for instance, are the general path's)
 template <PyObject *(*kCall)(PyObject *const *), Py_ssize_t kArgs, int kEntry>
 PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n) {
@@ -179,7 +317,7 @@ PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n) {
 }
 // The addresses of the entry points, in the order of the enumeration above
 PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t n) {
-    for (Py_ssize_t i = 0; i < n && i < 6; ++i) {
+    for (Py_ssize_t i = 0; i < n && i < kEntries; ++i) {
         g_entry[i] = PyLong_AsVoidPtr(args[i]);
         if (PyErr_Occurred()) return nullptr;
     }
@@ -198,6 +336,12 @@ PyMethodDef kMethods[] = {
     {"binary_gemm_sign", function(entry<binary_gemm_sign, 8, kBinaryGemmSign>), METH_FASTCALL, nullptr},
     {"bitplane_gemm", function(entry<bitplane_gemm, 9, kBitplaneGemm>), METH_FASTCALL, nullptr},
     {"bitplane_conv2d", function(entry<bitplane_conv2d, 11, kConv2d>), METH_FASTCALL, nullptr},
+    {"rms_norm_quant", function(entry<rms_norm_quant, 8, kRmsNormQuant>), METH_FASTCALL, nullptr},
+    {"rms_norm_backward", function(entry<rms_norm_backward, 9, kRmsNormBackward>), METH_FASTCALL, nullptr},
+    {"silu_gate_quant", function(entry<silu_gate_quant, 5, kSiluGateQuant>), METH_FASTCALL, nullptr},
+    {"silu_gate_backward", function(entry<silu_gate_backward, 6, kSiluGateBackward>), METH_FASTCALL, nullptr},
+    {"int8_gemm", function(entry<int8_gemm, 7, kInt8Gemm>), METH_FASTCALL, nullptr},
+    {"int8_moe", function(entry<int8_moe, 11, kInt8Moe>), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
