@@ -1,6 +1,8 @@
 // Matrix product of int8 codes with one scale for each row of either operand: out[m][n] = scaleA[m] scaleW[n] sum_k A[m][k] W[n][k] + bias[n], written as
 // fp32, fp16 or bf16.  The sums are exact int32 (v_mfma_i32_*_i8); the scales and the bias are applied in fp32 on the way out, rounded once.
-#include "qnn_int8.h"
+#include <cmath>
+
+#include "qnn_int8_panel.h"
 
 namespace qnn {
 namespace int8 {
@@ -10,47 +12,79 @@ using rows::bf16;
 using rows::f16;
 using rows::kVec;
 
-template <typename T>
-struct Args {
-    const int8_t *A, *W;
-    const float *scaleA, *scaleW, *bias;  // bias may be null
-    T *out;
-    int64_t lda, ldw, ldo, M, N, K;
-};
-
-// ---------------------------------------------------------------------------------------------------------------- few rows
-// Up to 16 kTiles rows of A: a workgroup has 16 weight rows, its waves every kWaves-th step of 64 codes, and adds its waves' sums in LDS.
-template <typename T, int kTiles, int kWaves>
-__global__ __launch_bounds__(64 * kWaves) void gemm_few_kernel(const Args<T> a) {
-    __shared__ int32_t sums[kWaves][16 * kTiles][17];
-    const int wave = threadIdx.x >> 6, r = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
-    const int64_t n0 = (int64_t)blockIdx.x * 16, m0 = (int64_t)blockIdx.y * (16 * kTiles);
-    const int8_t *w_row[1], *x_row[kTiles];
-    w_row[0] = a.W + min(n0 + r, a.N - 1) * a.ldw;
+// 16 kCols weight rows against 16 kTiles rows of A a workgroup, its waves every kWaves-th step of 128 codes, each through its own ring in LDS
+template <typename T, int kCols, int kTiles, int kWaves, int kStages, Layout kLayout>
+__global__ __launch_bounds__(64 * kWaves) void gemm_stream_kernel(const Args<T> a, const Tiles tiles) {
+    typedef Stream<kCols, kTiles, kStages, kLayout> S;
+    constexpr int kRows = 16 * kTiles, kColumns = 16 * kCols, kPitch = kColumns + 4, kHalf = kWaves / 2 > 0 ? kWaves / 2 : 1;
+    constexpr int kJoin = kHalf * kRows * kPitch * 4, kLds = S::kBytes * kWaves > kJoin ? S::kBytes * kWaves : kJoin;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[kLds];
+    uint32_t tm, tn;
+    tile_of_block(blockIdx.x, tiles, tm, tn);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    const int64_t m0 = (int64_t)tm * kRows, n0 = (int64_t)tn * kColumns;
+    S s;
+    s.lds = lds + wave * S::kBytes;
+    s.x_base = a.A, s.K = (uint32_t)a.K;
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t) x_row[t] = a.A + min(m0 + 16 * t + r, a.M - 1) * a.lda;
-    v4i acc[1][kTiles] = {};
-    multiply_rows<1, kTiles, 4>(w_row, x_row, a.K, 64 * wave, 64 * kWaves, acc);
+    for (int h = 0; h < 2; ++h) {
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t)
+        for (int c = 0; c < kCols; ++c) s.off[c][h] = (typename S::Offset)(min(n0 + 16 * c + 8 * h + (lane >> 3), a.N - 1) * a.ldw);
 #pragma unroll
-        for (int v = 0; v < 4; ++v) sums[wave][16 * t + r][4 * g + v] = acc[0][t][v];
+        for (int t = 0; t < kTiles; ++t) s.off[kCols + t][h] = (typename S::Offset)(min(m0 + 16 * t + 8 * h + (lane >> 3), a.M - 1) * a.lda);
+    }
+    v4i acc[kCols][kTiles] = {};
+    s.sums(a.W, 128u * wave, 128u * kWaves, acc);
+    __syncthreads();  // (every wave is done with its ring)
+    int32_t(*const sums)[kRows][kPitch] = reinterpret_cast<int32_t(*)[kRows][kPitch]>(lds);
+    auto put = [&](int at) __attribute__((always_inline)) {
+#pragma unroll
+        for (int c = 0; c < kCols; ++c)
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) *reinterpret_cast<v4i *>(&sums[at][16 * t + r][16 * c + 4 * g]) = acc[c][t];
+    };
+    // the upper half of the waves hands its sums to the lower half, and the sums of these are added where they are written
+    if (wave >= kHalf) put(wave - kHalf);
     __syncthreads();
-    for (int i = threadIdx.x; i < 256 * kTiles; i += 64 * kWaves) {
-        const int64_t m = m0 + (i >> 4), n = n0 + (i & 15);
-        if (m >= a.M || n >= a.N) continue;
-        int32_t s = 0;
+    if (wave < kHalf) {
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) s += sums[w][i >> 4][i & 15];
-        float y = (float)s * a.scaleA[m] * a.scaleW[n];
-        if (a.bias) y += a.bias[n];
-        a.out[m * a.ldo + n] = (T)y;
+        for (int c = 0; c < kCols; ++c)
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) acc[c][t] += *reinterpret_cast<const v4i *>(&sums[wave][16 * t + r][16 * c + 4 * g]);
+        put(wave);
+    }
+    __syncthreads();
+    constexpr int kFours = kColumns / 4;  // four columns a lane
+    for (int i = threadIdx.x; i < kRows * kFours; i += 64 * kWaves) {
+        const int row = i / kFours, col = 4 * (i % kFours);
+        const int64_t m = m0 + row, n = n0 + col, here = a.N - n;
+        if (m >= a.M || here <= 0) continue;
+        v4i sum = {0, 0, 0, 0};
+#pragma unroll
+        for (int w = 0; w < kHalf; ++w) sum += *reinterpret_cast<const v4i *>(&sums[w][row][col]);
+        const float sa = a.scaleA[m];
+        struct Four {
+            T e[4];
+        } four;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int64_t at = min(n + e, a.N - 1);
+            four.e[e] = (T)((float)sum[e] * sa * a.scaleW[at] + (a.bias ? a.bias[at] : 0.0f));
+        }
+        T *const to = a.out + m * a.ldo + n;
+        if (here >= 4) {
+            __builtin_memcpy(to, &four, sizeof four);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 3; ++e)
+                if (e < here) to[e] = four.e[e];
+        }
     }
 }
 
-// ---------------------------------------------------------------------------------------------------------------- tiles
-// 128 x 128 on four waves of 64 x 64; groups of 128 codes through registers to LDS, two buffers; rows of any length at any address.  16-byte piece c of
-// row r sits at piece c xor (r / 2 mod 8): the 16 rows that a read serves at a time lie on different banks.
+// 128 x 128 on four waves of 64 x 64, two workgroups on a compute unit; groups of 128 codes through registers to LDS, two buffers; rows of any length at
+// any address (K >= 16).  A group's loads are sent two groups ahead (one ahead, their latency was half of the time: 1999 x 3001 x 2500 38.2 -> 34.4 us).  16-byte piece
+// c of row r sits at piece c xor (r / 2 mod 8): the 16 rows that a read serves at a time lie on different banks.
 constexpr int kTile = 128, kGroup = 128, kPanel = kTile * kGroup;
 
 template <typename T>
@@ -68,49 +102,58 @@ __global__ __launch_bounds__(256, 2) void gemm_tile_kernel(const Args<T> a, cons
         src[i] = a.A + min(m0 + (t >> 3) + 32 * i, a.M - 1) * a.lda;
         src[4 + i] = a.W + min(n0 + (t >> 3) + 32 * i, a.N - 1) * a.ldw;
     }
-    v4i in[8];
-    auto fetch = [&](int64_t k) __attribute__((always_inline)) {
-        if (k + kGroup <= a.K) {
+    auto fetch = [&](int64_t k, v4i (&in)[8]) __attribute__((always_inline)) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) __builtin_memcpy(&in[i], src[i] + k + 16 * piece, 16);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) in[i] = load16(src[i], k + 16 * piece, a.K);
-        }
+        for (int i = 0; i < 8; ++i) in[i] = load_window(src[i], k + 16 * piece, a.K);
     };
-    auto put = [&](int buf) __attribute__((always_inline)) {
+    auto put = [&](int buf, v4i (&in)[8], int64_t k) __attribute__((always_inline)) {
+        if (k + kGroup > a.K) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) in[i] = in_place(in[i], k + 16 * piece, a.K);
+        }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const int r = (t >> 3) + 32 * (i & 3);
-            *reinterpret_cast<v4i *>(&lds[buf][(i >> 2) * kPanel + r * kGroup + 16 * (piece ^ ((r >> 1) & 7))]) = in[i];
+            const int row = (t >> 3) + 32 * (i & 3);
+            *reinterpret_cast<v4i *>(&lds[buf][(i >> 2) * kPanel + row * kGroup + 16 * (piece ^ ((row >> 1) & 7))]) = in[i];
         }
     };
-    v16i acc[2][2] = {};
-    const int r = lane & 31, kg = lane >> 5;
-    fetch(0);
-    put(0);
-    __syncthreads();
-    int buf = 0;
-    for (int64_t k = 0; k < a.K; k += kGroup, buf ^= 1) {
-        const bool more = k + kGroup < a.K;
-        if (more) fetch(k + kGroup);
+    v4i acc[4][4] = {};  // [n block][m block] of 16 x 16
+    const int r = lane & 15, g = lane >> 4;
+    auto multiply = [&](int buf) __attribute__((always_inline)) {
+        v4i x[2][4], w[2][4];
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            v4i x[2], w[2];
-            const int at = 16 * ((2 * s + kg) ^ ((r >> 1) & 7));
+        for (int h = 0; h < 2; ++h) {
+            const int at = r * kGroup + 16 * ((4 * h + g) ^ ((r >> 1) & 7));
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                x[i] = *reinterpret_cast<const v4i *>(&lds[buf][(64 * wm + 32 * i + r) * kGroup + at]);
-                w[i] = *reinterpret_cast<const v4i *>(&lds[buf][kPanel + (64 * wn + 32 * i + r) * kGroup + at]);
+            for (int i = 0; i < 4; ++i) {
+                x[h][i] = *reinterpret_cast<const v4i *>(&lds[buf][(64 * wm + 16 * i) * kGroup + at]);
+                w[h][i] = *reinterpret_cast<const v4i *>(&lds[buf][kPanel + (64 * wn + 16 * i) * kGroup + at]);
             }
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[i], x[j], acc[i][j], 0, 0, 0);
         }
-        if (more) put(buf ^ 1);
-        __syncthreads();
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[h][i], x[h][j], acc[i][j], 0, 0, 0);
+    };
+    v4i even[8], odd[8];
+    fetch(0, even);
+    fetch(kGroup, odd);
+    put(0, even, 0);
+    // at the top of a turn: group k in buffer 0, the loads of the next in `odd` under way
+    for (int64_t k = 0; k < a.K; k += 2 * kGroup) {
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // (written and, the other buffer, read; loads stay under way)
+        fetch(k + 2 * kGroup, even);
+        multiply(0);
+        if (k + kGroup >= a.K) break;
+        put(1, odd, k + kGroup);
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        fetch(k + 3 * kGroup, odd);
+        multiply(1);
+        if (k + 2 * kGroup < a.K) put(0, even, k + 2 * kGroup);
     }
+    __syncthreads();
     // A wave's sums of 32 rows pass through its part of LDS and leave as rows of 64 columns, 8 columns a lane
     constexpr int kPitch = 64 + 4;
     float *const stage = reinterpret_cast<float *>(&lds[0][0]) + wave * 32 * kPitch;
@@ -125,12 +168,12 @@ __global__ __launch_bounds__(256, 2) void gemm_tile_kernel(const Args<T> a, cons
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int v = 0; v < 16; v += 4) {
-                float *const to = stage + r * kPitch + 32 * i + 2 * v + 4 * kg;
+            for (int h = 0; h < 2; ++h) {
+                float *const to = stage + (16 * h + r) * kPitch + 16 * i + 4 * g;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) to[e] = (float)acc[i][j][v + e];
+                for (int e = 0; e < 4; ++e) to[e] = (float)acc[i][2 * j + h][e];
             }
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();
@@ -144,7 +187,17 @@ __global__ __launch_bounds__(256, 2) void gemm_tile_kernel(const Args<T> a, cons
                 float y[kVec];
 #pragma unroll
                 for (int e = 0; e < kVec; ++e) y[e] = stage[row * kPitch + 8 * (lane & 7) + e] * sa * sw[e] + bias[e];
-                rows::store_values(a.out + m * a.ldo + n, y, n_here);
+                T *const to = a.out + m * a.ldo + n;
+                rows::Raw<T> out;
+#pragma unroll
+                for (int e = 0; e < kVec; ++e) out.e[e] = (T)y[e];
+                if (n_here >= kVec) {
+                    __builtin_memcpy(to, &out, sizeof out);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < kVec; ++e)
+                        if (e < n_here) to[e] = out.e[e];
+                }
             }
         }
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -153,19 +206,60 @@ __global__ __launch_bounds__(256, 2) void gemm_tile_kernel(const Args<T> a, cons
     }
 }
 
+// The ways a product can go, by rows and columns of a workgroup's tile, and about how long each takes (us): start + more (R - 1) + k R K / 1024, with R the
+// rounds of one tile a compute unit.  Fitted to 66 products of 8 .. 5000 rows, 256 .. 4096 columns and K of 512 .. 7168 each, where the way that comes out
+// ahead is 1.4 % (any rows: 0.9 %) slower than the fastest in the mean.  (us of the fastest ways at N = K = 4096, M = 16: 16 x 16 5.7, 64 x 16 6.2; 64: 7.2
+// of 64 x 16, 8.3 and 7.7 of those beside it; 128: 64 x 32 8.1, 64 x 64 10.6; 256: 64 x 64 11.5, panels 12.7, 64 x 32 14.1; 512: panels of 64 x 64 17.0, of
+// 128 x 128 24.6; 1200: 36.0 and 28.5; 5000: 128 x 128 86, 256 x 256 90; 8192 x 8192 x 8192: 524 and 417.)
+enum WayId { kStream16x16, kStream64x16, kStream64x32, kStream64x64, kPanel64, kPanel128, kPanel256, kTile128 };
+struct Way {
+    WayId id;
+    int rows, columns;
+    double start, more, k;
+};
+constexpr Way kWaysOfPieces[] = {{kStream16x16, 16, 16, 2.7, 0.56, 0.276}, {kStream64x16, 64, 16, 3.1, 1.95, 0.743}, {kStream64x32, 64, 32, 3.3, 2.37, 0.924},
+                                 {kStream64x64, 64, 64, 4.3, 3.93, 1.306}, {kPanel64, 64, 64, 3.6, 0.03, 1.838},     {kPanel128, 128, 128, 4.1, 0.0, 4.254},
+                                 {kPanel256, 256, 256, 6.4, 9.10, 8.518}};
+constexpr Way kWaysOfAny[] = {{kStream16x16, 16, 16, 2.8, 0.25, 0.706}, {kStream64x16, 64, 16, 3.8, 0.98, 1.650}, {kStream64x32, 64, 32, 4.4, 3.44, 2.090},
+                              {kStream64x64, 64, 64, 6.1, 5.48, 2.843}, {kTile128, 128, 128, 7.1, 3.11, 6.853}};
+template <int kCount>
+const Way &fastest(const Way (&ways)[kCount], int64_t M, int64_t N, int64_t K) {
+    const Way *best = nullptr;
+    double least = 0.0;
+    for (const Way &w : ways) {
+        const double rounds = std::ceil((double)ceil_div(M, w.rows) * (double)ceil_div(N, w.columns) / compute_units());
+        const double us = w.start + w.more * (rounds - 1.0) + w.k * rounds * (double)K / 1024.0;
+        if (!best || us < least) best = &w, least = us;
+    }
+    return *best;
+}
+
 template <typename T>
 int launch(const Args<T> &a, hipStream_t s) {
-    if (a.M <= 64) {
-        const int64_t blocks = ceil_div(a.N, 16);
-        if (blocks > 0x7FFFFFFFLL) return fail(QNN_ERR_SHAPE, "int8_gemm: N = %lld", (long long)a.N);
-        const dim3 grid((unsigned)blocks);
-        if (a.M <= 16) return QNN_LAUNCH("int8_gemm", (gemm_few_kernel<T, 1, 8>), grid, dim3(512), 0, s, a);
-        if (a.M <= 32) return QNN_LAUNCH("int8_gemm", (gemm_few_kernel<T, 2, 8>), grid, dim3(512), 0, s, a);
-        return QNN_LAUNCH("int8_gemm", (gemm_few_kernel<T, 4, 8>), grid, dim3(512), 0, s, a);
+    const bool pieces = in_pieces(a.A, a.lda, a.M, a.K) && in_pieces(a.W, a.ldw, a.N, a.K), any = !pieces && a.K >= 16;
+    const Way &w = pieces ? fastest(kWaysOfPieces, a.M, a.N, a.K) : (any ? fastest(kWaysOfAny, a.M, a.N, a.K) : kWaysOfAny[0]);
+    const int64_t tm = ceil_div(a.M, w.rows), tn = ceil_div(a.N, w.columns);
+    // (8 columns of tiles and what lies in them have 32 bits)
+    if (tm > 0x7FFFFFFFLL || tn > 0x0FFFFFFFLL || tm * tn > 0x7FFFFFFFLL) return fail(QNN_ERR_SHAPE, "int8_gemm: M = %lld, N = %lld", (long long)a.M, (long long)a.N);
+    const Tiles tiles = make_tiles(tm, tn);
+    const dim3 grid((unsigned)(tm * tn));
+    auto stream = [&](auto on_pieces, auto on_any) { return QNN_LAUNCH("int8_gemm", (pieces ? on_pieces : on_any), grid, dim3(512), 0, s, a, tiles); };
+    auto panels = [&](auto kernel, int threads, int per_unit) {
+        const int64_t most = (int64_t)compute_units() * per_unit;
+        return QNN_LAUNCH("int8_gemm", kernel, dim3((unsigned)(tm * tn < most ? tm * tn : most)), dim3(threads), 0, s, a, tiles, (uint32_t)ceil_div(a.K, panel::kRow));
+    };
+    if (!pieces && !any) return QNN_LAUNCH("int8_gemm", (gemm_stream_kernel<T, 1, 1, 8, 1, kShortRows>), grid, dim3(512), 0, s, a, tiles);
+    switch (w.id) {
+    case kStream16x16: return stream(gemm_stream_kernel<T, 1, 1, 8, 2, kPieces>, gemm_stream_kernel<T, 1, 1, 8, 2, kAny>);
+    case kStream64x16: return stream(gemm_stream_kernel<T, 1, 4, 8, 2, kPieces>, gemm_stream_kernel<T, 1, 4, 8, 1, kAny>);
+    case kStream64x32: return stream(gemm_stream_kernel<T, 2, 4, 8, 1, kPieces>, gemm_stream_kernel<T, 2, 4, 8, 1, kAny>);
+    case kStream64x64: return stream(gemm_stream_kernel<T, 4, 4, 8, 1, kPieces>, gemm_stream_kernel<T, 4, 4, 8, 1, kAny>);
+    case kPanel64: return panels(panel::gemm_panel_kernel<T, panel::Tiny>, panel::Tiny::kThreads, panel::Tiny::kPerUnit);
+    case kPanel128: return panels(panel::gemm_panel_kernel<T, panel::Small>, panel::Small::kThreads, panel::Small::kPerUnit);
+    case kPanel256: return panels(panel::gemm_panel_kernel<T, panel::Large>, panel::Large::kThreads, panel::Large::kPerUnit);
+    case kTile128: return QNN_LAUNCH("int8_gemm", gemm_tile_kernel<T>, grid, dim3(256), 0, s, a, tiles);
     }
-    const int64_t tm = ceil_div(a.M, kTile), tn = ceil_div(a.N, kTile);
-    if (tm > 0x7FFFFFFFLL || tn > 0x7FFFFFFLL || tm * tn > 0x7FFFFFFFLL) return fail(QNN_ERR_SHAPE, "int8_gemm: M = %lld, N = %lld", (long long)a.M, (long long)a.N);
-    return QNN_LAUNCH("int8_gemm", gemm_tile_kernel<T>, dim3((unsigned)(tm * tn)), dim3(256), 0, s, a, make_tiles(tm, tn));
+    return fail(QNN_ERR_UNSUPPORTED, "int8_gemm: no way");
 }
 
 }  // namespace

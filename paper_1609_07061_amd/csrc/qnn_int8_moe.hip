@@ -16,6 +16,8 @@ using rows::Quantizer;
 
 static_assert(QNN_MOE_MAX_TOKENS == 64, "one lane a token");
 
+constexpr int kRingBytes = 72 * 1024;  // LDS of the first kernel's operands: two workgroups on a compute unit
+
 struct Route {  // a choice of a token: `weight` is exp(logit - largest logit); NaN: the token's logits say nothing; 0: takes no part
     int32_t expert;
     float weight;
@@ -33,9 +35,8 @@ struct MoeArgs {
     int64_t chunks;
 };
 
-// Lane t: where expert e stands among the choices of token t, 0 the first (top or more: not chosen), and its weight
-__device__ __forceinline__ int rank_of(const MoeArgs &a, int e, int t, float &weight) {
-    const float *const l = a.logits + (int64_t)(t < a.tokens ? t : 0) * a.ld_logits;
+// Where expert e stands among the choices of a token with these logits, 0 the first (top or more: not chosen), and its weight
+__device__ __forceinline__ int rank_of(const float *l, int experts, int e, float &weight) {
     const float mine = l[e];
     auto key = [](float v) __attribute__((always_inline)) {  // an unsigned integer in the order of the values; NaN somewhere, but a total order
         const uint32_t b = __float_as_uint(v + 0.0f);        // (-0 counts as +0)
@@ -45,7 +46,7 @@ __device__ __forceinline__ int rank_of(const MoeArgs &a, int e, int t, float &we
     int rank = 0;
     float top = -INFINITY;
     bool nan = false;
-    for (int j = 0; j < a.experts; ++j) {
+    for (int j = 0; j < experts; ++j) {
         const float v = l[j];
         const uint32_t k = key(v);
         rank += k > own || (k == own && j < e);
@@ -56,35 +57,28 @@ __device__ __forceinline__ int rank_of(const MoeArgs &a, int e, int t, float &we
     return rank;
 }
 
-template <int kTiles>
-__global__ __launch_bounds__(256) void moe_gate_up_kernel(const MoeArgs a) {
-    constexpr int kWaves = 4;
-    __shared__ int32_t sums[kWaves][2][16 * kTiles][17];
-    __shared__ int list[64], slot_of[64];
-    const int e = blockIdx.y, wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
-    float weight;
-    const int rank = rank_of(a, e, lane, weight);
-    const bool mine = lane < a.tokens && rank < a.top;
-    if (mine && blockIdx.x == 0 && wave == 0) a.route[lane * a.top + rank] = Route{e, weight};
-    const bool chosen = mine && weight > 0.0f;
-    const uint64_t who = __ballot(chosen);
-    const int count = __popcll(who);
-    if (count == 0) return;
-    if (wave == 0 && chosen) {
-        const int at = __popcll(who & ((1ull << lane) - 1ull));
-        list[at] = lane;
-        slot_of[at] = lane * a.top + rank;
-    }
-    __syncthreads();
-    const int64_t f0 = (int64_t)blockIdx.x * 16;
-    const int8_t *w_row[2], *x_row[kTiles];
-    const int64_t f_row = min(f0 + r, a.F - 1);
-#pragma unroll
-    for (int c = 0; c < 2; ++c) w_row[c] = a.W1 + ((int64_t)e * 2 * a.F + c * a.F + f_row) * a.ld_w1;
-#pragma unroll
-    for (int t = 0; t < kTiles; ++t) x_row[t] = a.x + (int64_t)list[min(16 * t + r, count - 1)] * a.ldx;
+// kTiles of 16 tokens: what a workgroup of the first kernel does once it knows its tokens
+template <int kTiles, Layout kLayout>
+__device__ __forceinline__ void gate_up(const MoeArgs &a, int e, int chunk, const int *list, const int *slot_of, int count, uint8_t *lds) {
+    constexpr int kWaves = 4, kStages = kTiles == 1 ? 3 : (kTiles == 2 ? 2 : 1);
+    typedef Stream<2, kTiles, kStages, kLayout> S;
+    static_assert(S::kBytes * kWaves <= kRingBytes && kWaves * 2 * 16 * kTiles * 17 * 4 <= kRingBytes, "");
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    const int64_t f0 = (int64_t)chunk * 16;
     v4i acc[2][kTiles] = {};
-    multiply_rows<2, kTiles, (kTiles == 1 ? 4 : 2)>(w_row, x_row, a.H, 64 * wave, 64 * kWaves, acc);
+    S s;
+    s.lds = lds + wave * S::kBytes;
+    s.x_base = a.x, s.K = (uint32_t)a.H;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c) s.off[c][h] = (typename S::Offset)((c * a.F + min(f0 + 8 * h + (lane >> 3), a.F - 1)) * a.ld_w1);
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) s.off[2 + t][h] = (typename S::Offset)(list[min(16 * t + 8 * h + (lane >> 3), count - 1)] * a.ldx);
+    }
+    s.sums(a.W1 + (int64_t)e * 2 * a.F * a.ld_w1, 128u * wave, 128u * kWaves, acc);
+    __syncthreads();
+    int32_t(*const sums)[2][16 * kTiles][17] = reinterpret_cast<int32_t(*)[2][16 * kTiles][17]>(lds);
 #pragma unroll
     for (int c = 0; c < 2; ++c)
 #pragma unroll
@@ -92,7 +86,7 @@ __global__ __launch_bounds__(256) void moe_gate_up_kernel(const MoeArgs a) {
 #pragma unroll
             for (int v = 0; v < 4; ++v) sums[wave][c][16 * t + r][4 * g + v] = acc[c][t][v];
     __syncthreads();
-    for (int i = threadIdx.x; i < 16 * count; i += 256) {  // (16 lanes of a wave share a token)
+    for (int i = threadIdx.x; i < 16 * count; i += 64 * kWaves) {  // (16 lanes of a wave share a token)
         const int m = i >> 4, c = i & 15;
         const int64_t f = f0 + c;
         float y = 0.0f;
@@ -109,106 +103,281 @@ __global__ __launch_bounds__(256) void moe_gate_up_kernel(const MoeArgs a) {
         uint32_t top = magnitude(y);
 #pragma unroll
         for (int d = 8; d >= 1; d >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d));
-        if (c == 0) a.tops[(int64_t)slot_of[m] * a.chunks + blockIdx.x] = top;
+        if (c == 0) a.tops[(int64_t)slot_of[m] * a.chunks + chunk] = top;
     }
 }
 
-template <typename T, int kTiles>
-__global__ __launch_bounds__(512) void moe_down_kernel(const MoeArgs a, T *out) {
-    constexpr int kWaves = 8, kRows = 16 * kTiles, kSlots = kRows * QNN_MOE_MAX_TOP;
-    constexpr int kChunk = kTiles == 1 ? 2048 : 1024, kPitch = kChunk + 16;  // codes of the inner width that are in LDS at a time
-    __shared__ __attribute__((aligned(16))) uint8_t codes[kRows * kPitch];
-    __shared__ int32_t sums[kWaves][kRows][17];
-    __shared__ float result[kSlots][16];
+// Grid: 16 columns of the inner width x as many experts as can be chosen.  Where those are fewer than there are, a workgroup finds the one that is its own
+// among the chosen (a workgroup for each of them that ended at once: 11.4 us for one token and two of 8 experts of 4096 x 2048, 8.9 like this).
+template <Layout kLayout>
+__global__ __launch_bounds__(256) void moe_gate_up_kernel(const MoeArgs a, int chosen_at_most) {
+    __shared__ __attribute__((aligned(16))) uint8_t lds[kRingBytes];
+    __shared__ int list[64], slot_of[64], any[QNN_MOE_MAX_EXPERTS];
+    const int t = threadIdx.x, wave = t >> 6, lane = t & 63, chunk = (int)(blockIdx.x / (uint32_t)chosen_at_most);
+    int e = (int)(blockIdx.x % (uint32_t)chosen_at_most);
+    // the logits, rows of an odd length: lanes that read a column meet different banks
+    float *const logits = reinterpret_cast<float *>(lds);
+    const int pitch = a.experts | 1;
+    static_assert(QNN_MOE_MAX_TOKENS * (QNN_MOE_MAX_EXPERTS + 1) * 4 <= kRingBytes, "");
+    for (int i0 = t; i0 < a.tokens * a.experts; i0 += 1024) {
+        float v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int i = min(i0 + 256 * j, a.tokens * a.experts - 1), tok = (int)((uint32_t)i / (uint32_t)a.experts);
+            v[j] = a.logits[(int64_t)tok * a.ld_logits + (i - tok * a.experts)];
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int i = min(i0 + 256 * j, a.tokens * a.experts - 1), tok = (int)((uint32_t)i / (uint32_t)a.experts);
+            logits[tok * pitch + (i - tok * a.experts)] = v[j];
+        }
+    }
+    any[t] = 0;
+    static_assert(QNN_MOE_MAX_EXPERTS == 256, "one thread an expert");
+    __syncthreads();
+    float weight;
+    if (chosen_at_most < a.experts) {
+        for (int i = t; i < a.tokens * a.experts; i += 256) {
+            const int tok = (int)((uint32_t)i / (uint32_t)a.experts), x = i - tok * a.experts;
+            if (rank_of(logits + tok * pitch, a.experts, x, weight) < a.top) any[x] = 1;
+        }
+        __syncthreads();
+        int left = e;
+        e = -1;
+        for (int x0 = 0; x0 < a.experts && e < 0; x0 += 64) {
+            uint64_t who = __ballot(x0 + lane < a.experts && any[x0 + lane] != 0);
+            const int here = __popcll(who);
+            if (left < here) {
+                for (; left > 0; --left) who &= who - 1ull;
+                e = x0 + __ffsll((unsigned long long)who) - 1;
+            }
+            left -= here;
+        }
+        if (e < 0) return;
+        e = __builtin_amdgcn_readfirstlane(e);
+    }
+    const int rank = rank_of(logits + min(lane, a.tokens - 1) * pitch, a.experts, e, weight);
+    const bool mine = lane < a.tokens && rank < a.top;
+    if (mine && chunk == 0 && wave == 0) a.route[lane * a.top + rank] = Route{e, weight};
+    const bool chosen = mine && weight > 0.0f;
+    const uint64_t who = __ballot(chosen);
+    const int count = __popcll(who);
+    if (count == 0) return;
+    if (wave == 0 && chosen) {
+        const int at = __popcll(who & ((1ull << lane) - 1ull));
+        list[at] = lane;
+        slot_of[at] = lane * a.top + rank;
+    }
+    __syncthreads();  // (the logits' place is free too)
+    if (count <= 16)
+        gate_up<1, kLayout>(a, e, chunk, list, slot_of, count, lds);
+    else if (count <= 32)
+        gate_up<2, kLayout>(a, e, chunk, list, slot_of, count, lds);
+    else
+        gate_up<4, kLayout>(a, e, chunk, list, slot_of, count, lds);
+}
+
+// The choices in the order of their experts; the experts that have any, and where each one's choices start (one more than there are).  One wave.
+__device__ __forceinline__ int in_order(const MoeArgs &a, const Route *route, int slots, int *order, int *active, int *start) {
+    const int lane = threadIdx.x & 63;
+    int at = 0, n = 0;
+    for (int e = 0; e < a.experts; ++e) {
+        const int before = at;
+        for (int s0 = 0; s0 < slots; s0 += 64) {
+            const bool is = s0 + lane < slots && route[s0 + lane].expert == e;
+            const uint64_t who = __ballot(is);
+            if (is) order[at + __popcll(who & ((1ull << lane) - 1ull))] = s0 + lane;
+            at += __popcll(who);
+        }
+        if (at > before) {
+            if (lane == 0) active[n] = e, start[n] = before;
+            ++n;
+        }
+    }
+    if (lane == 0) start[n] = at;
+    return n;
+}
+
+// Activations become codes in LDS, `chunk` of the inner width at a time and as many experts at a time as have up to kCodes / (chunk + 16) choices
+// together (mostly everything at once); then every wave goes through its steps of k of one expert after the other without a break in its loads, and adds
+// what it has of an expert to the results in LDS (whole numbers: in any order).
+template <typename T, int kSlots, int kCodes, int kStages, Layout kLayout>
+__global__ __launch_bounds__(512) void moe_down_kernel(const MoeArgs a, T *out, int chunk) {
+    constexpr int kWaves = 8;
+    constexpr bool kFactors = kSlots <= 128;  // what a result is multiplied with has room in LDS
+    typedef Stream<1, 0, kStages, kLayout> S;
+    __shared__ __attribute__((aligned(16))) uint8_t ring[kWaves * S::kBytes], codes[kCodes];
+    __shared__ int32_t result[kSlots][16];
+    __shared__ float factor[kFactors ? kSlots : 1][16];
     __shared__ Route route[kSlots];
     __shared__ float mul[kSlots], pre[kSlots], scale[kSlots];
-    __shared__ int order[kSlots], start[QNN_MOE_MAX_EXPERTS + 1];
-    const int t = threadIdx.x, wave = t >> 6, lane = t & 63, r = lane & 15, g = lane >> 4, slots = a.tokens * a.top;
-    const int64_t n0 = (int64_t)blockIdx.x * 16, n_row = min(n0 + r, a.H - 1);
-    for (int s = t; s < slots; s += 512) {
-        const Route c = a.route[s];
-        route[s] = Route{c.weight > 0.0f ? c.expert : -1, c.weight};
-    }
-    __syncthreads();
-    // how each activation is quantized
-    for (int s = wave; s < slots; s += kWaves) {
-        if (route[s].expert < 0) continue;
-        uint32_t top = 0u;
-        for (int64_t c = lane; c < a.chunks; c += 64) top = max(top, a.tops[(int64_t)s * a.chunks + c]);
+    __shared__ int order[kSlots], active[QNN_MOE_MAX_EXPERTS], start[QNN_MOE_MAX_EXPERTS + 1], n_active;
+    const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6), lane = t & 63, r = lane & 15, g = lane >> 4, slots = a.tokens * a.top;
+    const int64_t n0 = (int64_t)blockIdx.x * 16;
+    const uint32_t F = (uint32_t)a.F;
+    const int pitch = chunk + 16, most = kCodes / pitch;
+    const bool at_once = slots <= most && F <= (uint32_t)chunk;  // then rows of codes are in the order of the choices, else in that of the experts
+    // 1024 activations of a row by a wave: four loads of whole lines; kItems of these under way
+    constexpr int kItems = 4;
+    float v[kItems][4][4];
+    auto fetch = [&](float (&to)[4][4], int m, uint32_t f_first) __attribute__((always_inline)) {
+        const float *const p = a.act + (int64_t)m * a.F;
 #pragma unroll
-        for (int d = 32; d >= 1; d >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d));
-        const Quantizer q(top, 1.0f);
-        if (lane == 0) mul[s] = q.zero ? 0.0f : q.mul, pre[s] = q.zero ? 0.0f : q.pre, scale[s] = q.scale;
+        for (uint32_t u = 0; u < 4u; ++u) {
+            const uint32_t f = f_first + 4u * lane + 256u * u;
+            if (f + 4u <= F) {
+                __builtin_memcpy(to[u], p + f, 16);
+            } else {
+#pragma unroll
+                for (uint32_t j = 0; j < 4u; ++j) to[u][j] = f + j < F ? p[f + j] : 0.0f;
+            }
+        }
+    };
+    auto put = [&](const float (&from)[4][4], int m, int row, uint32_t at, uint32_t whole) __attribute__((always_inline)) {
+        Quantizer q(0u, 1.0f);
+        q.mul = mul[m], q.pre = pre[m], q.zero = pre[m] == 0.0f;
+#pragma unroll
+        for (uint32_t u = 0; u < 4u; ++u) {
+            const uint32_t f = at + 4u * lane + 256u * u;
+            if (f < whole) *reinterpret_cast<uint32_t *>(&codes[row * pitch + (int)f]) = q.four(from[u][0], from[u][1], from[u][2], from[u][3]);
+        }
+    };
+    const uint32_t all_parts = ((uint32_t)chunk + 1023u) / 1024u;
+    if (at_once) {
+#pragma unroll
+        for (int j = 0; j < kItems; ++j) {
+            const uint32_t i = (uint32_t)(wave + kWaves * j);
+            if (i < (uint32_t)slots * all_parts) fetch(v[j], (int)(i / all_parts), i % all_parts * 1024u);
+        }
     }
-    // the choices in the order of their experts
+    // One wave finds the order of the choices; the others how each activation is quantized (for a choice that takes no part: nothing that is used).
     if (wave == 0) {
-        int at = 0;
-        for (int e = 0; e < a.experts; ++e) {
-            if (lane == 0) start[e] = at;
-            for (int s0 = 0; s0 < slots; s0 += 64) {
-                const bool is = s0 + lane < slots && route[s0 + lane].expert == e;
-                const uint64_t who = __ballot(is);
-                if (is) order[at + __popcll(who & ((1ull << lane) - 1ull))] = s0 + lane;
-                at += __popcll(who);
-            }
+        for (int s = lane; s < slots; s += 64) {
+            const Route c = a.route[s];
+            route[s] = Route{c.weight > 0.0f ? c.expert : -1, c.weight};
         }
-        if (lane == 0) start[a.experts] = at;
-    }
-    __syncthreads();
-    for (int e = 0; e < a.experts; ++e) {
-        const int first = start[e], count = start[e + 1] - first;
-        if (count == 0) continue;
-        const int8_t *const w_row = a.W2 + ((int64_t)e * a.H + n_row) * a.ld_w2;
-        v4i acc[kTiles] = {};
-        for (int64_t f0 = 0; f0 < a.F; f0 += kChunk) {
-            const int here = (int)min((int64_t)kChunk, a.F - f0), groups = (here + 63) / 64 * 16;  // groups of four codes, zeros up to a whole step
-            for (int i = t; i < count * groups; i += 512) {
-                const int m = i / groups, f = 4 * (i - m * groups), s = order[first + m];
-                const float *const p = a.act + (int64_t)s * a.F + f0 + f;
-                float v[4];
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        const int n = in_order(a, route, slots, order, active, start);
+        if (lane == 0) n_active = n;
+    } else {
+        for (int i = t - 64; i < 16 * slots; i += 448) result[i >> 4][i & 15] = 0;
+        for (int s = (t - 64) >> 4; s < slots; s += 28) {  // 16 lanes each
+            uint32_t top = 0u;
+            const uint32_t *const from = a.tops + (int64_t)s * a.chunks;
+            for (int64_t c0 = 0; c0 < a.chunks; c0 += 128) {
+                uint32_t w[8];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) v[j] = f + j < here ? p[j] : 0.0f;
-                uint32_t w = 0u;
-                if (pre[s] != 0.0f) {
-                    Quantizer q(0u, 1.0f);
-                    q.mul = mul[s], q.pre = pre[s], q.zero = false;
-                    w = q.four(v[0], v[1], v[2], v[3]);
-                }
-                *reinterpret_cast<uint32_t *>(&codes[m * kPitch + f]) = w;
+                for (int j = 0; j < 8; ++j) w[j] = from[min(c0 + 16 * j + r, a.chunks - 1)];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) top = max(top, w[j]);
             }
-            __syncthreads();
-            for (int k = 64 * wave; k < here; k += 64 * kWaves) {
-                const v4i w = load16(w_row, f0 + k + 16 * g, a.F);
 #pragma unroll
-                for (int j = 0; j < kTiles; ++j) {
-                    const v4i x = *reinterpret_cast<const v4i *>(&codes[(16 * j + r) * kPitch + k + 16 * g]);
-                    acc[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w, x, acc[j], 0, 0, 0);
-                }
-            }
-            __syncthreads();
-        }
-#pragma unroll
-        for (int j = 0; j < kTiles; ++j)
-#pragma unroll
-            for (int v = 0; v < 4; ++v) sums[wave][16 * j + r][4 * g + v] = acc[j][v];
-        __syncthreads();
-        for (int i = t; i < 16 * count; i += 512) {
-            const int s = order[first + (i >> 4)];
-            int32_t total = 0;
-#pragma unroll
-            for (int w = 0; w < kWaves; ++w) total += sums[w][i >> 4][i & 15];
-            result[s][i & 15] = (float)total * scale[s] * a.scale2[(int64_t)e * a.H + min(n0 + (i & 15), a.H - 1)];
+            for (int d = 8; d >= 1; d >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d));
+            const Quantizer q(top, 1.0f);
+            if (r == 0) mul[s] = q.zero ? 0.0f : q.mul, pre[s] = q.zero ? 0.0f : q.pre, scale[s] = q.scale;
         }
     }
     __syncthreads();
-    for (int i = t; i < 16 * a.tokens; i += 512) {
-        const int tok = i >> 4;
-        const int64_t n = n0 + (i & 15);
-        if (n >= a.H) continue;
-        float whole = 0.0f, y = 0.0f;
+    const int experts = __builtin_amdgcn_readfirstlane(n_active);
+    // share of a choice in its token's output and the scales of its product (whole: the sum of the weights, NaN where the logits say nothing)
+    auto share = [&](int m, int64_t n, float whole) __attribute__((always_inline)) {
+        return route[m].weight > 0.0f ? route[m].weight / whole * (scale[m] * a.scale2[(int64_t)route[m].expert * a.H + n]) : 0.0f;
+    };
+    auto sum_of = [&](int tok) __attribute__((always_inline)) {
+        float whole = 0.0f;
         for (int j = 0; j < a.top; ++j) whole += route[tok * a.top + j].weight;
-        for (int j = 0; j < a.top; ++j)
-            if (route[tok * a.top + j].weight > 0.0f) y = __fmaf_rn(route[tok * a.top + j].weight / whole, result[tok * a.top + j][i & 15], y);
+        return whole;
+    };
+    S s;
+    s.lds = ring + wave * S::kBytes;
+    s.K = F;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) s.off[0][h] = (typename S::Offset)(min(n0 + 8 * h + (lane >> 3), a.H - 1) * a.ld_w2);
+    for (int from = 0, to; from < experts; from = to) {
+        // the experts whose activations are in LDS together
+        const int first_row = __builtin_amdgcn_readfirstlane(start[from]);
+        to = at_once ? experts : from + 1;
+        while (to < experts && __builtin_amdgcn_readfirstlane(start[to + 1]) - first_row <= most) ++to;
+        const int n_rows = __builtin_amdgcn_readfirstlane(start[to]) - first_row;
+        for (uint32_t f0 = 0; f0 < F; f0 += (uint32_t)chunk) {
+            // this wave's steps: expert by expert, `per` each; the loads' cursor and the products'
+            const uint32_t end = min(F, f0 + (uint32_t)chunk), k0 = f0 + 128u * wave;
+            const int per = end > k0 ? (int)((end - k0 - 1u) / (128u * kWaves)) + 1 : 0, steps = per * (to - from);
+            int send_x = from, send_step = 0, x = from, step = 0;
+            const int8_t *w_base = a.W2;
+            auto base = [&](int) __attribute__((always_inline)) {
+                if (send_step == 0) w_base = a.W2 + (int64_t)__builtin_amdgcn_readfirstlane(active[send_x]) * a.H * a.ld_w2;
+                return w_base;
+            };
+            auto at = [&](int) __attribute__((always_inline)) {  // (called after base)
+                const uint32_t k = k0 + (uint32_t)send_step * (128u * kWaves);
+                if (++send_step == per) send_step = 0, ++send_x;
+                return k;
+            };
+            s.start(steps, base, at);
+            // activations to codes, zeros from their end to a whole step
+            const uint32_t whole = min((uint32_t)chunk, (F - f0 + 127u) / 128u * 128u), parts = (whole + 1023u) / 1024u;
+            const uint32_t items = (uint32_t)(at_once ? slots : n_rows) * parts;
+            for (uint32_t i0 = wave; i0 < items; i0 += kWaves * kItems) {
+                if (!at_once || i0 != (uint32_t)wave) {
+#pragma unroll
+                    for (uint32_t j = 0; j < kItems; ++j) {
+                        const uint32_t i = i0 + kWaves * j;
+                        if (i < items) fetch(v[j], at_once ? (int)(i / parts) : order[first_row + (int)(i / parts)], f0 + i % parts * 1024u);
+                    }
+                }
+#pragma unroll
+                for (uint32_t j = 0; j < kItems; ++j) {
+                    const uint32_t i = i0 + kWaves * j;
+                    if (i < items) put(v[j], at_once ? (int)(i / parts) : order[first_row + (int)(i / parts)], (int)(i / parts), i % parts * 1024u, whole);
+                }
+            }
+            if (kFactors && from == 0 && f0 == 0u) {
+                for (int i = t; i < 16 * slots; i += 512) factor[i >> 4][i & 15] = share(i >> 4, min(n0 + (i & 15), a.H - 1), sum_of((i >> 4) / a.top));
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // (weights may still be on their way)
+            v4i acc[4];
+            int row[4], first = 0, count = 0;
+            s.run(steps, base, at, [&](int, const typename S::Operands &o) __attribute__((always_inline)) {
+                if (step == 0) {
+                    first = __builtin_amdgcn_readfirstlane(start[x]), count = __builtin_amdgcn_readfirstlane(start[x + 1]) - first;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int pos = first + min(16 * j + r, count - 1);
+                        row[j] = (at_once ? order[pos] : pos - first_row) * pitch, acc[j] = v4i{0, 0, 0, 0};
+                    }
+                }
+                const int k = (int)(k0 - f0) + step * (128 * kWaves) + 16 * g;
+                const bool last = ++step == per;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (16 * j < count) {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+                            acc[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(o.w[h][0], *reinterpret_cast<const v4i *>(&codes[row[j] + k + 64 * h]), acc[j], 0, 0, 0);
+                        if (last && 16 * j + r < count) {
+                            const int m = order[first + 16 * j + r];
+#pragma unroll
+                            for (int w = 0; w < 4; ++w) atomicAdd(&result[m][4 * g + w], acc[j][w]);
+                        }
+                    }
+                if (last) step = 0, ++x;
+            });
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        }
+    }
+    for (int q = t; q < 16 * a.tokens; q += 512) {
+        const int tok = q >> 4, c = q & 15;
+        const int64_t n = n0 + c;
+        if (n >= a.H) continue;
+        const float whole = sum_of(tok);
+        float y = 0.0f;
+        for (int j = 0; j < a.top; ++j) {
+            const int m = tok * a.top + j;
+            if (route[m].weight > 0.0f) y = __fmaf_rn(kFactors ? factor[m][c] : share(m, n, whole), (float)result[m][c], y);
+        }
         out[(int64_t)tok * a.ldo + n] = (T)(whole == whole ? y : whole);
     }
 }
@@ -218,12 +387,29 @@ size_t route_bytes(int64_t tokens, int top) { return round_up_256((size_t)(token
 size_t act_bytes(int64_t tokens, int top, int64_t F) { return round_up_256((size_t)(tokens * top) * (size_t)F * 4); }
 size_t tops_bytes(int64_t tokens, int top, int64_t F) { return round_up_256((size_t)(tokens * top) * (size_t)ceil_div(F, 16) * 4); }
 
-template <int kTiles>
 int launch_moe(const MoeArgs &a, void *out, int type, hipStream_t s) {
-    if (int rc = QNN_LAUNCH("int8_moe", moe_gate_up_kernel<kTiles>, dim3((unsigned)a.chunks, (unsigned)a.experts), dim3(256), 0, s, a)) return rc;
+    const int most = a.tokens * a.top < a.experts ? a.tokens * a.top : a.experts;
+    const dim3 grid((unsigned)(a.chunks * most));
+    const bool pieces1 = in_pieces(a.x, a.ldx, a.tokens, a.H) && in_pieces(a.W1, a.ld_w1, 2 * a.F, a.H), pieces2 = in_pieces(a.W2, a.ld_w2, a.H, a.F);
+    auto up = pieces1 ? moe_gate_up_kernel<kPieces> : (a.H >= 16 ? moe_gate_up_kernel<kAny> : moe_gate_up_kernel<kShortRows>);
+    if (int rc = QNN_LAUNCH("int8_moe", up, grid, dim3(256), 0, s, a, most)) return rc;
+    const int64_t whole = ceil_div(a.F, 128) * 128;
+    const int slots = a.tokens * a.top;
     return rows::with_type(type, [&](auto tag) {
         typedef decltype(tag) T;
-        return QNN_LAUNCH("int8_moe", (moe_down_kernel<T, kTiles>), dim3((unsigned)ceil_div(a.H, 16)), dim3(512), 0, s, a, static_cast<T *>(out));
+        const dim3 columns((unsigned)ceil_div(a.H, 16)), threads(512);
+        T *const o = static_cast<T *>(out);
+        // few choices: two workgroups on a compute unit; many: LDS holds the results of all and the codes of one expert's 64 tokens at least
+        constexpr int kFew = 16 * 1024, kMore = 88 * 1024, kMost = 64 * (1024 + 16);
+        auto launch = [&](auto pieces, auto any, auto short_rows, int chunk) {
+            return QNN_LAUNCH("int8_moe", (pieces2 ? pieces : (a.F >= 16 ? any : short_rows)), columns, threads, 0, s, a, o, chunk);
+        };
+        if (slots <= 32 && slots * (whole + 16) <= kFew)
+            return launch(moe_down_kernel<T, 32, kFew, 3, kPieces>, moe_down_kernel<T, 32, kFew, 2, kAny>, moe_down_kernel<T, 32, kFew, 1, kShortRows>, (int)whole);
+        const int chunk = whole <= 1024 || (slots <= 128 && slots * (whole + 16) <= kMore) ? (int)whole : 1024;
+        if (slots <= 128)
+            return launch(moe_down_kernel<T, 128, kMore, 3, kPieces>, moe_down_kernel<T, 128, kMore, 2, kAny>, moe_down_kernel<T, 128, kMore, 1, kShortRows>, chunk);
+        return launch(moe_down_kernel<T, 512, kMost, 2, kPieces>, moe_down_kernel<T, 512, kMost, 2, kAny>, moe_down_kernel<T, 512, kMost, 1, kShortRows>, chunk);
     });
 }
 
@@ -262,5 +448,5 @@ extern "C" int qnn_int8_moe(const int8_t *x, int64_t ldx, const float *scale_x, 
     const int8::MoeArgs a = {x, W1, W2, scale_x, logits, scale1, scale2, ldx, ld_logits, ld_w1, ld_w2, H, F, ldo, (int)tokens, experts, top,
                              reinterpret_cast<int8::Route *>(ws), reinterpret_cast<float *>(ws + r), reinterpret_cast<uint32_t *>(ws + r + v), ceil_div(F, 16)};
     hipStream_t s = static_cast<hipStream_t>(stream);
-    return tokens <= 16 ? int8::launch_moe<1>(a, out, type, s) : int8::launch_moe<4>(a, out, type, s);
+    return int8::launch_moe(a, out, type, s);
 }

@@ -5,6 +5,8 @@
 // max |y| = r max |h gamma|: the sum and the maximum come from ONE pass over the row, which stays in registers, and the codes need no r at all.
 // The norm and the codes take h in fp32; the sum that is written is rounded once.
 // Bound by memory: 2 reads and a write of a 16-bit float and a write of a byte for each value.
+#include <type_traits>
+
 #include "qnn_rows.h"
 
 namespace qnn {
@@ -12,7 +14,7 @@ namespace {
 
 using namespace rows;
 
-template <typename T>
+template <typename T, bool kOnce>
 struct NormSource {
     struct Kept {
         float h[kVec];
@@ -23,12 +25,13 @@ struct NormSource {
     int64_t ldx, ldr, lds;
     bool gamma_f32;
     float eps;
-    __device__ __forceinline__ void load(int64_t row, int64_t k, int64_t n, float (&v)[kVec], Kept &kept, float &total) const {
-        const Raw<T> a = load_raw(x + row * ldx + k, n);
+    template <bool kShort>
+    __device__ __forceinline__ void load(int64_t row, const Window &w, int64_t K, float (&v)[kVec], Kept &kept) const {
+        const Raw<T> a = load_raw<kOnce, kShort>(x + row * ldx, w, K);
         float g[kVec];
-        load_either<T>(gamma, gamma_f32, k, n, g);
+        load_either<kShort, T>(gamma, gamma_f32, w, K, g);
         if (residual) {
-            const Raw<T> b = load_raw(residual + row * ldr + k, n);
+            const Raw<T> b = load_raw<kOnce, kShort>(residual + row * ldr, w, K);
 #pragma unroll
             for (int i = 0; i < kVec; ++i) kept.h[i] = (float)a.e[i] + (float)b.e[i];
         } else {
@@ -36,25 +39,25 @@ struct NormSource {
             for (int i = 0; i < kVec; ++i) kept.h[i] = (float)a.e[i];
         }
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) {
-            total = __fmaf_rn(kept.h[i], kept.h[i], total);
-            v[i] = kept.h[i] * g[i];
-        }
+        for (int i = 0; i < kVec; ++i) v[i] = kept.h[i] * g[i];
     }
+    __device__ __forceinline__ float add(const Kept &kept, int i, float sum) const { return __fmaf_rn(kept.h[i], kept.h[i], sum); }
     __device__ __forceinline__ float factor(float total, int64_t K) const {
         const float mean = total / (float)K;
         // (a mean beyond fp32 would give the factor 0 and a row of zeros)
         return magnitude(mean) < 0x7F800000u ? 1.0f / sqrtf(mean + eps) : __uint_as_float(0x7FC00000u);
     }
-    __device__ __forceinline__ void keep(int64_t row, int64_t k, int64_t n, const Kept &kept) const {
-        if (sum) store_values(sum + row * lds + k, kept.h, n);
+    template <bool kShort>
+    __device__ __forceinline__ void keep(int64_t row, const Window &w, int64_t K, const Kept &kept) const {
+        if (sum) store_values<kOnce, kShort>(sum + row * lds, w, K, kept.h);
     }
 };
 
 // Gradient.  With g the gradient at y and z one that reaches h by another way (the residual path):
 //   gh = r (gamma g - h r^2 mean(gamma g h)) + z,   ggamma = sum over the rows of g h r.
-// A workgroup (a wave, for short rows) takes every gridDim-th row, keeps its lanes' part of ggamma in registers over all of them and writes it once;
-// the second kernel adds these partial sums in a fixed order.  Up to kParts of them, so that they are a small part of what is moved.
+// A workgroup takes kGroups rows at a time, every gridDim-th such group, keeps its lanes' part of ggamma in registers over all of them and writes it once;
+// the second kernel adds these partial sums in a fixed order.  Up to kParts of them, so that they are a small part of what is moved.  (10000 x 4096 bf16
+// with a residual's gradient, 328 MB: two rows at a time 61.0 us, one 70.9; with the next row's loads sent ahead 71.5 and 68.3: more registers, fewer waves.)
 constexpr int kParts = 512;
 
 template <typename T>
@@ -69,46 +72,54 @@ struct NormGradArgs {
     float *parts;
 };
 
-template <typename T, int kThreads, int kPer>
-__global__ __launch_bounds__(kThreads >= 256 ? kThreads : 256) void rms_norm_backward_kernel(const NormGradArgs<T> a) {
-    constexpr int kRows = rows_per_block(kThreads);
-    __shared__ TwoSums shared[2][kThreads / 64];
-    const int lane = threadIdx.x % kThreads;
+// rows that a workgroup takes at a time, and its threads
+constexpr int groups_of(int threads) { return threads == 64 ? 4 : (threads == 256 ? 2 : 1); }
+
+template <typename T, int kThreads, int kPer, bool kOnce, bool kShort>
+__global__ __launch_bounds__(kThreads *groups_of(kThreads)) void rms_norm_backward_kernel(const NormGradArgs<T> a) {
+    constexpr int kGroups = groups_of(kThreads);
+    __shared__ TwoSums shared[kGroups][2][kThreads / 64];
+    __shared__ float joined[kGroups > 1 ? kThreads * kPer * kVec : 1];
+    const int lane = threadIdx.x % kThreads, group = threadIdx.x / kThreads;
     float gamma[kPer][kVec], acc[kPer][kVec];
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-        const int64_t k = (int64_t)(i * kThreads + lane) * kVec;
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) acc[i][e] = gamma[i][e] = 0.0f;
-        if (k < a.K) load_either<T>(a.gamma, a.gamma_f32, k, a.K - k, gamma[i]);
+        for (int e = 0; e < kVec; ++e) acc[i][e] = 0.0f;
+        load_either<kShort, T>(a.gamma, a.gamma_f32, Window((int64_t)(i * kThreads + lane) * kVec, a.K), a.K, gamma[i]);
     }
-    int turn = 0;
-    for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / kThreads; row < a.n_rows; row += (int64_t)gridDim.x * kRows) {
+    struct Row {
         Raw<T> h[kPer], g[kPer], z[kPer];
-        TwoSums s = {0.0f, 0.0f};
+    };
+    const int64_t step = (int64_t)gridDim.x * kGroups;
+    auto load = [&](int64_t row, Row &v) __attribute__((always_inline)) {
+        if (row >= a.n_rows) return;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
-            const int64_t k = (int64_t)(i * kThreads + lane) * kVec;
-            if (k < a.K) {
-                h[i] = load_raw(a.h + row * a.ldh + k, a.K - k);
-                g[i] = load_raw(a.grad + row * a.ldg + k, a.K - k);
-                if (a.grad_sum) z[i] = load_raw(a.grad_sum + row * a.ldz + k, a.K - k);
-            }
+            const Window w((int64_t)(i * kThreads + lane) * kVec, a.K);
+            v.h[i] = load_raw<kOnce, kShort>(a.h + row * a.ldh, w, a.K);
+            v.g[i] = load_raw<kOnce, kShort>(a.grad + row * a.ldg, w, a.K);
+            if (a.grad_sum) v.z[i] = load_raw<kOnce, kShort>(a.grad_sum + row * a.ldz, w, a.K);
         }
+    };
+    int turn = 0;
+    auto finish = [&](int64_t row, const Row &v) __attribute__((always_inline)) {
+        TwoSums s = {0.0f, 0.0f};
+        if (row < a.n_rows) {
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            const int64_t k = (int64_t)(i * kThreads + lane) * kVec;
-            if (k < a.K) {
+            for (int i = 0; i < kPer; ++i) {
+                const Window w((int64_t)(i * kThreads + lane) * kVec, a.K);
 #pragma unroll
                 for (int e = 0; e < kVec; ++e) {
-                    const float hv = (float)h[i].e[e];
+                    const float hv = e >= w.skip && (!kShort || w.from + e < a.K) ? (float)v.h[i].e[e] : 0.0f;
                     s.a = __fmaf_rn(hv, hv, s.a);
-                    s.b = __fmaf_rn(gamma[i][e] * (float)g[i].e[e], hv, s.b);
+                    s.b = __fmaf_rn(gamma[i][e] * (float)v.g[i].e[e], hv, s.b);
                 }
             }
         }
-        s = across<kThreads>(s, TwoSums::join, shared, turn);
+        s = across<kThreads>(s, TwoSums::join, shared[group], turn);
         turn ^= 1;
+        if (row >= a.n_rows) return;
         const float r = 1.0f / sqrtf(s.a / (float)a.K + a.eps), c = r * r * (s.b / (float)a.K);
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
@@ -117,48 +128,63 @@ __global__ __launch_bounds__(kThreads >= 256 ? kThreads : 256) void rms_norm_bac
                 float o[kVec];
 #pragma unroll
                 for (int e = 0; e < kVec; ++e) {
-                    const float hv = (float)h[i].e[e], gv = (float)g[i].e[e];
+                    const float hv = (float)v.h[i].e[e], gv = (float)v.g[i].e[e];
                     o[e] = r * __fmaf_rn(-hv, c, gamma[i][e] * gv);
-                    if (a.grad_sum) o[e] += (float)z[i].e[e];
+                    if (a.grad_sum) o[e] += (float)v.z[i].e[e];
                     acc[i][e] = __fmaf_rn(gv, hv * r, acc[i][e]);
                 }
-                store_values(a.out + row * a.ldo + k, o, a.K - k);
+                store_values<kOnce, kShort>(a.out + row * a.ldo, Window(k, a.K), a.K, o);
             }
         }
+    };
+    // (every group of a workgroup makes the same number of turns, with a row or without)
+    const int64_t first = (int64_t)blockIdx.x * kGroups;
+    Row v;
+    for (int64_t row = first; row < a.n_rows; row += step) {
+        load(row + group, v);
+        finish(row + group, v);
     }
     float *part = a.parts + (int64_t)blockIdx.x * a.K;
-    if constexpr (kRows == 1) {
+    if constexpr (kGroups == 1) {
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             const int64_t k = (int64_t)(i * kThreads + lane) * kVec;
-            if (k < a.K) store_values(part + k, acc[i], a.K - k);
+            if (k < a.K) store_values<false, kShort>(part, Window(k, a.K), a.K, acc[i]);
         }
-    } else {  // the waves' sums, one after the other
-        __shared__ float joined[kThreads * kPer * kVec];
-        for (int w = 0; w < kRows; ++w) {
-            if ((int)threadIdx.x / kThreads == w) {
+    } else {  // the groups' sums, one after the other
+        for (int w = 0; w < kGroups; ++w) {
+            if (group == w) {
 #pragma unroll
                 for (int i = 0; i < kPer; ++i)
 #pragma unroll
                     for (int e = 0; e < kVec; ++e) {
-                        float &to = joined[(i * kThreads + lane) * kVec + e];
+                        float &to = joined[(i * kVec + e) * kThreads + lane];  // (neighbouring lanes, neighbouring banks)
                         to = w == 0 ? acc[i][e] : to + acc[i][e];
                     }
             }
             __syncthreads();
         }
-        for (int k = threadIdx.x; k < a.K; k += blockDim.x) part[k] = joined[k];
+        for (int k = threadIdx.x; k < a.K; k += blockDim.x) {
+            const int v = k / kVec, e = k - (int)Window((int64_t)v * kVec, a.K).from;  // value k: lane, and place in its window
+            part[k] = joined[((v / kThreads) * kVec + e) * kThreads + v % kThreads];
+        }
     }
 }
 
-// ggamma[k] = sum of n_parts rows of `parts`: 32 columns a workgroup, 32 lanes a column
+// ggamma[k] = sum of n_parts rows of `parts`: 32 columns a workgroup, 32 lanes a column, eight loads of each under way
 __global__ __launch_bounds__(1024) void add_parts_kernel(const float *parts, int n_parts, int64_t K, float *out) {
     __shared__ float sums[32][33];
     const int c = threadIdx.x & 31, g = threadIdx.x >> 5;
     const int64_t k = (int64_t)blockIdx.x * 32 + c;
     float s = 0.0f;
     if (k < K)
-        for (int p = g; p < n_parts; p += 32) s += parts[(int64_t)p * K + k];
+        for (int p0 = g; p0 < n_parts; p0 += 256) {
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = p0 + 32 * j < n_parts ? parts[(int64_t)(p0 + 32 * j) * K + k] : 0.0f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s += v[j];
+        }
     sums[g][c] = s;
     __syncthreads();
     float t = sums[c][g];  // column g, part c
@@ -171,12 +197,12 @@ __global__ __launch_bounds__(1024) void add_parts_kernel(const float *parts, int
 constexpr int64_t kWidest = 2048 * kVec;  // of the gradient, whose rows stay in registers
 int64_t parts_of(int64_t rows) { return rows < kParts ? rows : kParts; }
 
-template <typename T, int kThreads, int kPer>
+template <typename T, int kThreads, int kPer, bool kShort = false>
 int launch_backward(const NormGradArgs<T> &a, float *grad_gamma, hipStream_t s) {
-    const int64_t blocks = ceil_div(a.n_rows, rows_per_block(kThreads)), parts = blocks < kParts ? blocks : kParts;
-    if (int rc = QNN_LAUNCH("rms_norm_backward", (rms_norm_backward_kernel<T, kThreads, kPer>), dim3((unsigned)parts),
-                            dim3(kThreads >= 256 ? kThreads : 256), 0, s, a))
-        return rc;
+    const int64_t blocks = ceil_div(a.n_rows, groups_of(kThreads)), parts = blocks < kParts ? blocks : kParts;
+    const bool once = beyond_caches((a.grad_sum ? 4.0 : 3.0) * sizeof(T) * (double)a.n_rows * (double)a.K);
+    auto kernel = once ? rms_norm_backward_kernel<T, kThreads, kPer, !kShort, kShort> : rms_norm_backward_kernel<T, kThreads, kPer, false, kShort>;
+    if (int rc = QNN_LAUNCH("rms_norm_backward", kernel, dim3((unsigned)parts), dim3(kThreads * groups_of(kThreads)), 0, s, a)) return rc;
     return QNN_LAUNCH("rms_norm_backward", add_parts_kernel, dim3((unsigned)ceil_div(a.K, 32)), dim3(1024), 0, s, a.parts, (int)parts, a.K, grad_gamma);
 }
 
@@ -202,9 +228,13 @@ extern "C" int qnn_rms_norm_quant(const void *x, int64_t ldx, const void *residu
         return fail(QNN_ERR_ALIGN, "rms_norm_quant: pointer not aligned to its type");
     return rows::with_type(type, [&](auto tag) {
         typedef decltype(tag) T;
-        const NormSource<T> src = {static_cast<const T *>(x), static_cast<const T *>(residual), static_cast<T *>(sum), gamma, ldx, ld_residual, ld_sum,
-                                   gamma_type == QNN_F32, eps};
-        return rows::launch_quant_rows("rms_norm_quant", src, rows, K, codes, ld_codes, scale, static_cast<hipStream_t>(stream));
+        auto launch = [&](auto once) {
+            const NormSource<T, decltype(once)::value> src = {static_cast<const T *>(x), static_cast<const T *>(residual), static_cast<T *>(sum), gamma, ldx,
+                                                              ld_residual, ld_sum, gamma_type == QNN_F32, eps};
+            return rows::launch_quant_rows("rms_norm_quant", src, rows, K, codes, ld_codes, scale, static_cast<hipStream_t>(stream));
+        };
+        const double bytes = (w * (1.0 + (residual ? 1.0 : 0.0) + (sum ? 1.0 : 0.0)) + 1.0) * (double)rows * (double)K;
+        return rows::beyond_caches(bytes) ? launch(std::true_type{}) : launch(std::false_type{});
     });
 }
 
@@ -235,6 +265,7 @@ extern "C" int qnn_rms_norm_backward(const void *grad, int64_t ld_grad, const vo
         const NormGradArgs<T> a = {static_cast<const T *>(grad), static_cast<const T *>(h), static_cast<const T *>(grad_sum), static_cast<T *>(grad_h),
                                    gamma, ld_grad, ld_h, ld_grad_sum, ld_grad_h, gamma_type == QNN_F32, eps, rows, K, static_cast<float *>(workspace)};
         hipStream_t s = static_cast<hipStream_t>(stream);
+        if (K < kVec) return launch_backward<T, 64, 1, true>(a, grad_gamma, s);
         if (K <= 64 * kVec) return launch_backward<T, 64, 1>(a, grad_gamma, s);
         if (K <= 128 * kVec) return launch_backward<T, 64, 2>(a, grad_gamma, s);
         if (K <= 256 * kVec) return launch_backward<T, 256, 1>(a, grad_gamma, s);

@@ -19,40 +19,64 @@ template <typename T>
 struct Raw {
     T e[kVec];
 };
-// n (1 .. kVec) values from an address aligned to one value; the rest is zero.  Loads of whole groups are wide whatever the address.
-template <typename T>
-__device__ __forceinline__ Raw<T> load_raw(const T *p, int64_t n) {
+// The kVec values of a row of K that belong to the lane at k: the window from `from` on, of which the values before `skip` are another lane's (or nobody's).
+// A row's last window ends where the row does, so that every load is whole, wide and within the row; loads that a lane's place in the row decided upon
+// would have to be waited for one by one.  kShort: rows of fewer values than a window, loaded and stored one by one.
+struct Window {
+    int64_t from;
+    int skip;
+    __device__ __forceinline__ Window(int64_t k, int64_t K) : from(K < kVec ? k : (k < K - kVec ? k : K - kVec)), skip((int)((k - from) < kVec ? k - from : kVec)) {}
+};
+// kOnce: past the caches, for matrices that they could not hold anyway (10000 x 4096 bf16 and its residual to sum and codes, 287 MB: 88.6 -> 52.0 us; but
+// 60 MB of fp32 20 -> 22).
+typedef uint32_t Words4 __attribute__((ext_vector_type(4), aligned(2)));
+template <bool kOnce, bool kShort, typename T>
+__device__ __forceinline__ Raw<T> load_raw(const T *row, const Window &w, int64_t K) {
     Raw<T> r;
-    if (n >= kVec) {
-        __builtin_memcpy(&r, p, sizeof r);
-    } else {
+    if constexpr (kShort) {
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) r.e[i] = i < n ? p[i] : (T)0.0f;
+        for (int i = 0; i < kVec; ++i) r.e[i] = w.from + i < K ? row[w.from + i] : (T)0.0f;
+    } else if constexpr (kOnce) {
+        Words4 v[sizeof r / 16];
+#pragma unroll
+        for (int i = 0; i < (int)(sizeof r / 16); ++i) v[i] = __builtin_nontemporal_load(reinterpret_cast<const Words4 *>(row + w.from) + i);
+        __builtin_memcpy(&r, v, sizeof r);
+    } else {
+        __builtin_memcpy(&r, row + w.from, sizeof r);
     }
     return r;
 }
-template <typename T>
-__device__ __forceinline__ void store_values(T *p, const float (&v)[kVec], int64_t n) {
+template <bool kOnce, bool kShort, typename T>
+__device__ __forceinline__ void store_values(T *row, const Window &w, int64_t K, const float (&v)[kVec]) {
     Raw<T> r;
 #pragma unroll
     for (int i = 0; i < kVec; ++i) r.e[i] = (T)v[i];  // to nearest, ties to even
-    if (n >= kVec) {
-        __builtin_memcpy(p, &r, sizeof r);
+    if (!kShort && w.skip == 0) {
+        if constexpr (kOnce) {
+            Words4 u[sizeof r / 16];
+            __builtin_memcpy(u, &r, sizeof r);
+#pragma unroll
+            for (int i = 0; i < (int)(sizeof r / 16); ++i) __builtin_nontemporal_store(u[i], reinterpret_cast<Words4 *>(row + w.from) + i);
+        } else {
+            __builtin_memcpy(row + w.from, &r, sizeof r);
+        }
     } else {
 #pragma unroll
         for (int i = 0; i < kVec; ++i)
-            if (i < n) p[i] = r.e[i];
+            if (i >= w.skip && w.from + i < K) row[w.from + i] = r.e[i];
     }
 }
+// Whether a call's matrices, this many bytes together, are for the caches or not (256 MB on the card)
+inline bool beyond_caches(double bytes) { return bytes > 128e6; }
 // kVec values of fp32 or T, as is_f32 (the same for all lanes) says
-template <typename T>
-__device__ __forceinline__ void load_either(const void *p, bool is_f32, int64_t k, int64_t n, float (&v)[kVec]) {
+template <bool kShort, typename T>
+__device__ __forceinline__ void load_either(const void *p, bool is_f32, const Window &w, int64_t K, float (&v)[kVec]) {
     if (is_f32) {
-        const Raw<float> r = load_raw(static_cast<const float *>(p) + k, n);
+        const Raw<float> r = load_raw<false, kShort>(static_cast<const float *>(p), w, K);
 #pragma unroll
         for (int i = 0; i < kVec; ++i) v[i] = r.e[i];
     } else {
-        const Raw<T> r = load_raw(static_cast<const T *>(p) + k, n);
+        const Raw<T> r = load_raw<false, kShort>(static_cast<const T *>(p), w, K);
 #pragma unroll
         for (int i = 0; i < kVec; ++i) v[i] = (float)r.e[i];
     }
@@ -83,19 +107,28 @@ struct Quantizer {
         return zero ? 0u : code(a) | code(b) << 8 | code(c) << 16 | code(d) << 24;
     }
 };
-__device__ __forceinline__ void store_codes(int8_t *p, const Quantizer &q, const float (&v)[kVec], int64_t n) {
-    uint32_t w[2] = {q.four(v[0], v[1], v[2], v[3]), q.four(v[4], v[5], v[6], v[7])};
-    if (n >= kVec) {
-        __builtin_memcpy(p, w, sizeof w);
+template <bool kShort>
+__device__ __forceinline__ void store_codes(int8_t *row, const Window &at, int64_t K, const Quantizer &q, const float (&v)[kVec]) {
+    const uint32_t w[2] = {q.four(v[0], v[1], v[2], v[3]), q.four(v[4], v[5], v[6], v[7])};
+    if (!kShort && at.skip == 0) {
+        __builtin_memcpy(row + at.from, w, sizeof w);
     } else {
 #pragma unroll
         for (int i = 0; i < kVec; ++i)
-            if (i < n) p[i] = (int8_t)(w[i >> 2] >> (8 * (i & 3)));
+            if (i >= at.skip && at.from + i < K) row[at.from + i] = (int8_t)(w[i >> 2] >> (8 * (i & 3)));
     }
 }
 
-// 1 / (1 + exp(-x)) times x
-__device__ __forceinline__ float silu(float x) { return x / (1.0f + expf(-x)); }
+// 1 / (1 + exp(-x)), within 3 units in the last place; below 2^-126 it is 0.  exp(-x) = 2^n 2^f with n + f = -x log2(e), f to twice the digits.  Infinities have
+// the limits; a NaN is lost, and has to be in the factor beside.  (With expf
+// and a correctly rounded quotient the vector ALU bounds the gated activation: 47 us at 10000 x 4096, 205 MB.)
+__device__ __forceinline__ float sigmoid(float x) {
+    constexpr float kLog2e = 0x1.715476p+0f, kRest = 0x1.4ae0cp-26f;  // together log2(e)
+    const float y = __builtin_amdgcn_fmed3f(x, -1000.0f, 1000.0f), n = rintf(y * -kLog2e), f = __fmaf_rn(y, -kRest, __fmaf_rn(y, -kLog2e, -n));
+    const float e = __builtin_amdgcn_ldexpf(__builtin_amdgcn_exp2f(f), (int)n);
+    return __builtin_amdgcn_rcpf(1.0f + e);
+}
+__device__ __forceinline__ float silu(float x) { return x * sigmoid(x); }
 
 // Sums over the lanes that share a row, given to all of them: a wave, or a workgroup of kThreads, whose waves meet in `shared` (two buffers used in
 // turn: a wave writes one only behind the barrier after which every wave has read the other)
@@ -105,7 +138,7 @@ __device__ __forceinline__ V across(V v, Join join, V (*shared)[kThreads / 64], 
     for (int d = 32; d >= 1; d >>= 1) v = join(v, v.shuffled(d));
     if constexpr (kThreads > 64) {
         constexpr int kWaves = kThreads / 64;
-        if ((threadIdx.x & 63) == 0) shared[turn][threadIdx.x >> 6] = v;
+        if ((threadIdx.x & 63) == 0) shared[turn][threadIdx.x % kThreads >> 6] = v;
         __syncthreads();
         v = shared[turn][0];
 #pragma unroll
@@ -127,10 +160,10 @@ struct TwoSums {
 
 constexpr int rows_per_block(int threads) { return threads >= 256 ? 1 : 256 / threads; }
 
-// One row per kThreads lanes.  Source: `stats(values)` what a group of values adds to the sum; `load(row, k, n, values)` the values to be quantized, up
-// to the factor `factor(sum)`; `keep(row, k, n)` what else it writes, called once for every group after all were loaded.
-// kPer: groups of kVec values that a lane keeps in registers; 0: as many as there are, loaded a second time for the codes.
-template <typename Source, int kThreads, int kPer>
+// One row per kThreads lanes.  Source: `load<kShort>(row, window, K, values, kept)` the values to be quantized, up to the factor `factor(sum)`;
+// `add(kept, i, sum)` the sum with value i's part; `keep<kShort>(row, window, K, kept)` writes what else it does.
+// kPer: windows that a lane keeps in registers; 0: as many as there are, loaded a second time for the codes.
+template <typename Source, int kThreads, int kPer, bool kShort>
 __global__ __launch_bounds__(kThreads >= 256 ? kThreads : 256) void quant_rows_kernel(const Source src, int64_t n_rows, int64_t K, int8_t *codes,
                                                                                      int64_t ld_codes, float *scale) {
     __shared__ SumTop shared[2][kThreads / 64];
@@ -141,51 +174,57 @@ __global__ __launch_bounds__(kThreads >= 256 ? kThreads : 256) void quant_rows_k
     float v[kHeld][kVec];
     typename Source::Kept kept[kHeld];
     SumTop s = {0.0f, 0u};
-    auto take = [&](int i, int64_t k) __attribute__((always_inline)) {
-        src.load(row, k, K - k, v[i], kept[i], s.sum);
+    auto stats = [&](int i, const Window &w) __attribute__((always_inline)) {
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) s.top = max(s.top, magnitude(v[i][e]));
+        for (int e = 0; e < kVec; ++e) {
+            const bool mine = e >= w.skip && (!kShort || w.from + e < K);
+            s.sum = mine ? src.add(kept[i], e, s.sum) : s.sum;
+            s.top = max(s.top, mine ? magnitude(v[i][e]) : 0u);
+        }
+    };
+    auto give = [&](const Quantizer &q, int i, const Window &w) __attribute__((always_inline)) {
+        src.template keep<kShort>(row, w, K, kept[i]);
+        store_codes<kShort>(codes + row * ld_codes, w, K, q, v[i]);
     };
     if constexpr (kPer > 0) {
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            const int64_t k = (int64_t)(i * kThreads + lane) * kVec;
-            if (k < K) take(i, k);
-        }
+        for (int i = 0; i < kPer; ++i) src.template load<kShort>(row, Window((int64_t)(i * kThreads + lane) * kVec, K), K, v[i], kept[i]);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) stats(i, Window((int64_t)(i * kThreads + lane) * kVec, K));
     } else {
-        for (int64_t k = lane * kVec; k < K; k += kThreads * kVec) take(0, k);
+        for (int64_t k = lane * kVec; k < K; k += kThreads * kVec) {
+            src.template load<kShort>(row, Window(k, K), K, v[0], kept[0]);
+            stats(0, Window(k, K));
+        }
     }
     s = across<kThreads>(s, SumTop::join, shared, 0);
     const Quantizer q(s.top, src.factor(s.sum, K));
     if (lane == 0) scale[row] = q.scale;
-    auto give = [&](int i, int64_t k) __attribute__((always_inline)) {
-        src.keep(row, k, K - k, kept[i]);
-        store_codes(codes + row * ld_codes + k, q, v[i], K - k);
-    };
     if constexpr (kPer > 0) {
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             const int64_t k = (int64_t)(i * kThreads + lane) * kVec;
-            if (k < K) give(i, k);
+            if (k < K) give(q, i, Window(k, K));
         }
     } else {
         for (int64_t k = lane * kVec; k < K; k += kThreads * kVec) {
-            take(0, k);
-            give(0, k);
+            src.template load<kShort>(row, Window(k, K), K, v[0], kept[0]);
+            give(q, 0, Window(k, K));
         }
     }
 }
 
-template <typename Source, int kThreads, int kPer>
+template <typename Source, int kThreads, int kPer, bool kShort = false>
 int launch_shape(const char *what, const Source &src, int64_t n_rows, int64_t K, int8_t *codes, int64_t ld_codes, float *scale, hipStream_t s) {
     const int64_t blocks = ceil_div(n_rows, rows_per_block(kThreads));
     if (blocks > 0x7FFFFFFFLL) return fail(QNN_ERR_SHAPE, "%s: %lld rows", what, (long long)n_rows);
-    return QNN_LAUNCH(what, (quant_rows_kernel<Source, kThreads, kPer>), dim3((unsigned)blocks), dim3(kThreads >= 256 ? kThreads : 256), 0, s, src, n_rows,
+    return QNN_LAUNCH(what, (quant_rows_kernel<Source, kThreads, kPer, kShort>), dim3((unsigned)blocks), dim3(kThreads >= 256 ? kThreads : 256), 0, s, src, n_rows,
                       K, codes, ld_codes, scale);
 }
 // Lanes and groups by the length of a row
 template <typename Source>
 int launch_quant_rows(const char *what, const Source &src, int64_t n_rows, int64_t K, int8_t *codes, int64_t ld_codes, float *scale, hipStream_t s) {
+    if (K < kVec) return launch_shape<Source, 64, 1, true>(what, src, n_rows, K, codes, ld_codes, scale, s);
     if (K <= 64 * kVec) return launch_shape<Source, 64, 1>(what, src, n_rows, K, codes, ld_codes, scale, s);
     if (K <= 128 * kVec) return launch_shape<Source, 64, 2>(what, src, n_rows, K, codes, ld_codes, scale, s);
     if (K <= 256 * kVec) return launch_shape<Source, 256, 1>(what, src, n_rows, K, codes, ld_codes, scale, s);

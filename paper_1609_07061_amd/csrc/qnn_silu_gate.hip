@@ -1,6 +1,8 @@
 // Gated activation between the two products of a feed-forward block, y = up * gate / (1 + exp(-gate)), with int8 codes and one scale a row behind it
 // (what qnn_int8_gemm takes), and its gradient (straight through the quantizer, as Sec. 2.3 does for the sign).
 // Bound by memory: 2 reads of a 16-bit float and a write of a byte for each value; gradient: 3 reads and 2 writes.
+#include <type_traits>
+
 #include "qnn_rows.h"
 
 namespace qnn {
@@ -8,37 +10,42 @@ namespace {
 
 using namespace rows;
 
-template <typename T>
+template <typename T, bool kOnce>
 struct GateSource {
     struct Kept {};
     const T *gate, *up;
     int64_t ld_gate, ld_up;
-    __device__ __forceinline__ void load(int64_t row, int64_t k, int64_t n, float (&v)[kVec], Kept &, float &) const {
-        const Raw<T> a = load_raw(gate + row * ld_gate + k, n), b = load_raw(up + row * ld_up + k, n);
+    template <bool kShort>
+    __device__ __forceinline__ void load(int64_t row, const Window &w, int64_t K, float (&v)[kVec], Kept &) const {
+        const Raw<T> a = load_raw<kOnce, kShort>(gate + row * ld_gate, w, K), b = load_raw<kOnce, kShort>(up + row * ld_up, w, K);
 #pragma unroll
         for (int i = 0; i < kVec; ++i) v[i] = silu((float)a.e[i]) * (float)b.e[i];
     }
+    __device__ __forceinline__ float add(const Kept &, int, float sum) const { return sum; }
     __device__ __forceinline__ float factor(float, int64_t) const { return 1.0f; }
-    __device__ __forceinline__ void keep(int64_t, int64_t, int64_t, const Kept &) const {}
+    template <bool kShort>
+    __device__ __forceinline__ void keep(int64_t, const Window &, int64_t, const Kept &) const {}
 };
 
 // With s = 1 / (1 + exp(-gate)): ggate = g up s (1 + gate (1 - s)), gup = g gate s
-template <typename T>
+template <typename T, bool kOnce, bool kShort>
 __global__ __launch_bounds__(256) void silu_gate_backward_kernel(const T *grad, int64_t ldg, const T *gate, int64_t ld_gate, const T *up, int64_t ld_up,
                                                                  int64_t n_rows, int64_t F, int64_t groups, T *grad_gate, int64_t ld_ggate, T *grad_up,
                                                                  int64_t ld_gup) {
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n_rows * groups; i += (int64_t)gridDim.x * 256) {
-        const int64_t row = i / groups, k = (i - row * groups) * kVec, n = F - k;
-        const Raw<T> a = load_raw(gate + row * ld_gate + k, n), b = load_raw(up + row * ld_up + k, n), c = load_raw(grad + row * ldg + k, n);
+        const int64_t row = i / groups;
+        const Window w((i - row * groups) * kVec, F);
+        const Raw<T> a = load_raw<kOnce, kShort>(gate + row * ld_gate, w, F), b = load_raw<kOnce, kShort>(up + row * ld_up, w, F),
+                     c = load_raw<kOnce, kShort>(grad + row * ldg, w, F);
         float p[kVec], q[kVec];
 #pragma unroll
         for (int e = 0; e < kVec; ++e) {
-            const float x = (float)a.e[e], s = 1.0f / (1.0f + expf(-x)), g = (float)c.e[e];
+            const float x = (float)a.e[e], s = sigmoid(x), g = (float)c.e[e];
             p[e] = g * (float)b.e[e] * s * __fmaf_rn(x, 1.0f - s, 1.0f);
             q[e] = g * x * s;
         }
-        store_values(grad_gate + row * ld_ggate + k, p, n);
-        store_values(grad_up + row * ld_gup + k, q, n);
+        store_values<kOnce, kShort>(grad_gate + row * ld_ggate, w, F, p);
+        store_values<kOnce, kShort>(grad_up + row * ld_gup, w, F, q);
     }
 }
 
@@ -59,8 +66,11 @@ extern "C" int qnn_silu_gate_quant(const void *gate, int64_t ld_gate, const void
         return fail(QNN_ERR_ALIGN, "silu_gate_quant: pointer not aligned to its type");
     return rows::with_type(type, [&](auto tag) {
         typedef decltype(tag) T;
-        const GateSource<T> src = {static_cast<const T *>(gate), static_cast<const T *>(up), ld_gate, ld_up};
-        return rows::launch_quant_rows("silu_gate_quant", src, rows, F, codes, ld_codes, scale, static_cast<hipStream_t>(stream));
+        auto launch = [&](auto once) {
+            const GateSource<T, decltype(once)::value> src = {static_cast<const T *>(gate), static_cast<const T *>(up), ld_gate, ld_up};
+            return rows::launch_quant_rows("silu_gate_quant", src, rows, F, codes, ld_codes, scale, static_cast<hipStream_t>(stream));
+        };
+        return rows::beyond_caches((2.0 * w + 1.0) * (double)rows * (double)F) ? launch(std::true_type{}) : launch(std::false_type{});
     });
 }
 
@@ -79,7 +89,9 @@ extern "C" int qnn_silu_gate_backward(const void *grad, int64_t ld_grad, const v
     const int64_t groups = ceil_div(F, rows::kVec), blocks = ceil_div(rows * groups, 256);
     return rows::with_type(type, [&](auto tag) {
         typedef decltype(tag) T;
-        return QNN_LAUNCH("silu_gate_backward", silu_gate_backward_kernel<T>, dim3((unsigned)(blocks > 16384 ? 16384 : blocks)), dim3(256), 0,
+        auto kernel = rows::beyond_caches(5.0 * w * (double)rows * (double)F) ? silu_gate_backward_kernel<T, true, false> : silu_gate_backward_kernel<T, false, false>;
+        if (F < rows::kVec) kernel = silu_gate_backward_kernel<T, false, true>;
+        return QNN_LAUNCH("silu_gate_backward", kernel, dim3((unsigned)(blocks > 16384 ? 16384 : blocks)), dim3(256), 0,
                           static_cast<hipStream_t>(stream), static_cast<const T *>(grad), ld_grad, static_cast<const T *>(gate), ld_gate,
                           static_cast<const T *>(up), ld_up, rows, F, groups, static_cast<T *>(grad_gate), ld_grad_gate, static_cast<T *>(grad_up),
                           ld_grad_up);
