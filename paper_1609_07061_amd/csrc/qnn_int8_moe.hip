@@ -1,10 +1,11 @@
-// Mixture-of-experts layer on int8 codes for a few tokens, in two kernels.  What bounds it is reading the chosen experts' weights once.
+// Mixture-of-experts layer on int8 codes for a few tokens, in two kernels or three.  What bounds it is reading the chosen experts' weights once.
 //   moe_gate_up_kernel: a workgroup has 16 columns of one expert's inner width, that is 32 rows of W1, and all the tokens that chose the expert; which
 //     tokens these are it finds itself from the logits.  The activation goes to the workspace in fp32, beside the largest magnitude of each token's 16
 //     values; the expert's first workgroup also writes the tokens' weights.
-//   moe_down_kernel: a workgroup has 16 columns of the output, that is 16 rows of every expert's W2.  It quantizes the activations as it reads them (a
-//     row's scale is known once the first kernel has ended), multiplies expert by expert and adds the weighted results in the order of the choices.
-// Both give 16 x 16 blocks of sums to the matrix cores, with the weights on the row side, and split k over their waves.
+//   quant_rows_kernel (qnn_rows.h), for more than a few choices: the activations to codes.
+//   moe_down_kernel: a workgroup has 16 columns of the output, that is 16 rows of every expert's W2.  For a few choices it quantizes the activations itself
+//     (a row's scale is known once the first kernel has ended).  It multiplies expert by expert and adds the weighted results in the order of the choices.
+// Both products give 16 x 16 blocks of sums to the matrix cores, with the weights on the row side, and split k over their waves.
 #include "qnn_int8.h"
 
 namespace qnn {
@@ -28,11 +29,32 @@ struct MoeArgs {
     const float *scale_x, *logits, *scale1, *scale2;
     int64_t ldx, ld_logits, ld_w1, ld_w2, H, F, ldo;
     int tokens, experts, top;
-    // workspace: [tokens * top] routes, [tokens * top][F] activations, [tokens * top][ceil(F / 16)] largest magnitudes
+    // workspace: [tokens * top] routes, [tokens * top][F] activations, [tokens * top][ceil(F / 16)] largest magnitudes, then
     Route *route;
     float *act;
     uint32_t *tops;
     int64_t chunks;
+    // (for more than a few choices) [tokens * top][ld_codes] activations as codes and [tokens * top] scales
+    int8_t *codes;
+    float *scales;
+    int64_t ld_codes;
+};
+
+// Activations as they are, to codes (qnn_rows.h)
+struct PlainSource {
+    struct Kept {};
+    const float *x;
+    int64_t ld;
+    template <bool kShort>
+    __device__ __forceinline__ void load(int64_t row, const rows::Window &w, int64_t K, float (&v)[rows::kVec], Kept &) const {
+        const rows::Raw<float> r = rows::load_raw<false, kShort>(x + row * ld, w, K);
+#pragma unroll
+        for (int i = 0; i < rows::kVec; ++i) v[i] = r.e[i];
+    }
+    __device__ __forceinline__ float add(const Kept &, int, float sum) const { return sum; }
+    __device__ __forceinline__ float factor(float, int64_t) const { return 1.0f; }
+    template <bool kShort>
+    __device__ __forceinline__ void keep(int64_t, const rows::Window &, int64_t, const Kept &) const {}
 };
 
 // Where expert e stands among the choices of a token with these logits, 0 the first (top or more: not chosen), and its weight
@@ -59,12 +81,15 @@ __device__ __forceinline__ int rank_of(const float *l, int experts, int e, float
 
 // kTiles of 16 tokens: what a workgroup of the first kernel does once it knows its tokens
 template <int kTiles, Layout kLayout>
-__device__ __forceinline__ void gate_up(const MoeArgs &a, int e, int chunk, const int *list, const int *slot_of, int count, uint8_t *lds) {
+__device__ __forceinline__ void gate_up(const MoeArgs &a, int e, int chunk, const int *list, const int *slot_of, const float *scale_of, int count, uint8_t *lds) {
     constexpr int kWaves = 4, kStages = kTiles == 1 ? 3 : (kTiles == 2 ? 2 : 1);
     typedef Stream<2, kTiles, kStages, kLayout> S;
     static_assert(S::kBytes * kWaves <= kRingBytes && kWaves * 2 * 16 * kTiles * 17 * 4 <= kRingBytes, "");
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const int64_t f0 = (int64_t)chunk * 16;
+    // (the scales of this thread's column on their way before the weights, behind which they would wait)
+    const float *const scales = a.scale1 + (int64_t)e * 2 * a.F + min(f0 + (threadIdx.x & 15), a.F - 1);
+    const float scale_gate = scales[0], scale_up = scales[a.F];
     v4i acc[2][kTiles] = {};
     S s;
     s.lds = lds + wave * S::kBytes;
@@ -94,9 +119,7 @@ __device__ __forceinline__ void gate_up(const MoeArgs &a, int e, int chunk, cons
             int32_t s0 = 0, s1 = 0;
 #pragma unroll
             for (int w = 0; w < kWaves; ++w) s0 += sums[w][0][m][c], s1 += sums[w][1][m][c];
-            const float sx = a.scale_x[list[m]];
-            const float *const s = a.scale1 + (int64_t)e * 2 * a.F + f;
-            const float gate = (float)s0 * sx * s[0], up = (float)s1 * sx * s[a.F];
+            const float gate = (float)s0 * scale_of[m] * scale_gate, up = (float)s1 * scale_of[m] * scale_up;
             y = rows::silu(gate) * up;
             a.act[(int64_t)slot_of[m] * a.F + f] = y;
         }
@@ -113,8 +136,10 @@ template <Layout kLayout>
 __global__ __launch_bounds__(256) void moe_gate_up_kernel(const MoeArgs a, int chosen_at_most) {
     __shared__ __attribute__((aligned(16))) uint8_t lds[kRingBytes];
     __shared__ int list[64], slot_of[64], any[QNN_MOE_MAX_EXPERTS];
+    __shared__ float scale_of[64];
     const int t = threadIdx.x, wave = t >> 6, lane = t & 63, chunk = (int)(blockIdx.x / (uint32_t)chosen_at_most);
     int e = (int)(blockIdx.x % (uint32_t)chosen_at_most);
+    const float my_scale = a.scale_x[min(lane, a.tokens - 1)];
     // the logits, rows of an odd length: lanes that read a column meet different banks
     float *const logits = reinterpret_cast<float *>(lds);
     const int pitch = a.experts | 1;
@@ -167,14 +192,15 @@ __global__ __launch_bounds__(256) void moe_gate_up_kernel(const MoeArgs a, int c
         const int at = __popcll(who & ((1ull << lane) - 1ull));
         list[at] = lane;
         slot_of[at] = lane * a.top + rank;
+        scale_of[at] = my_scale;
     }
     __syncthreads();  // (the logits' place is free too)
     if (count <= 16)
-        gate_up<1, kLayout>(a, e, chunk, list, slot_of, count, lds);
+        gate_up<1, kLayout>(a, e, chunk, list, slot_of, scale_of, count, lds);
     else if (count <= 32)
-        gate_up<2, kLayout>(a, e, chunk, list, slot_of, count, lds);
+        gate_up<2, kLayout>(a, e, chunk, list, slot_of, scale_of, count, lds);
     else
-        gate_up<4, kLayout>(a, e, chunk, list, slot_of, count, lds);
+        gate_up<4, kLayout>(a, e, chunk, list, slot_of, scale_of, count, lds);
 }
 
 // The choices in the order of their experts; the experts that have any, and where each one's choices start (one more than there are).  One wave.
@@ -198,10 +224,13 @@ __device__ __forceinline__ int in_order(const MoeArgs &a, const Route *route, in
     return n;
 }
 
-// Activations become codes in LDS, `chunk` of the inner width at a time and as many experts at a time as have up to kCodes / (chunk + 16) choices
-// together (mostly everything at once); then every wave goes through its steps of k of one expert after the other without a break in its loads, and adds
-// what it has of an expert to the results in LDS (whole numbers: in any order).
-template <typename T, int kSlots, int kCodes, int kStages, Layout kLayout>
+// Activations lie in LDS as codes, `chunk` of the inner width at a time and as many experts at a time as have up to kCodes / (chunk + 16) choices together
+// (mostly everything at once); then every wave goes through its steps of k of one expert after the other without a break in its loads, and adds what it has
+// of an expert to the results in LDS (whole numbers: in any order).
+// kQuantize: the codes are made here, from the first kernel's activations and maxima, all at once; else they and their scales are in memory.  The first
+// saves a launch, but every workgroup reads four times as much and makes all the codes (7 tokens, three of 5 experts of 1000 x 700: 10.8 us, in two kernels
+// 4.2 + 9.8; 20 tokens, two of 8 experts of 4096 x 2048: 24.6 us, in two kernels 4.3 + 18.6).
+template <typename T, int kSlots, int kCodes, int kStages, Layout kLayout, bool kQuantize>
 __global__ __launch_bounds__(512) void moe_down_kernel(const MoeArgs a, T *out, int chunk) {
     constexpr int kWaves = 8;
     constexpr bool kFactors = kSlots <= 128;  // what a result is multiplied with has room in LDS
@@ -210,45 +239,31 @@ __global__ __launch_bounds__(512) void moe_down_kernel(const MoeArgs a, T *out, 
     __shared__ int32_t result[kSlots][16];
     __shared__ float factor[kFactors ? kSlots : 1][16];
     __shared__ Route route[kSlots];
-    __shared__ float mul[kSlots], pre[kSlots], scale[kSlots];
+    __shared__ float mul[kQuantize ? kSlots : 1], pre[kQuantize ? kSlots : 1], scale[kSlots];
     __shared__ int order[kSlots], active[QNN_MOE_MAX_EXPERTS], start[QNN_MOE_MAX_EXPERTS + 1], n_active;
     const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6), lane = t & 63, r = lane & 15, g = lane >> 4, slots = a.tokens * a.top;
     const int64_t n0 = (int64_t)blockIdx.x * 16;
     const uint32_t F = (uint32_t)a.F;
     const int pitch = chunk + 16, most = kCodes / pitch;
-    const bool at_once = slots <= most && F <= (uint32_t)chunk;  // then rows of codes are in the order of the choices, else in that of the experts
-    // 1024 activations of a row by a wave: four loads of whole lines; kItems of these under way
-    constexpr int kItems = 4;
+    const bool at_once = kQuantize || (slots <= most && F <= (uint32_t)chunk);  // then rows of codes are in the order of the choices, else in that of the experts
+    // kQuantize: 1024 activations of a row by a wave, four loads of whole lines; the first kItems of a wave's are on their way from here on
+    constexpr int kItems = 2;
     float v[kItems][4][4];
-    auto fetch = [&](float (&to)[4][4], int m, uint32_t f_first) __attribute__((always_inline)) {
-        const float *const p = a.act + (int64_t)m * a.F;
+    const uint32_t parts = ((uint32_t)chunk + 1023u) / 1024u, items = (uint32_t)slots * parts;
+    auto fetch = [&](float (&to)[4][4], uint32_t item) __attribute__((always_inline)) {
+        const float *const p = a.act + (int64_t)(item / parts) * a.F;
 #pragma unroll
         for (uint32_t u = 0; u < 4u; ++u) {
-            const uint32_t f = f_first + 4u * lane + 256u * u;
-            if (f + 4u <= F) {
-                __builtin_memcpy(to[u], p + f, 16);
-            } else {
+            const uint32_t f = item % parts * 1024u + 4u * lane + 256u * u;  // (the rows are followed by more than they lack to a group of four)
+            __builtin_memcpy(to[u], p + min(f, F - 1u), 16);
 #pragma unroll
-                for (uint32_t j = 0; j < 4u; ++j) to[u][j] = f + j < F ? p[f + j] : 0.0f;
-            }
+            for (uint32_t j = 0; j < 4u; ++j) to[u][j] = f + j < F ? to[u][j] : 0.0f;
         }
     };
-    auto put = [&](const float (&from)[4][4], int m, int row, uint32_t at, uint32_t whole) __attribute__((always_inline)) {
-        Quantizer q(0u, 1.0f);
-        q.mul = mul[m], q.pre = pre[m], q.zero = pre[m] == 0.0f;
+    if constexpr (kQuantize) {
 #pragma unroll
-        for (uint32_t u = 0; u < 4u; ++u) {
-            const uint32_t f = at + 4u * lane + 256u * u;
-            if (f < whole) *reinterpret_cast<uint32_t *>(&codes[row * pitch + (int)f]) = q.four(from[u][0], from[u][1], from[u][2], from[u][3]);
-        }
-    };
-    const uint32_t all_parts = ((uint32_t)chunk + 1023u) / 1024u;
-    if (at_once) {
-#pragma unroll
-        for (int j = 0; j < kItems; ++j) {
-            const uint32_t i = (uint32_t)(wave + kWaves * j);
-            if (i < (uint32_t)slots * all_parts) fetch(v[j], (int)(i / all_parts), i % all_parts * 1024u);
-        }
+        for (int j = 0; j < kItems; ++j)
+            if ((uint32_t)(wave + kWaves * j) < items) fetch(v[j], (uint32_t)(wave + kWaves * j));
     }
     // One wave finds the order of the choices; the others how each activation is quantized (for a choice that takes no part: nothing that is used).
     if (wave == 0) {
@@ -263,20 +278,24 @@ __global__ __launch_bounds__(512) void moe_down_kernel(const MoeArgs a, T *out, 
         if (lane == 0) n_active = n;
     } else {
         for (int i = t - 64; i < 16 * slots; i += 448) result[i >> 4][i & 15] = 0;
-        for (int s = (t - 64) >> 4; s < slots; s += 28) {  // 16 lanes each
-            uint32_t top = 0u;
-            const uint32_t *const from = a.tops + (int64_t)s * a.chunks;
-            for (int64_t c0 = 0; c0 < a.chunks; c0 += 128) {
-                uint32_t w[8];
+        if constexpr (kQuantize) {
+            for (int s = (t - 64) >> 4; s < slots; s += 28) {  // 16 lanes each
+                uint32_t top = 0u;
+                const uint32_t *const from = a.tops + (int64_t)s * a.chunks;
+                for (int64_t c0 = 0; c0 < a.chunks; c0 += 128) {
+                    uint32_t w[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) w[j] = from[min(c0 + 16 * j + r, a.chunks - 1)];
+                    for (int j = 0; j < 8; ++j) w[j] = from[min(c0 + 16 * j + r, a.chunks - 1)];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) top = max(top, w[j]);
+                    for (int j = 0; j < 8; ++j) top = max(top, w[j]);
+                }
+#pragma unroll
+                for (int d = 8; d >= 1; d >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d));
+                const Quantizer q(top, 1.0f);
+                if (r == 0) mul[s] = q.zero ? 0.0f : q.mul, pre[s] = q.zero ? 0.0f : q.pre, scale[s] = q.scale;
             }
-#pragma unroll
-            for (int d = 8; d >= 1; d >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d));
-            const Quantizer q(top, 1.0f);
-            if (r == 0) mul[s] = q.zero ? 0.0f : q.mul, pre[s] = q.zero ? 0.0f : q.pre, scale[s] = q.scale;
+        } else {
+            for (int s = t - 64; s < slots; s += 448) scale[s] = a.scales[s];
         }
     }
     __syncthreads();
@@ -317,21 +336,40 @@ __global__ __launch_bounds__(512) void moe_down_kernel(const MoeArgs a, T *out, 
                 return k;
             };
             s.start(steps, base, at);
-            // activations to codes, zeros from their end to a whole step
-            const uint32_t whole = min((uint32_t)chunk, (F - f0 + 127u) / 128u * 128u), parts = (whole + 1023u) / 1024u;
-            const uint32_t items = (uint32_t)(at_once ? slots : n_rows) * parts;
-            for (uint32_t i0 = wave; i0 < items; i0 += kWaves * kItems) {
-                if (!at_once || i0 != (uint32_t)wave) {
+            if constexpr (kQuantize) {  // zeros from an activation's end to a whole step
+                for (uint32_t i0 = wave; i0 < items; i0 += kWaves * kItems) {
+#pragma unroll
+                    for (uint32_t j = 0; j < kItems; ++j)
+                        if (i0 != (uint32_t)wave && i0 + kWaves * j < items) fetch(v[j], i0 + kWaves * j);
 #pragma unroll
                     for (uint32_t j = 0; j < kItems; ++j) {
                         const uint32_t i = i0 + kWaves * j;
-                        if (i < items) fetch(v[j], at_once ? (int)(i / parts) : order[first_row + (int)(i / parts)], f0 + i % parts * 1024u);
+                        if (i >= items) break;
+                        const int m = (int)(i / parts);
+                        Quantizer q(0u, 1.0f);
+                        q.mul = mul[m], q.pre = pre[m], q.zero = pre[m] == 0.0f;
+#pragma unroll
+                        for (uint32_t u = 0; u < 4u; ++u) {
+                            const uint32_t f = i % parts * 1024u + 4u * lane + 256u * u;
+                            if (f < (uint32_t)chunk) *reinterpret_cast<uint32_t *>(&codes[m * pitch + (int)f]) = q.four(v[j][u][0], v[j][u][1], v[j][u][2], v[j][u][3]);
+                        }
                     }
                 }
+            } else {  // 16 codes a lane, whole rows of the part (what lies beyond the inner width meets zeros), eight loads under way
+                const uint32_t per_row = min((uint32_t)chunk, (uint32_t)a.ld_codes - f0) / 16u, n = (uint32_t)(at_once ? slots : n_rows) * per_row;
+                for (uint32_t i0 = t; i0 < n; i0 += 8u * 512u) {
+                    v4i c[8];
 #pragma unroll
-                for (uint32_t j = 0; j < kItems; ++j) {
-                    const uint32_t i = i0 + kWaves * j;
-                    if (i < items) put(v[j], at_once ? (int)(i / parts) : order[first_row + (int)(i / parts)], (int)(i / parts), i % parts * 1024u, whole);
+                    for (uint32_t j = 0; j < 8u; ++j) {
+                        const uint32_t i = min(i0 + 512u * j, n - 1u), row = i / per_row;
+                        const int m = at_once ? (int)row : order[first_row + (int)row];
+                        __builtin_memcpy(&c[j], a.codes + (int64_t)m * a.ld_codes + f0 + 16u * (i - row * per_row), 16);
+                    }
+#pragma unroll
+                    for (uint32_t j = 0; j < 8u; ++j) {
+                        const uint32_t i = min(i0 + 512u * j, n - 1u), row = i / per_row;
+                        *reinterpret_cast<v4i *>(&codes[(int)row * pitch + 16 * (int)(i - row * per_row)]) = c[j];
+                    }
                 }
             }
             if (kFactors && from == 0 && f0 == 0u) {
@@ -385,7 +423,10 @@ __global__ __launch_bounds__(512) void moe_down_kernel(const MoeArgs a, T *out, 
 size_t round_up_256(size_t v) { return (v + 255) / 256 * 256; }
 size_t route_bytes(int64_t tokens, int top) { return round_up_256((size_t)(tokens * top) * sizeof(Route)); }
 size_t act_bytes(int64_t tokens, int top, int64_t F) { return round_up_256((size_t)(tokens * top) * (size_t)F * 4); }
-size_t tops_bytes(int64_t tokens, int top, int64_t F) { return round_up_256((size_t)(tokens * top) * (size_t)ceil_div(F, 16) * 4); }
+size_t tops_bytes(int64_t tokens, int top, int64_t F) { return round_up_256((size_t)(tokens * top) * (size_t)ceil_div(F, 16) * 4 + 16); }  // (and see fetch)
+int64_t codes_pitch(int64_t F) { return ceil_div(F, 128) * 128; }
+size_t codes_bytes(int64_t tokens, int top, int64_t F) { return round_up_256((size_t)(tokens * top) * (size_t)codes_pitch(F)); }
+size_t scales_bytes(int64_t tokens, int top) { return round_up_256((size_t)(tokens * top) * 4); }
 
 int launch_moe(const MoeArgs &a, void *out, int type, hipStream_t s) {
     const int most = a.tokens * a.top < a.experts ? a.tokens * a.top : a.experts;
@@ -393,23 +434,32 @@ int launch_moe(const MoeArgs &a, void *out, int type, hipStream_t s) {
     const bool pieces1 = in_pieces(a.x, a.ldx, a.tokens, a.H) && in_pieces(a.W1, a.ld_w1, 2 * a.F, a.H), pieces2 = in_pieces(a.W2, a.ld_w2, a.H, a.F);
     auto up = pieces1 ? moe_gate_up_kernel<kPieces> : (a.H >= 16 ? moe_gate_up_kernel<kAny> : moe_gate_up_kernel<kShortRows>);
     if (int rc = QNN_LAUNCH("int8_moe", up, grid, dim3(256), 0, s, a, most)) return rc;
-    const int64_t whole = ceil_div(a.F, 128) * 128;
+    const int64_t whole = codes_pitch(a.F);
     const int slots = a.tokens * a.top;
+    // a few choices: codes are made by the second kernel, two workgroups on a compute unit; many: LDS holds the results of all and the codes of one expert's 64
+    // tokens at least
+    constexpr int kFew = 20 * 1024, kMore = 88 * 1024, kMost = 64 * (1024 + 16);
+    const bool few = slots <= 32 && slots * (whole + 16) <= kFew;
+    if (!few) {
+        const PlainSource act = {a.act, a.F};
+        if (int rc = rows::launch_quant_rows("int8_moe", act, slots, a.F, a.codes, a.ld_codes, a.scales, s)) return rc;
+    }
     return rows::with_type(type, [&](auto tag) {
         typedef decltype(tag) T;
         const dim3 columns((unsigned)ceil_div(a.H, 16)), threads(512);
         T *const o = static_cast<T *>(out);
-        // few choices: two workgroups on a compute unit; many: LDS holds the results of all and the codes of one expert's 64 tokens at least
-        constexpr int kFew = 16 * 1024, kMore = 88 * 1024, kMost = 64 * (1024 + 16);
         auto launch = [&](auto pieces, auto any, auto short_rows, int chunk) {
             return QNN_LAUNCH("int8_moe", (pieces2 ? pieces : (a.F >= 16 ? any : short_rows)), columns, threads, 0, s, a, o, chunk);
         };
-        if (slots <= 32 && slots * (whole + 16) <= kFew)
-            return launch(moe_down_kernel<T, 32, kFew, 3, kPieces>, moe_down_kernel<T, 32, kFew, 2, kAny>, moe_down_kernel<T, 32, kFew, 1, kShortRows>, (int)whole);
+        if (few)
+            return launch(moe_down_kernel<T, 32, kFew, 3, kPieces, true>, moe_down_kernel<T, 32, kFew, 2, kAny, true>, moe_down_kernel<T, 32, kFew, 1, kShortRows, true>,
+                          (int)whole);
         const int chunk = whole <= 1024 || (slots <= 128 && slots * (whole + 16) <= kMore) ? (int)whole : 1024;
         if (slots <= 128)
-            return launch(moe_down_kernel<T, 128, kMore, 3, kPieces>, moe_down_kernel<T, 128, kMore, 2, kAny>, moe_down_kernel<T, 128, kMore, 1, kShortRows>, chunk);
-        return launch(moe_down_kernel<T, 512, kMost, 2, kPieces>, moe_down_kernel<T, 512, kMost, 2, kAny>, moe_down_kernel<T, 512, kMost, 1, kShortRows>, chunk);
+            return launch(moe_down_kernel<T, 128, kMore, 3, kPieces, false>, moe_down_kernel<T, 128, kMore, 2, kAny, false>,
+                          moe_down_kernel<T, 128, kMore, 1, kShortRows, false>, chunk);
+        return launch(moe_down_kernel<T, 512, kMost, 2, kPieces, false>, moe_down_kernel<T, 512, kMost, 2, kAny, false>,
+                      moe_down_kernel<T, 512, kMost, 1, kShortRows, false>, chunk);
     });
 }
 
@@ -421,7 +471,8 @@ using namespace qnn;
 
 extern "C" size_t qnn_int8_moe_workspace_bytes(int64_t tokens, int top, int64_t F) {
     if (tokens < 1 || tokens > QNN_MOE_MAX_TOKENS || top < 1 || top > QNN_MOE_MAX_TOP || F < 1 || F > int8::kMostK) return 0;
-    return int8::route_bytes(tokens, top) + int8::act_bytes(tokens, top, F) + int8::tops_bytes(tokens, top, F);
+    return int8::route_bytes(tokens, top) + int8::act_bytes(tokens, top, F) + int8::tops_bytes(tokens, top, F) + int8::codes_bytes(tokens, top, F) +
+           int8::scales_bytes(tokens, top);
 }
 
 extern "C" int qnn_int8_moe(const int8_t *x, int64_t ldx, const float *scale_x, const float *logits, int64_t ld_logits, int64_t tokens, int experts,
@@ -444,9 +495,11 @@ extern "C" int qnn_int8_moe(const int8_t *x, int64_t ldx, const float *scale_x, 
     if (!workspace || !rows::aligned_to(workspace, 256) || workspace_bytes < need)
         return fail(QNN_ERR_WORKSPACE, "int8_moe: workspace NULL, misaligned or smaller than %zu bytes", need);
     uint8_t *const ws = static_cast<uint8_t *>(workspace);
-    const size_t r = int8::route_bytes(tokens, top), v = int8::act_bytes(tokens, top, F);
+    const size_t r = int8::route_bytes(tokens, top), v = r + int8::act_bytes(tokens, top, F), c = v + int8::tops_bytes(tokens, top, F),
+                 f = c + int8::codes_bytes(tokens, top, F);
     const int8::MoeArgs a = {x, W1, W2, scale_x, logits, scale1, scale2, ldx, ld_logits, ld_w1, ld_w2, H, F, ldo, (int)tokens, experts, top,
-                             reinterpret_cast<int8::Route *>(ws), reinterpret_cast<float *>(ws + r), reinterpret_cast<uint32_t *>(ws + r + v), ceil_div(F, 16)};
+                             reinterpret_cast<int8::Route *>(ws), reinterpret_cast<float *>(ws + r), reinterpret_cast<uint32_t *>(ws + v), ceil_div(F, 16),
+                             reinterpret_cast<int8_t *>(ws + c), reinterpret_cast<float *>(ws + f), int8::codes_pitch(F)};
     hipStream_t s = static_cast<hipStream_t>(stream);
     return int8::launch_moe(a, out, type, s);
 }

@@ -31,7 +31,7 @@ def _check(got, layer, top):
 
 SHAPES = [(1, 1, 1, 1, 1), (1, 8, 2, 64, 32), (1, 8, 2, 512, 256), (2, 3, 3, 100, 70), (5, 5, 3, 1000, 700), (16, 16, 4, 256, 128), (17, 4, 1, 300, 200), (20, 8, 2, 512, 300),
           (33, 6, 2, 200, 1500), (64, 8, 8, 130, 65), (64, 2, 1, 128, 2500), (64, 70, 5, 64, 48), (7, 256, 8, 48, 40), (3, 200, 2, 80, 17), (4, 2, 2, 5000, 16), (1, 3, 1, 40, 4200),
-          (40, 1, 1, 256, 2049)]
+          (40, 1, 1, 256, 2049), (64, 5, 4, 96, 1536), (50, 9, 4, 100, 1300), (64, 3, 2, 64, 2048), (10, 4, 3, 96, 624), (64, 6, 6, 48, 10), (30, 4, 1, 80, 6)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
