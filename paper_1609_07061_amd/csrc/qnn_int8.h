@@ -35,18 +35,19 @@ __device__ __forceinline__ v4i load_short(const int8_t *row, int64_t k, int64_t 
         if (k + i < K) w[i >> 2] |= (uint32_t)(uint8_t)row[k + i] << (8 * (i & 3));
     return v4i{(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
 }
-// How rows of codes are loaded: kPieces: whole 16-byte pieces at 16-byte aligned addresses, within 4 GiB; kAny; kShortRows: fewer than 16 codes
-enum Layout { kPieces, kAny, kShortRows };
+// How rows of codes are loaded: kPieces: whole 16-byte pieces at 16-byte aligned addresses, within 4 GiB; kPiecesOnce: the same, and the weights past the
+// caches; kAny; kShortRows: fewer than 16 codes
+enum Layout { kPieces, kPiecesOnce, kAny, kShortRows };
 
 // A wave's own stream of operands: steps of 128 codes of 16 kCols weight rows and 16 kTiles rows of codes, brought to LDS in whole lines (8 rows of 128
 // bytes a load) and read from there as the matrix cores take them.  Loaded straight into place, lane l of an operand having 16 codes of row l mod 16,
 // neighbouring lanes are different rows and the 64 pieces of a load are taken one by one: 16 bytes a cycle and compute unit, against 64 in whole lines (4096
 // codes of 128 x 4096 rows: 18.8 us, and 8.3 like this).  Nobody waits for another wave.  Piece c of row r is at piece c xor (r / 2 mod 8): the 16 rows
 // that a read serves at a time lie on different banks.
-// kPieces: loads straight to LDS, kStages steps there.  Otherwise kStages steps in registers, which pass through one place in LDS.
+// Pieces: loads straight to LDS, kStages steps there.  Otherwise kStages steps in registers, which pass through one place in LDS.
 template <int kCols, int kTiles, int kStages, Layout kLayout>
 struct Stream {
-    static constexpr bool kRing = kLayout == kPieces;
+    static constexpr bool kRing = kLayout == kPieces || kLayout == kPiecesOnce;
     static constexpr int kRows = kCols + kTiles, kLoads = 2 * kRows, kStage = 1024 * kLoads, kBytes = (kRing ? kStages : 1) * kStage;
     static_assert(kStages <= 4 && (kStages - 1) * kLoads <= 63, "a count of loads that s_waitcnt can name");
     typedef std::conditional_t<kRing, uint32_t, int64_t> Offset;
@@ -75,7 +76,10 @@ struct Stream {
                 if constexpr (kRing) {
                     const uint32_t to = __builtin_amdgcn_readfirstlane((uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) uint8_t *)lds)) +
                                         (uint32_t)(s * kStage + 2048 * b + 1024 * h);
-                    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(off[b][h] + k), "s"(base) : "memory");
+                    if (kLayout == kPiecesOnce && b < kCols)
+                        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" : : "s"(to), "v"(off[b][h] + k), "s"(base) : "memory");
+                    else
+                        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(off[b][h] + k), "s"(base) : "memory");
                 } else {
                     held[s][2 * b + h] = kLayout == kAny ? load_window(base + off[b][h], k, K) : load_short(base + off[b][h], k, K);
                 }

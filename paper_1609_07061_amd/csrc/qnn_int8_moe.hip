@@ -17,6 +17,10 @@ using rows::Quantizer;
 
 static_assert(QNN_MOE_MAX_TOKENS == 64, "one lane a token");
 
+// With more logits or experts the choices are found by a kernel of their own, not by every workgroup.  Per call, in every workgroup and in a kernel: one token,
+// 8 experts 16.6 and 18.3 us; 32 tokens, 16 experts 44.6 and 46.2; one token, 128 experts 24.2 and 22.1; 8 tokens, 128 experts 178 and 82.
+constexpr int kRoutedFrom = 512, kRoutedExperts = 64;
+
 constexpr int kRingBytes = 72 * 1024;  // LDS of the first kernel's operands: two workgroups on a compute unit
 
 struct Route {  // a choice of a token: `weight` is exp(logit - largest logit); NaN: the token's logits say nothing; 0: takes no part
@@ -57,26 +61,57 @@ struct PlainSource {
     __device__ __forceinline__ void keep(int64_t, const rows::Window &, int64_t, const Kept &) const {}
 };
 
-// Where expert e stands among the choices of a token with these logits, 0 the first (top or more: not chosen), and its weight
-__device__ __forceinline__ int rank_of(const float *l, int experts, int e, float &weight) {
-    const float mine = l[e];
-    auto key = [](float v) __attribute__((always_inline)) {  // an unsigned integer in the order of the values; NaN somewhere, but a total order
-        const uint32_t b = __float_as_uint(v + 0.0f);        // (-0 counts as +0)
-        return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
-    };
-    const uint32_t own = key(mine);
+// A logit as an unsigned integer in the order of the values: -0 counts as +0, NaN is above all
+__device__ __forceinline__ uint32_t key_of(float v) {
+    const uint32_t b = __float_as_uint(v + 0.0f);
+    return v != v ? 0xFFFFFFFFu : b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+}
+constexpr uint32_t kKeyOfInf = 0xFF800000u, kKeyOfMinusInf = 0x007FFFFFu;
+__device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float(key ^ (key >> 31 ? 0x80000000u : 0xFFFFFFFFu)); }
+
+// Words of a token's keys in LDS: whole groups of four, an odd number of them (lanes that read a column meet different banks)
+__host__ __device__ constexpr int keys_pitch(int experts) { return 4 * (((experts + 3) / 4) | 1); }
+
+// Where expert e stands among the choices of a token with these keys (zeros from the last to a group of four), 0 the first (top or more: not chosen), and its
+// weight
+__device__ __forceinline__ int rank_of(const uint32_t *keys, int experts, int e, float &weight) {
+    const uint32_t own = keys[e];
     int rank = 0;
-    float top = -INFINITY;
-    bool nan = false;
-    for (int j = 0; j < experts; ++j) {
-        const float v = l[j];
-        const uint32_t k = key(v);
-        rank += k > own || (k == own && j < e);
-        top = fmaxf(top, v);
-        nan |= v != v;
+    uint32_t top = 0u;
+    for (int j = 0; j < experts; j += 4) {
+        const v4i k = *reinterpret_cast<const v4i *>(keys + j);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) rank += (uint32_t)k[i] > own || ((uint32_t)k[i] == own && j + i < e), top = max(top, (uint32_t)k[i]);
     }
-    weight = nan || top == INFINITY ? __uint_as_float(0x7FC00000u) : (top == -INFINITY ? 0.0f : expf(mine - top));
+    weight = top >= kKeyOfInf ? __uint_as_float(0x7FC00000u) : (top == kKeyOfMinusInf ? 0.0f : expf(value_of(own) - value_of(top)));
     return rank;
+}
+
+// The n-th (from 0) of the experts with a nonzero in any[], -1 if there are fewer; by a wave
+__device__ __forceinline__ int nth_of(const int *any, int n) {
+    const int lane = threadIdx.x & 63;
+    for (int x0 = 0; x0 < QNN_MOE_MAX_EXPERTS; x0 += 64) {
+        uint64_t who = __ballot(any[x0 + lane] != 0);
+        const int here = __popcll(who);
+        if (n < here) {
+            for (; n > 0; --n) who &= who - 1ull;
+            return __builtin_amdgcn_readfirstlane(x0 + __ffsll((unsigned long long)who) - 1);
+        }
+        n -= here;
+    }
+    return -1;
+}
+
+// Choices of a token, a workgroup each
+__global__ __launch_bounds__(QNN_MOE_MAX_EXPERTS) void moe_route_kernel(const MoeArgs a) {
+    __shared__ __attribute__((aligned(16))) uint32_t keys[QNN_MOE_MAX_EXPERTS];
+    const int t = threadIdx.x, tok = blockIdx.x;
+    keys[t] = t < a.experts ? key_of(a.logits[(int64_t)tok * a.ld_logits + t]) : 0u;
+    __syncthreads();
+    if (t >= a.experts) return;
+    float weight;
+    const int rank = rank_of(keys, a.experts, t, weight);
+    if (rank < a.top) a.route[tok * a.top + rank] = Route{t, weight};
 }
 
 // kTiles of 16 tokens: what a workgroup of the first kernel does once it knows its tokens
@@ -132,69 +167,87 @@ __device__ __forceinline__ void gate_up(const MoeArgs &a, int e, int chunk, cons
 
 // Grid: 16 columns of the inner width x as many experts as can be chosen.  Where those are fewer than there are, a workgroup finds the one that is its own
 // among the chosen (a workgroup for each of them that ended at once: 11.4 us for one token and two of 8 experts of 4096 x 2048, 8.9 like this).
-template <Layout kLayout>
+// kRouted: the choices are known; else every workgroup finds them from the logits
+template <Layout kLayout, bool kRouted>
 __global__ __launch_bounds__(256) void moe_gate_up_kernel(const MoeArgs a, int chosen_at_most) {
     __shared__ __attribute__((aligned(16))) uint8_t lds[kRingBytes];
     __shared__ int list[64], slot_of[64], any[QNN_MOE_MAX_EXPERTS];
     __shared__ float scale_of[64];
     const int t = threadIdx.x, wave = t >> 6, lane = t & 63, chunk = (int)(blockIdx.x / (uint32_t)chosen_at_most);
     int e = (int)(blockIdx.x % (uint32_t)chosen_at_most);
-    const float my_scale = a.scale_x[min(lane, a.tokens - 1)];
-    // the logits, rows of an odd length: lanes that read a column meet different banks
-    float *const logits = reinterpret_cast<float *>(lds);
-    const int pitch = a.experts | 1;
-    static_assert(QNN_MOE_MAX_TOKENS * (QNN_MOE_MAX_EXPERTS + 1) * 4 <= kRingBytes, "");
-    for (int i0 = t; i0 < a.tokens * a.experts; i0 += 1024) {
-        float v[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int i = min(i0 + 256 * j, a.tokens * a.experts - 1), tok = (int)((uint32_t)i / (uint32_t)a.experts);
-            v[j] = a.logits[(int64_t)tok * a.ld_logits + (i - tok * a.experts)];
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int i = min(i0 + 256 * j, a.tokens * a.experts - 1), tok = (int)((uint32_t)i / (uint32_t)a.experts);
-            logits[tok * pitch + (i - tok * a.experts)] = v[j];
-        }
-    }
     any[t] = 0;
     static_assert(QNN_MOE_MAX_EXPERTS == 256, "one thread an expert");
-    __syncthreads();
-    float weight;
-    if (chosen_at_most < a.experts) {
-        for (int i = t; i < a.tokens * a.experts; i += 256) {
-            const int tok = (int)((uint32_t)i / (uint32_t)a.experts), x = i - tok * a.experts;
-            if (rank_of(logits + tok * pitch, a.experts, x, weight) < a.top) any[x] = 1;
+    bool chosen;
+    int slot;
+    float my_scale;
+    if constexpr (kRouted) {
+        constexpr int kSlots = QNN_MOE_MAX_TOKENS * QNN_MOE_MAX_TOP;
+        static_assert(kSlots == 512, "");
+        __shared__ int expert[kSlots], slot_at[64];
+        const int slots = a.tokens * a.top;
+        int mine[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const Route c = a.route[min(t + 256 * j, slots - 1)];
+            mine[j] = t + 256 * j < slots && c.weight > 0.0f ? c.expert : -1;
         }
         __syncthreads();
-        int left = e;
-        e = -1;
-        for (int x0 = 0; x0 < a.experts && e < 0; x0 += 64) {
-            uint64_t who = __ballot(x0 + lane < a.experts && any[x0 + lane] != 0);
-            const int here = __popcll(who);
-            if (left < here) {
-                for (; left > 0; --left) who &= who - 1ull;
-                e = x0 + __ffsll((unsigned long long)who) - 1;
-            }
-            left -= here;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            expert[t + 256 * j] = mine[j];
+            if (mine[j] >= 0) any[mine[j]] = 1;
         }
+        __syncthreads();
+        e = nth_of(any, e);
         if (e < 0) return;
-        e = __builtin_amdgcn_readfirstlane(e);
+        int count = 0;
+        for (int s0 = 0; s0 < slots; s0 += 64) {
+            const bool is = expert[s0 + lane] == e;
+            const uint64_t who = __ballot(is);
+            if (wave == 0 && is) slot_at[count + __popcll(who & ((1ull << lane) - 1ull))] = s0 + lane;
+            count += __popcll(who);
+        }
+        __syncthreads();
+        chosen = lane < count;
+        slot = chosen ? slot_at[lane] : 0;
+        my_scale = a.scale_x[(uint32_t)slot / (uint32_t)a.top];
+    } else {
+        my_scale = a.scale_x[min(lane, a.tokens - 1)];
+        uint32_t *const keys = reinterpret_cast<uint32_t *>(lds);
+        const int pitch = keys_pitch(a.experts), padded = (a.experts + 3) / 4 * 4;
+        static_assert(kRoutedFrom * 4 * 2 + QNN_MOE_MAX_TOKENS * 16 <= kRingBytes, "");
+        for (int i = t; i < a.tokens * padded; i += 256) {
+            const int tok = (int)((uint32_t)i / (uint32_t)padded), x = i - tok * padded;
+            const float v = a.logits[(int64_t)tok * a.ld_logits + min(x, a.experts - 1)];
+            keys[tok * pitch + x] = x < a.experts ? key_of(v) : 0u;
+        }
+        __syncthreads();
+        float weight;
+        if (chosen_at_most < a.experts) {
+            for (int i = t; i < a.tokens * a.experts; i += 256) {
+                const int tok = (int)((uint32_t)i / (uint32_t)a.experts), x = i - tok * a.experts;
+                if (rank_of(keys + tok * pitch, a.experts, x, weight) < a.top) any[x] = 1;
+            }
+            __syncthreads();
+            e = nth_of(any, e);
+            if (e < 0) return;
+        }
+        const int rank = rank_of(keys + min(lane, a.tokens - 1) * pitch, a.experts, e, weight);
+        const bool mine = lane < a.tokens && rank < a.top;
+        if (mine && chunk == 0 && wave == 0) a.route[lane * a.top + rank] = Route{e, weight};
+        chosen = mine && weight > 0.0f;
+        slot = lane * a.top + rank;
     }
-    const int rank = rank_of(logits + min(lane, a.tokens - 1) * pitch, a.experts, e, weight);
-    const bool mine = lane < a.tokens && rank < a.top;
-    if (mine && chunk == 0 && wave == 0) a.route[lane * a.top + rank] = Route{e, weight};
-    const bool chosen = mine && weight > 0.0f;
     const uint64_t who = __ballot(chosen);
     const int count = __popcll(who);
     if (count == 0) return;
     if (wave == 0 && chosen) {
         const int at = __popcll(who & ((1ull << lane) - 1ull));
-        list[at] = lane;
-        slot_of[at] = lane * a.top + rank;
+        list[at] = (int)((uint32_t)slot / (uint32_t)a.top);
+        slot_of[at] = slot;
         scale_of[at] = my_scale;
     }
-    __syncthreads();  // (the logits' place is free too)
+    __syncthreads();  // (the keys' place is free too)
     if (count <= 16)
         gate_up<1, kLayout>(a, e, chunk, list, slot_of, scale_of, count, lds);
     else if (count <= 32)
@@ -203,25 +256,55 @@ __global__ __launch_bounds__(256) void moe_gate_up_kernel(const MoeArgs a, int c
         gate_up<4, kLayout>(a, e, chunk, list, slot_of, scale_of, count, lds);
 }
 
-// The choices in the order of their experts; the experts that have any, and where each one's choices start (one more than there are).  One wave.
-__device__ __forceinline__ int in_order(const MoeArgs &a, const Route *route, int slots, int *order, int *active, int *start) {
+// The choices that take part, expert by expert: order[] of the choices, active[] experts, start[] of each in order[] and the end.  By one wave; returns the
+// number of experts.  (Within an expert in any order: each choice has its own result.)
+template <int kSlots>
+__device__ __forceinline__ int in_order(const MoeArgs &a, Route *route, int slots, int *order, int *active, int *start, int *place) {
+    constexpr int kPer = (kSlots + 63) / 64;
+    typedef Stream<1, 0, 1, kPieces> S;
     const int lane = threadIdx.x & 63;
-    int at = 0, n = 0;
-    for (int e = 0; e < a.experts; ++e) {
-        const int before = at;
-        for (int s0 = 0; s0 < slots; s0 += 64) {
-            const bool is = s0 + lane < slots && route[s0 + lane].expert == e;
-            const uint64_t who = __ballot(is);
-            if (is) order[at + __popcll(who & ((1ull << lane) - 1ull))] = s0 + lane;
-            at += __popcll(who);
-        }
-        if (at > before) {
-            if (lane == 0) active[n] = e, start[n] = before;
-            ++n;
-        }
+    int expert[kPer], at[kPer];
+    *reinterpret_cast<v4i *>(&place[4 * lane]) = v4i{0, 0, 0, 0};
+    static_assert(QNN_MOE_MAX_EXPERTS == 256, "four a lane");
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        const int s = 64 * j + lane;
+        const Route c = a.route[min(s, slots - 1)];
+        expert[j] = s < slots && c.weight > 0.0f ? c.expert : -1;
+        if (s < slots) route[s] = Route{expert[j], c.weight};
     }
-    if (lane == 0) start[n] = at;
-    return n;
+    S::in_wave();
+#pragma unroll
+    for (int j = 0; j < kPer; ++j)
+        if (expert[j] >= 0) at[j] = atomicAdd(&place[expert[j]], 1);
+    S::in_wave();
+    const v4i count = *reinterpret_cast<const v4i *>(&place[4 * lane]);
+    // choices in the low half, experts in the high one
+    uint32_t own = 0u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) own += (uint32_t)count[i] + (count[i] > 0 ? 0x10000u : 0u);
+    uint32_t before = own;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const uint32_t other = (uint32_t)__shfl_up((int)before, d);
+        before += lane >= d ? other : 0u;
+    }
+    const uint32_t whole = (uint32_t)__shfl((int)before, 63);
+    before -= own;
+    v4i places;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        places[i] = (int)(before & 0xFFFFu);
+        if (count[i] > 0) active[before >> 16] = 4 * lane + i, start[before >> 16] = places[i];
+        before += (uint32_t)count[i] + (count[i] > 0 ? 0x10000u : 0u);
+    }
+    *reinterpret_cast<v4i *>(&place[4 * lane]) = places;
+    if (lane == 0) start[whole >> 16] = (int)(whole & 0xFFFFu);
+    S::in_wave();
+#pragma unroll
+    for (int j = 0; j < kPer; ++j)
+        if (expert[j] >= 0) order[place[expert[j]] + at[j]] = 64 * j + lane;
+    return (int)(whole >> 16);
 }
 
 // Activations lie in LDS as codes, `chunk` of the inner width at a time and as many experts at a time as have up to kCodes / (chunk + 16) choices together
@@ -240,6 +323,7 @@ __global__ __launch_bounds__(512) void moe_down_kernel(const MoeArgs a, T *out, 
     __shared__ float factor[kFactors ? kSlots : 1][16];
     __shared__ Route route[kSlots];
     __shared__ float mul[kQuantize ? kSlots : 1], pre[kQuantize ? kSlots : 1], scale[kSlots];
+    __shared__ __attribute__((aligned(16))) int place[QNN_MOE_MAX_EXPERTS];
     __shared__ int order[kSlots], active[QNN_MOE_MAX_EXPERTS], start[QNN_MOE_MAX_EXPERTS + 1], n_active;
     const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6), lane = t & 63, r = lane & 15, g = lane >> 4, slots = a.tokens * a.top;
     const int64_t n0 = (int64_t)blockIdx.x * 16;
@@ -267,14 +351,7 @@ __global__ __launch_bounds__(512) void moe_down_kernel(const MoeArgs a, T *out, 
     }
     // One wave finds the order of the choices; the others how each activation is quantized (for a choice that takes no part: nothing that is used).
     if (wave == 0) {
-        for (int s = lane; s < slots; s += 64) {
-            const Route c = a.route[s];
-            route[s] = Route{c.weight > 0.0f ? c.expert : -1, c.weight};
-        }
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-        const int n = in_order(a, route, slots, order, active, start);
+        const int n = in_order<kSlots>(a, route, slots, order, active, start, place);
         if (lane == 0) n_active = n;
     } else {
         for (int i = t - 64; i < 16 * slots; i += 448) result[i >> 4][i & 15] = 0;
@@ -321,18 +398,24 @@ __global__ __launch_bounds__(512) void moe_down_kernel(const MoeArgs a, T *out, 
         while (to < experts && __builtin_amdgcn_readfirstlane(start[to + 1]) - first_row <= most) ++to;
         const int n_rows = __builtin_amdgcn_readfirstlane(start[to]) - first_row;
         for (uint32_t f0 = 0; f0 < F; f0 += (uint32_t)chunk) {
-            // this wave's steps: expert by expert, `per` each; the loads' cursor and the products'
-            const uint32_t end = min(F, f0 + (uint32_t)chunk), k0 = f0 + 128u * wave;
-            const int per = end > k0 ? (int)((end - k0 - 1u) / (128u * kWaves)) + 1 : 0, steps = per * (to - from);
-            int send_x = from, send_step = 0, x = from, step = 0;
+            // the steps of all experts here, expert by expert, blocks of 128 of them: a wave has every eighth; the loads' cursor and the products'
+            const int blocks = (int)((min(F, f0 + (uint32_t)chunk) - f0 + 127u) / 128u), all = blocks * (to - from), steps = all > wave ? (all - wave - 1) / kWaves + 1 : 0;
+            int send_x = from + wave / blocks, send_block = wave % blocks, x = send_x, block = send_block;
+            auto next = [&](int &x, int &block) __attribute__((always_inline)) {
+                block += kWaves;
+                const bool other = block >= blocks;
+                while (block >= blocks) block -= blocks, ++x;
+                return other;
+            };
             const int8_t *w_base = a.W2;
+            bool send_other = true;
             auto base = [&](int) __attribute__((always_inline)) {
-                if (send_step == 0) w_base = a.W2 + (int64_t)__builtin_amdgcn_readfirstlane(active[send_x]) * a.H * a.ld_w2;
+                if (send_other) w_base = a.W2 + (int64_t)__builtin_amdgcn_readfirstlane(active[send_x]) * a.H * a.ld_w2;
                 return w_base;
             };
             auto at = [&](int) __attribute__((always_inline)) {  // (called after base)
-                const uint32_t k = k0 + (uint32_t)send_step * (128u * kWaves);
-                if (++send_step == per) send_step = 0, ++send_x;
+                const uint32_t k = f0 + 128u * (uint32_t)send_block;
+                send_other = next(send_x, send_block);
                 return k;
             };
             s.start(steps, base, at);
@@ -378,8 +461,9 @@ __global__ __launch_bounds__(512) void moe_down_kernel(const MoeArgs a, T *out, 
             asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // (weights may still be on their way)
             v4i acc[4];
             int row[4], first = 0, count = 0;
+            bool other = true;
             s.run(steps, base, at, [&](int, const typename S::Operands &o) __attribute__((always_inline)) {
-                if (step == 0) {
+                if (other) {
                     first = __builtin_amdgcn_readfirstlane(start[x]), count = __builtin_amdgcn_readfirstlane(start[x + 1]) - first;
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
@@ -387,21 +471,20 @@ __global__ __launch_bounds__(512) void moe_down_kernel(const MoeArgs a, T *out, 
                         row[j] = (at_once ? order[pos] : pos - first_row) * pitch, acc[j] = v4i{0, 0, 0, 0};
                     }
                 }
-                const int k = (int)(k0 - f0) + step * (128 * kWaves) + 16 * g;
-                const bool last = ++step == per;
+                const int k = 128 * block + 16 * g;
+                other = next(x, block);
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
                     if (16 * j < count) {
 #pragma unroll
                         for (int h = 0; h < 2; ++h)
                             acc[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(o.w[h][0], *reinterpret_cast<const v4i *>(&codes[row[j] + k + 64 * h]), acc[j], 0, 0, 0);
-                        if (last && 16 * j + r < count) {
+                        if (other && 16 * j + r < count) {
                             const int m = order[first + 16 * j + r];
 #pragma unroll
                             for (int w = 0; w < 4; ++w) atomicAdd(&result[m][4 * g + w], acc[j][w]);
                         }
                     }
-                if (last) step = 0, ++x;
             });
             asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         }
@@ -432,8 +515,15 @@ int launch_moe(const MoeArgs &a, void *out, int type, hipStream_t s) {
     const int most = a.tokens * a.top < a.experts ? a.tokens * a.top : a.experts;
     const dim3 grid((unsigned)(a.chunks * most));
     const bool pieces1 = in_pieces(a.x, a.ldx, a.tokens, a.H) && in_pieces(a.W1, a.ld_w1, 2 * a.F, a.H), pieces2 = in_pieces(a.W2, a.ld_w2, a.H, a.F);
-    auto up = pieces1 ? moe_gate_up_kernel<kPieces> : (a.H >= 16 ? moe_gate_up_kernel<kAny> : moe_gate_up_kernel<kShortRows>);
-    if (int rc = QNN_LAUNCH("int8_moe", up, grid, dim3(256), 0, s, a, most)) return rc;
+    const bool routed = a.tokens * a.experts > kRoutedFrom || a.experts > kRoutedExperts;
+    // weights past the caches (20 tokens, two of 8 experts of 4096 x 2048, 201 MB: 56.3 -> 49.4 us; one token, 50 MB, which stay: 16.6 -> 17.4)
+    const bool once = pieces1 && pieces2 && rows::beyond_caches(3.0 * most * (double)a.F * (double)a.H);
+    auto up = [&](auto pieces, auto pieces_once, auto any, auto short_rows) { return pieces1 ? (once ? pieces_once : pieces) : (a.H >= 16 ? any : short_rows); };
+    auto gate_up = routed ? up(moe_gate_up_kernel<kPieces, true>, moe_gate_up_kernel<kPiecesOnce, true>, moe_gate_up_kernel<kAny, true>, moe_gate_up_kernel<kShortRows, true>)
+                          : up(moe_gate_up_kernel<kPieces, false>, moe_gate_up_kernel<kPiecesOnce, false>, moe_gate_up_kernel<kAny, false>, moe_gate_up_kernel<kShortRows, false>);
+    if (routed)
+        if (int rc = QNN_LAUNCH("int8_moe", moe_route_kernel, dim3((unsigned)a.tokens), dim3(QNN_MOE_MAX_EXPERTS), 0, s, a)) return rc;
+    if (int rc = QNN_LAUNCH("int8_moe", gate_up, grid, dim3(256), 0, s, a, most)) return rc;
     const int64_t whole = codes_pitch(a.F);
     const int slots = a.tokens * a.top;
     // a few choices: codes are made by the second kernel, two workgroups on a compute unit; many: LDS holds the results of all and the codes of one expert's 64
@@ -448,18 +538,18 @@ int launch_moe(const MoeArgs &a, void *out, int type, hipStream_t s) {
         typedef decltype(tag) T;
         const dim3 columns((unsigned)ceil_div(a.H, 16)), threads(512);
         T *const o = static_cast<T *>(out);
-        auto launch = [&](auto pieces, auto any, auto short_rows, int chunk) {
-            return QNN_LAUNCH("int8_moe", (pieces2 ? pieces : (a.F >= 16 ? any : short_rows)), columns, threads, 0, s, a, o, chunk);
+        auto launch = [&](auto pieces, auto pieces_once, auto any, auto short_rows, int chunk) {
+            return QNN_LAUNCH("int8_moe", (pieces2 ? (once ? pieces_once : pieces) : (a.F >= 16 ? any : short_rows)), columns, threads, 0, s, a, o, chunk);
         };
         if (few)
-            return launch(moe_down_kernel<T, 32, kFew, 3, kPieces, true>, moe_down_kernel<T, 32, kFew, 2, kAny, true>, moe_down_kernel<T, 32, kFew, 1, kShortRows, true>,
-                          (int)whole);
+            return launch(moe_down_kernel<T, 32, kFew, 3, kPieces, true>, moe_down_kernel<T, 32, kFew, 3, kPiecesOnce, true>, moe_down_kernel<T, 32, kFew, 2, kAny, true>,
+                          moe_down_kernel<T, 32, kFew, 1, kShortRows, true>, (int)whole);
         const int chunk = whole <= 1024 || (slots <= 128 && slots * (whole + 16) <= kMore) ? (int)whole : 1024;
         if (slots <= 128)
-            return launch(moe_down_kernel<T, 128, kMore, 3, kPieces, false>, moe_down_kernel<T, 128, kMore, 2, kAny, false>,
-                          moe_down_kernel<T, 128, kMore, 1, kShortRows, false>, chunk);
-        return launch(moe_down_kernel<T, 512, kMost, 2, kPieces, false>, moe_down_kernel<T, 512, kMost, 2, kAny, false>,
-                      moe_down_kernel<T, 512, kMost, 1, kShortRows, false>, chunk);
+            return launch(moe_down_kernel<T, 128, kMore, 3, kPieces, false>, moe_down_kernel<T, 128, kMore, 3, kPiecesOnce, false>,
+                          moe_down_kernel<T, 128, kMore, 2, kAny, false>, moe_down_kernel<T, 128, kMore, 1, kShortRows, false>, chunk);
+        return launch(moe_down_kernel<T, 512, kMost, 2, kPieces, false>, moe_down_kernel<T, 512, kMost, 2, kPiecesOnce, false>,
+                      moe_down_kernel<T, 512, kMost, 2, kAny, false>, moe_down_kernel<T, 512, kMost, 1, kShortRows, false>, chunk);
     });
 }
 

@@ -31,7 +31,7 @@ def _check(got, layer, top):
 
 SHAPES = [(1, 1, 1, 1, 1), (1, 8, 2, 64, 32), (1, 8, 2, 512, 256), (2, 3, 3, 100, 70), (5, 5, 3, 1000, 700), (16, 16, 4, 256, 128), (17, 4, 1, 300, 200), (20, 8, 2, 512, 300),
           (33, 6, 2, 200, 1500), (64, 8, 8, 130, 65), (64, 2, 1, 128, 2500), (64, 70, 5, 64, 48), (7, 256, 8, 48, 40), (3, 200, 2, 80, 17), (4, 2, 2, 5000, 16), (1, 3, 1, 40, 4200),
-          (40, 1, 1, 256, 2049), (64, 5, 4, 96, 1536), (50, 9, 4, 100, 1300), (64, 3, 2, 64, 2048), (10, 4, 3, 96, 624), (64, 6, 6, 48, 10), (30, 4, 1, 80, 6)]
+          (40, 1, 1, 256, 2049), (64, 5, 4, 96, 1536), (50, 9, 4, 100, 1300), (64, 3, 2, 64, 2048), (10, 4, 3, 96, 624), (64, 6, 6, 48, 10), (30, 4, 1, 80, 6), (9, 12, 4, 2048, 2048), (3, 12, 4, 4096, 1024), (40, 16, 4, 2048, 1536)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
@@ -70,6 +70,29 @@ def test_masked_and_tied_logits(seed, T):
     got = _call(q, layer, 3, dtype=torch.float32)
     assert (got[0] == 0).all() and torch.isnan(got[4:6]).all()
     _check(got, layer, 3)
+
+
+@pytest.mark.parametrize("T,E", [(9, 70), (64, 256)])
+def test_masked_logits_of_many_experts(seed, T, E):
+    import paper_1609_07061_amd as q
+
+    layer = _layer(seed, T, E, 64, 40)
+    l = layer[2]
+    l[0] = -math.inf
+    l[1] = -math.inf
+    l[1, E - 1] = 0.5
+    l[2] = 1.0                                # the first five
+    l[3] = torch.finfo(torch.float32).min
+    l[4, 2] = math.nan
+    l[5, E - 2] = math.inf
+    l[6, : E - 3] = -math.inf                 # three of five
+    l[7] = 0.0
+    l[7, ::2] = -0.0
+    l[8:] = -math.inf
+    l[8:, 17:22] = torch.arange(5.0)          # all the others on five experts
+    got = _call(q, layer, 5, dtype=torch.float32)
+    assert (got[0] == 0).all() and torch.isnan(got[4:6]).all()
+    _check(got, layer, 5)
 
 
 def test_values(seed):
