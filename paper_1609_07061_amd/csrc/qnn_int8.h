@@ -182,6 +182,11 @@ inline bool in_pieces(const int8_t *p, int64_t ld, int64_t n_rows, int64_t K) {
     return K % 16 == 0 && ld % 16 == 0 && rows::aligned_to(p, 16) && (long double)n_rows * ld < 4294967296.0L;
 }
 
+// Rows of whole 4-byte words at 4-byte aligned addresses, within 4 GiB
+inline bool in_words(const int8_t *p, int64_t ld, int64_t n_rows, int64_t K) {
+    return K % 4 == 0 && ld % 4 == 0 && rows::aligned_to(p, 4) && (long double)n_rows * ld < 4294967296.0L;
+}
+
 // Products with K codes of at most 128 in magnitude are exact in int32
 constexpr int64_t kMostK = 131071;
 

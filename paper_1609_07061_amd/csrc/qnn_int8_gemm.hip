@@ -83,8 +83,8 @@ __global__ __launch_bounds__(64 * kWaves) void gemm_stream_kernel(const Args<T> 
 }
 
 // 128 x 128 on four waves of 64 x 64, two workgroups on a compute unit; groups of 128 codes through registers to LDS, two buffers; rows of any length at
-// any address (K >= 16).  A group's loads are sent two groups ahead (one ahead, their latency was half of the time: 1999 x 3001 x 2500 38.2 -> 34.4 us).  16-byte piece
-// c of row r sits at piece c xor (r / 2 mod 8): the 16 rows that a read serves at a time lie on different banks.
+// any address (K >= 16).  A group's loads are sent two groups ahead (one ahead, their latency was half of the time: 1999 x 3001 x 2500 38.2 us, and 34.4).
+// 16-byte piece c of row r sits at piece c xor (r / 2 mod 8): the 16 rows that a read serves at a time lie on different banks.
 constexpr int kTile = 128, kGroup = 128, kPanel = kTile * kGroup;
 
 template <typename T>
@@ -222,6 +222,12 @@ constexpr Way kWaysOfPieces[] = {{kStream16x16, 16, 16, 2.7, 0.56, 0.276}, {kStr
                                  {kPanel256, 256, 256, 6.4, 9.10, 8.518}};
 constexpr Way kWaysOfAny[] = {{kStream16x16, 16, 16, 2.8, 0.25, 0.706}, {kStream64x16, 64, 16, 3.8, 0.98, 1.650}, {kStream64x32, 64, 32, 4.4, 3.44, 2.090},
                               {kStream64x64, 64, 64, 6.1, 5.48, 2.843}, {kTile128, 128, 128, 7.1, 3.11, 6.853}};
+// Rows of whole words: the streams' as above, panels fitted to 75 products of 60 .. 8192 rows, where the way ahead is 1.0 % slower than the fastest in the
+// mean.  (300 x 4100 x 3004: 64 x 64 18.4 us, without panels 25.0; 4000 x 4000 x 4004: 256 x 256 69.5, 128 x 128 94.5, without panels 104; 1999 x 3001 x 2500:
+// 128 x 128 36.9, without panels 37.7.)
+constexpr Way kWaysOfWords[] = {{kStream16x16, 16, 16, 2.8, 0.25, 0.706}, {kStream64x16, 64, 16, 3.8, 0.98, 1.650}, {kStream64x32, 64, 32, 4.4, 3.44, 2.090},
+                                {kStream64x64, 64, 64, 6.1, 5.48, 2.843}, {kPanel64, 64, 64, 5.4, 0.80, 2.486},     {kPanel128, 128, 128, 6.8, 1.21, 5.749},
+                                {kPanel256, 256, 256, 9.8, 11.65, 12.12}};
 template <int kCount>
 const Way &fastest(const Way (&ways)[kCount], int64_t M, int64_t N, int64_t K) {
     const Way *best = nullptr;
@@ -237,16 +243,24 @@ const Way &fastest(const Way (&ways)[kCount], int64_t M, int64_t N, int64_t K) {
 template <typename T>
 int launch(const Args<T> &a, hipStream_t s) {
     const bool pieces = in_pieces(a.A, a.lda, a.M, a.K) && in_pieces(a.W, a.ldw, a.N, a.K), any = !pieces && a.K >= 16;
-    const Way &w = pieces ? fastest(kWaysOfPieces, a.M, a.N, a.K) : (any ? fastest(kWaysOfAny, a.M, a.N, a.K) : kWaysOfAny[0]);
+    const bool words = any && in_words(a.A, a.lda, a.M, a.K) && in_words(a.W, a.ldw, a.N, a.K);
+    const Way &w = pieces  ? fastest(kWaysOfPieces, a.M, a.N, a.K)
+                   : words ? fastest(kWaysOfWords, a.M, a.N, a.K)
+                   : any   ? fastest(kWaysOfAny, a.M, a.N, a.K)
+                           : kWaysOfAny[0];
     const int64_t tm = ceil_div(a.M, w.rows), tn = ceil_div(a.N, w.columns);
     // (8 columns of tiles and what lies in them have 32 bits)
-    if (tm > 0x7FFFFFFFLL || tn > 0x0FFFFFFFLL || tm * tn > 0x7FFFFFFFLL) return fail(QNN_ERR_SHAPE, "int8_gemm: M = %lld, N = %lld", (long long)a.M, (long long)a.N);
+    if (tm > 0x7FFFFFFFLL || tn > 0x0FFFFFFFLL || tm * tn > 0x7FFFFFFFLL)
+        return fail(QNN_ERR_SHAPE, "int8_gemm: M = %lld, N = %lld", (long long)a.M, (long long)a.N);
     const Tiles tiles = make_tiles(tm, tn);
     const dim3 grid((unsigned)(tm * tn));
     auto stream = [&](auto on_pieces, auto on_any) { return QNN_LAUNCH("int8_gemm", (pieces ? on_pieces : on_any), grid, dim3(512), 0, s, a, tiles); };
-    auto panels = [&](auto kernel, int threads, int per_unit) {
-        const int64_t most = (int64_t)compute_units() * per_unit;
-        return QNN_LAUNCH("int8_gemm", kernel, dim3((unsigned)(tm * tn < most ? tm * tn : most)), dim3(threads), 0, s, a, tiles, (uint32_t)ceil_div(a.K, panel::kRow));
+    auto panels = [&](auto shape, auto shape_of_words) {
+        typedef decltype(shape) S;
+        const int64_t most = (int64_t)compute_units() * S::kPerUnit;
+        auto kernel = words ? panel::gemm_panel_kernel<T, decltype(shape_of_words)> : panel::gemm_panel_kernel<T, S>;
+        return QNN_LAUNCH("int8_gemm", kernel, dim3((unsigned)(tm * tn < most ? tm * tn : most)), dim3(S::kThreads), 0, s, a, tiles,
+                          (uint32_t)ceil_div(a.K, panel::kRow));
     };
     if (!pieces && !any) return QNN_LAUNCH("int8_gemm", (gemm_stream_kernel<T, 1, 1, 8, 1, kShortRows>), grid, dim3(512), 0, s, a, tiles);
     switch (w.id) {
@@ -254,9 +268,9 @@ int launch(const Args<T> &a, hipStream_t s) {
     case kStream64x16: return stream(gemm_stream_kernel<T, 1, 4, 8, 2, kPieces>, gemm_stream_kernel<T, 1, 4, 8, 1, kAny>);
     case kStream64x32: return stream(gemm_stream_kernel<T, 2, 4, 8, 1, kPieces>, gemm_stream_kernel<T, 2, 4, 8, 1, kAny>);
     case kStream64x64: return stream(gemm_stream_kernel<T, 4, 4, 8, 1, kPieces>, gemm_stream_kernel<T, 4, 4, 8, 1, kAny>);
-    case kPanel64: return panels(panel::gemm_panel_kernel<T, panel::Tiny>, panel::Tiny::kThreads, panel::Tiny::kPerUnit);
-    case kPanel128: return panels(panel::gemm_panel_kernel<T, panel::Small>, panel::Small::kThreads, panel::Small::kPerUnit);
-    case kPanel256: return panels(panel::gemm_panel_kernel<T, panel::Large>, panel::Large::kThreads, panel::Large::kPerUnit);
+    case kPanel64: return panels(panel::Tiny(), panel::TinyWords());
+    case kPanel128: return panels(panel::Small(), panel::SmallWords());
+    case kPanel256: return panels(panel::Large(), panel::LargeWords());
     case kTile128: return QNN_LAUNCH("int8_gemm", gemm_tile_kernel<T>, grid, dim3(256), 0, s, a, tiles);
     }
     return fail(QNN_ERR_UNSUPPORTED, "int8_gemm: no way");

@@ -116,7 +116,8 @@ __global__ __launch_bounds__(QNN_MOE_MAX_EXPERTS) void moe_route_kernel(const Mo
 
 // kTiles of 16 tokens: what a workgroup of the first kernel does once it knows its tokens
 template <int kTiles, Layout kLayout>
-__device__ __forceinline__ void gate_up(const MoeArgs &a, int e, int chunk, const int *list, const int *slot_of, const float *scale_of, int count, uint8_t *lds) {
+__device__ __forceinline__ void gate_up(const MoeArgs &a, int e, int chunk, const int *list, const int *slot_of, const float *scale_of, int count,
+                                        uint8_t *lds) {
     constexpr int kWaves = 4, kStages = kTiles == 1 ? 3 : (kTiles == 2 ? 2 : 1);
     typedef Stream<2, kTiles, kStages, kLayout> S;
     static_assert(S::kBytes * kWaves <= kRingBytes && kWaves * 2 * 16 * kTiles * 17 * 4 <= kRingBytes, "");
@@ -329,7 +330,8 @@ __global__ __launch_bounds__(512) void moe_down_kernel(const MoeArgs a, T *out, 
     const int64_t n0 = (int64_t)blockIdx.x * 16;
     const uint32_t F = (uint32_t)a.F;
     const int pitch = chunk + 16, most = kCodes / pitch;
-    const bool at_once = kQuantize || (slots <= most && F <= (uint32_t)chunk);  // then rows of codes are in the order of the choices, else in that of the experts
+    // everything at once: rows of codes are in the order of the choices, else in that of the experts
+    const bool at_once = kQuantize || (slots <= most && F <= (uint32_t)chunk);
     // kQuantize: 1024 activations of a row by a wave, four loads of whole lines; the first kItems of a wave's are on their way from here on
     constexpr int kItems = 2;
     float v[kItems][4][4];
@@ -399,7 +401,8 @@ __global__ __launch_bounds__(512) void moe_down_kernel(const MoeArgs a, T *out, 
         const int n_rows = __builtin_amdgcn_readfirstlane(start[to]) - first_row;
         for (uint32_t f0 = 0; f0 < F; f0 += (uint32_t)chunk) {
             // the steps of all experts here, expert by expert, blocks of 128 of them: a wave has every eighth; the loads' cursor and the products'
-            const int blocks = (int)((min(F, f0 + (uint32_t)chunk) - f0 + 127u) / 128u), all = blocks * (to - from), steps = all > wave ? (all - wave - 1) / kWaves + 1 : 0;
+            const int blocks = (int)((min(F, f0 + (uint32_t)chunk) - f0 + 127u) / 128u), all = blocks * (to - from);
+            const int steps = all > wave ? (all - wave - 1) / kWaves + 1 : 0;
             int send_x = from + wave / blocks, send_block = wave % blocks, x = send_x, block = send_block;
             auto next = [&](int &x, int &block) __attribute__((always_inline)) {
                 block += kWaves;
@@ -459,14 +462,15 @@ __global__ __launch_bounds__(512) void moe_down_kernel(const MoeArgs a, T *out, 
                 for (int i = t; i < 16 * slots; i += 512) factor[i >> 4][i & 15] = share(i >> 4, min(n0 + (i & 15), a.H - 1), sum_of((i >> 4) / a.top));
             }
             asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // (weights may still be on their way)
-            v4i acc[4];
-            int row[4], first = 0, count = 0;
+            constexpr int kBlocks = kSlots < 64 ? kSlots / 16 : 4;  // of 16 tokens of an expert
+            v4i acc[kBlocks];
+            int row[kBlocks], first = 0, count = 0;
             bool other = true;
             s.run(steps, base, at, [&](int, const typename S::Operands &o) __attribute__((always_inline)) {
                 if (other) {
                     first = __builtin_amdgcn_readfirstlane(start[x]), count = __builtin_amdgcn_readfirstlane(start[x + 1]) - first;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
+                    for (int j = 0; j < kBlocks; ++j) {
                         const int pos = first + min(16 * j + r, count - 1);
                         row[j] = (at_once ? order[pos] : pos - first_row) * pitch, acc[j] = v4i{0, 0, 0, 0};
                     }
@@ -474,7 +478,7 @@ __global__ __launch_bounds__(512) void moe_down_kernel(const MoeArgs a, T *out, 
                 const int k = 128 * block + 16 * g;
                 other = next(x, block);
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
+                for (int j = 0; j < kBlocks; ++j)
                     if (16 * j < count) {
 #pragma unroll
                         for (int h = 0; h < 2; ++h)
@@ -518,9 +522,13 @@ int launch_moe(const MoeArgs &a, void *out, int type, hipStream_t s) {
     const bool routed = a.tokens * a.experts > kRoutedFrom || a.experts > kRoutedExperts;
     // weights past the caches (20 tokens, two of 8 experts of 4096 x 2048, 201 MB: 56.3 -> 49.4 us; one token, 50 MB, which stay: 16.6 -> 17.4)
     const bool once = pieces1 && pieces2 && rows::beyond_caches(3.0 * most * (double)a.F * (double)a.H);
-    auto up = [&](auto pieces, auto pieces_once, auto any, auto short_rows) { return pieces1 ? (once ? pieces_once : pieces) : (a.H >= 16 ? any : short_rows); };
-    auto gate_up = routed ? up(moe_gate_up_kernel<kPieces, true>, moe_gate_up_kernel<kPiecesOnce, true>, moe_gate_up_kernel<kAny, true>, moe_gate_up_kernel<kShortRows, true>)
-                          : up(moe_gate_up_kernel<kPieces, false>, moe_gate_up_kernel<kPiecesOnce, false>, moe_gate_up_kernel<kAny, false>, moe_gate_up_kernel<kShortRows, false>);
+    auto up = [&](auto pieces, auto pieces_once, auto any, auto short_rows) {
+        return pieces1 ? (once ? pieces_once : pieces) : (a.H >= 16 ? any : short_rows);
+    };
+    auto gate_up = routed ? up(moe_gate_up_kernel<kPieces, true>, moe_gate_up_kernel<kPiecesOnce, true>, moe_gate_up_kernel<kAny, true>,
+                               moe_gate_up_kernel<kShortRows, true>)
+                          : up(moe_gate_up_kernel<kPieces, false>, moe_gate_up_kernel<kPiecesOnce, false>, moe_gate_up_kernel<kAny, false>,
+                               moe_gate_up_kernel<kShortRows, false>);
     if (routed)
         if (int rc = QNN_LAUNCH("int8_moe", moe_route_kernel, dim3((unsigned)a.tokens), dim3(QNN_MOE_MAX_EXPERTS), 0, s, a)) return rc;
     if (int rc = QNN_LAUNCH("int8_moe", gate_up, grid, dim3(256), 0, s, a, most)) return rc;
@@ -541,15 +549,17 @@ int launch_moe(const MoeArgs &a, void *out, int type, hipStream_t s) {
         auto launch = [&](auto pieces, auto pieces_once, auto any, auto short_rows, int chunk) {
             return QNN_LAUNCH("int8_moe", (pieces2 ? (once ? pieces_once : pieces) : (a.F >= 16 ? any : short_rows)), columns, threads, 0, s, a, o, chunk);
         };
+        // (Few steps under way where there is little to do: each one more is code to fetch, which a short kernel waits for.  One token, two of 8 experts of
+        // 4096 x 2048: 7.07 us, with a third 7.45; rows of any length: with four 9.9 us where one takes 9.3.)
         if (few)
-            return launch(moe_down_kernel<T, 32, kFew, 3, kPieces, true>, moe_down_kernel<T, 32, kFew, 3, kPiecesOnce, true>, moe_down_kernel<T, 32, kFew, 2, kAny, true>,
-                          moe_down_kernel<T, 32, kFew, 1, kShortRows, true>, (int)whole);
+            return launch(moe_down_kernel<T, 32, kFew, 2, kPieces, true>, moe_down_kernel<T, 32, kFew, 2, kPiecesOnce, true>,
+                          moe_down_kernel<T, 32, kFew, 1, kAny, true>, moe_down_kernel<T, 32, kFew, 1, kShortRows, true>, (int)whole);
         const int chunk = whole <= 1024 || (slots <= 128 && slots * (whole + 16) <= kMore) ? (int)whole : 1024;
         if (slots <= 128)
             return launch(moe_down_kernel<T, 128, kMore, 3, kPieces, false>, moe_down_kernel<T, 128, kMore, 3, kPiecesOnce, false>,
-                          moe_down_kernel<T, 128, kMore, 2, kAny, false>, moe_down_kernel<T, 128, kMore, 1, kShortRows, false>, chunk);
+                          moe_down_kernel<T, 128, kMore, 1, kAny, false>, moe_down_kernel<T, 128, kMore, 1, kShortRows, false>, chunk);
         return launch(moe_down_kernel<T, 512, kMost, 2, kPieces, false>, moe_down_kernel<T, 512, kMost, 2, kPiecesOnce, false>,
-                      moe_down_kernel<T, 512, kMost, 2, kAny, false>, moe_down_kernel<T, 512, kMost, 1, kShortRows, false>, chunk);
+                      moe_down_kernel<T, 512, kMost, 1, kAny, false>, moe_down_kernel<T, 512, kMost, 1, kShortRows, false>, chunk);
     });
 }
 

@@ -1,10 +1,14 @@
 // Large products of int8 codes with scales: both operands through LDS in whole 128-byte lines (global_load_lds), sums on the matrix cores
-// (v_mfma_i32_16x16x64_i8), scales and rounding on the way out.  Rows of whole 16-byte pieces at 16-byte aligned addresses.
+// (v_mfma_i32_16x16x64_i8), scales and rounding on the way out.  Rows of whole 16-byte pieces at 16-byte aligned addresses, or of 4-byte words.
 //
-// As in gemm_bytes_panel_kernel, a group of 128 codes of k is in one of two LDS buffers while the next is loaded, 16-byte piece c of row r at piece c xor
-// (r / 2 mod 8), and a persistent workgroup runs from tile to tile, its loads two groups ahead of its products, so that a tile's end has the next one's
-// operands in flight.  What is different is the way out (floats, half as wide or as wide as the sums) and that nothing pads the operands: codes of k
+// As in gemm_bytes_panel_kernel, a group of 128 codes of k is in an LDS buffer while others are loaded, 16-byte piece c of row r at piece c xor (r / 2 mod 8),
+// and a persistent workgroup runs from tile to tile, its loads as many groups ahead of its products as there are buffers, so that a tile's end has the next
+// one's operands in flight.  What is different is the way out (floats, half as wide or as wide as the sums) and that nothing pads the operands: codes of k
 // beyond the rows are loaded from the rows' beginning and zeroed on one side behind LDS.
+//
+// What bounds it: at 8192 x 8192 x 8192 the card's power (codes of a normal distribution: 403 - 417 us, 2.6 - 2.7 P op/s, the matrix cores busy 73 % of
+// 710 k cycles at 1.76 GHz; all zeros run at 2.44 GHz).  16 x 16 x 64 instead of 32 x 32 x 32 matrix instructions: half as many updates of sums a product,
+// 484 -> 425 us.  At middle sizes the fixed part and LDS: 64 x 64 sums a wave read 64 KB and write 32 KB of LDS for 512 cycles of matrix instructions.
 #pragma once
 #include "qnn_int8.h"
 
@@ -25,11 +29,13 @@ constexpr int kRow = 128;  // codes of a row in a group
 
 // WM x WN waves, each with 32 BA rows of A and 32 BW rows of W; kRing groups in LDS; kPerUnit workgroups on a compute unit.  (Two such teams of waves on
 // alternate groups of k were no faster than one: 1024 x 4096 x 4096 on 128 x 128 24.0 us, one team with four groups in LDS 24.5.)
-template <int WM_, int WN_, int BA_, int BW_, int kRing_, int kPerUnit_>
+template <int WM_, int WN_, int BA_, int BW_, int kRing_, int kPerUnit_, bool kWords_ = false>
 struct Shape {
     static constexpr int WM = WM_, WN = WN_, BA = BA_, BW = BW_, kRing = kRing_, kPerUnit = kPerUnit_;
     static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves, kRowsA = 32 * BA * WM, kRowsW = 32 * BW * WN;
-    static constexpr int kLoadsA = kRowsA / (8 * kWaves), kLoadsW = kRowsW / (8 * kWaves), kLoads = kLoadsA + kLoadsW;  // a wave's of a group, 8 rows each
+    static constexpr bool kWords = kWords_;  // rows of whole 4-byte words at 4-byte aligned addresses, loaded word by word
+    static constexpr int kPart = kWords ? 4 : 1;  // loads of 8 rows
+    static constexpr int kLoadsA = kPart * kRowsA / (8 * kWaves), kLoadsW = kPart * kRowsW / (8 * kWaves), kLoads = kLoadsA + kLoadsW;  // a wave's of a group
     static constexpr int kGroup = (kRowsA + kRowsW) * kRow, kStage = 4096;  // bytes of a group; of a wave's part of the way out
     static constexpr int kLds = kRing * kGroup + kWaves * kStage;
     static_assert(kRowsA % (8 * kWaves) == 0 && kRowsW % (8 * kWaves) == 0 && kWaves % 2 == 0 && kLds * kPerUnit <= 160 * 1024, "");
@@ -51,24 +57,31 @@ __global__ __launch_bounds__(S::kThreads, S::kThreads / 256 * S::kPerUnit) void 
         return x;
     };
 
-    // ---- loads.  The cursor (tile p_vb, group p_G) runs kRing groups ahead.  Load i of an operand brings rows 8 (kWaves i + wave) .. + 7 of its panel: lane
-    // l lands in piece l mod 8 of row l / 8 and fetches piece (l mod 8) xor (row / 2 mod 8).
+    // ---- loads.  The cursor (tile p_vb, group p_G) runs kRing groups ahead.  The waves have 8 rows each in turn.  Pieces: a load brings 8 rows, lane l lands
+    // in piece l mod 8 of row l / 8 and fetches piece (l mod 8) xor (row / 2 mod 8).  Words: a load brings 2 rows, lane l lands in word l mod 32 of row l / 32.
     const uint32_t n_mine = (tiles.total - blockIdx.x + gridDim.x - 1u) / gridDim.x;
-    uint32_t p_vb = blockIdx.x, p_G = 0, p_item = 0, p_k = 0;
+    constexpr int kPart = S::kPart;
+    uint32_t p_vb = blockIdx.x, p_G = 0, p_item = 0, p_k[kPart];
     uint32_t off_a[S::kLoadsA], off_w[S::kLoadsW];
     auto p_locate = [&]() __attribute__((always_inline)) {
         uint32_t tm, tn;
         tile_of_block(p_vb, tiles, tm, tn);
-        const uint32_t row = 8u * wave + ((opaque(tid) & 63u) >> 3);
+        const uint32_t lane = opaque(tid) & 63u, row = 8u * wave + (S::kWords ? lane >> 5 : lane >> 3);
+        auto row_of = [&](int i) { return row + (uint32_t)(8 * S::kWaves * (i / kPart) + 2 * (i % kPart)); };
 #pragma unroll
-        for (int i = 0; i < S::kLoadsA; ++i) off_a[i] = min(tm * (uint32_t)S::kRowsA + (uint32_t)(8 * S::kWaves * i) + row, last_m) * lda;
+        for (int i = 0; i < S::kLoadsA; ++i) off_a[i] = min(tm * (uint32_t)S::kRowsA + row_of(i), last_m) * lda;
 #pragma unroll
-        for (int i = 0; i < S::kLoadsW; ++i) off_w[i] = min(tn * (uint32_t)S::kRowsW + (uint32_t)(8 * S::kWaves * i) + row, last_n) * ldw;
+        for (int i = 0; i < S::kLoadsW; ++i) off_w[i] = min(tn * (uint32_t)S::kRowsW + row_of(i), last_n) * ldw;
     };
     auto p_piece = [&]() __attribute__((always_inline)) {
         const uint32_t t = opaque(tid);
-        const uint32_t k = p_G * (uint32_t)kRow + (((t & 7u) ^ ((t >> 4) & 7u)) << 4);  // (the row is t / 8, and more by multiples of 16)
-        p_k = k < K ? k : 0u;  // a piece beyond the rows: their beginning
+#pragma unroll
+        for (int j = 0; j < kPart; ++j) {
+            // (row / 2 mod 8: of rows t / 8 and, words, 8 wave + 2 j + ..; more by multiples of 16)
+            const uint32_t in = S::kWords ? (((((t & 31u) >> 2) ^ ((4u * wave + j) & 7u)) << 4) | ((t & 3u) << 2)) : (((t & 7u) ^ ((t >> 4) & 7u)) << 4);
+            const uint32_t k = p_G * (uint32_t)kRow + in;
+            p_k[j] = k < K ? k : 0u;  // beyond the rows: their beginning
+        }
     };
     auto p_advance = [&]() __attribute__((always_inline)) {
         ++p_G;
@@ -81,20 +94,27 @@ __global__ __launch_bounds__(S::kThreads, S::kThreads / 256 * S::kPerUnit) void 
         }
         p_piece();
     };
-    auto load16_to_lds = [](const void *base, uint32_t voff, uint32_t vadd, uint32_t lds_addr) __attribute__((always_inline)) {
+    auto load_to_lds = [](const void *base, uint32_t voff, uint32_t vadd, uint32_t lds_addr) __attribute__((always_inline)) {
         uint32_t tmp;
-        asm volatile("s_mov_b32 m0, %1\n\tv_add_u32 %0, %2, %3\n\tglobal_load_lds_dwordx4 %0, %4"
-                     : "=&v"(tmp)
-                     : "s"(lds_addr), "v"(voff), "v"(vadd), "s"(base)
-                     : "memory");
+        if constexpr (S::kWords)
+            asm volatile("s_mov_b32 m0, %1\n\tv_add_u32 %0, %2, %3\n\tglobal_load_lds_dword %0, %4"
+                         : "=&v"(tmp)
+                         : "s"(lds_addr), "v"(voff), "v"(vadd), "s"(base)
+                         : "memory");
+        else
+            asm volatile("s_mov_b32 m0, %1\n\tv_add_u32 %0, %2, %3\n\tglobal_load_lds_dwordx4 %0, %4"
+                         : "=&v"(tmp)
+                         : "s"(lds_addr), "v"(voff), "v"(vadd), "s"(base)
+                         : "memory");
     };
     constexpr int kLoads = S::kLoads;
     auto load = [&](const int i, const uint32_t buf) __attribute__((always_inline)) {
         const uint32_t dst = lds_base + buf + wave * (8u * kRow);
+        auto at = [](int i) { return (uint32_t)(i / kPart * 8 * S::kWaves * kRow + i % kPart * 2 * kRow); };
         if (i < S::kLoadsA)
-            load16_to_lds(a.A, off_a[i < S::kLoadsA ? i : 0], p_k, dst + (uint32_t)(i * 8 * S::kWaves * kRow));
+            load_to_lds(a.A, off_a[i < S::kLoadsA ? i : 0], p_k[i % kPart], dst + at(i));
         else
-            load16_to_lds(a.W, off_w[i < S::kLoadsA ? 0 : i - S::kLoadsA], p_k, dst + (uint32_t)((S::kRowsA + (i - S::kLoadsA) * 8 * S::kWaves) * kRow));
+            load_to_lds(a.W, off_w[i < S::kLoadsA ? 0 : i - S::kLoadsA], p_k[i % kPart], dst + (uint32_t)(S::kRowsA * kRow) + at(i - S::kLoadsA));
     };
 
     // ---- products: blocks of 16 x 16, 64 codes at a time (step 0, 1 of a group)
@@ -119,8 +139,14 @@ __global__ __launch_bounds__(S::kThreads, S::kThreads / 256 * S::kPerUnit) void 
     auto clear_beyond = [&](v4i (&f)[NW], const uint32_t k_end, const int s) __attribute__((always_inline)) {
         const uint32_t k = k_end - (uint32_t)kRow + 64u * s + 16u * ((opaque(tid) & 63u) >> 4);
 #pragma unroll
-        for (int i = 0; i < NW; ++i)
-            if (k >= K) f[i] = v4i{0, 0, 0, 0};
+        for (int i = 0; i < NW; ++i) {
+            if constexpr (S::kWords) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) f[i][e] = k + 4u * e < K ? f[i][e] : 0;
+            } else {
+                if (k >= K) f[i] = v4i{0, 0, 0, 0};
+            }
+        }
     };
 
     // ---- a tile's way out: 32 rows x 128 bytes at a time through the wave's part of LDS, rows of 128 bytes leave as they are
@@ -274,6 +300,10 @@ __global__ __launch_bounds__(S::kThreads, S::kThreads / 256 * S::kPerUnit) void 
 typedef Shape<2, 4, 4, 2, 2, 1> Large;  // 256 x 256
 typedef Shape<2, 2, 2, 2, 2, 2> Small;  // 128 x 128
 typedef Shape<2, 2, 1, 1, 4, 2> Tiny;   // 64 x 64
+// the same for words (a line of 256 bytes a load: slower by half, but 4000 x 4000 x 4004 104 us through registers, 69.5 like this)
+typedef Shape<2, 4, 4, 2, 2, 1, true> LargeWords;
+typedef Shape<2, 2, 2, 2, 2, 2, true> SmallWords;
+typedef Shape<2, 2, 1, 1, 4, 2, true> TinyWords;
 
 }  // namespace panel
 }  // namespace int8

@@ -27,12 +27,15 @@ PIECES = [("stream", 3, 40, 16), ("stream", 16, 4096, 1040), ("stream", 60, 4000
           ("panel", 700, 1000, 272), ("panel", 1200, 1024, 1040), ("panel", 5000, 130, 528), ("panel", 300, 4100, 144), ("panel", 1190, 4000, 1008), ("panel", 5000, 1000, 400),
           ("panel", 130, 20000, 656), ("panel", 5000, 4099, 16), ("panel", 9000, 9001, 256), ("panel", 5003, 4097, 1168), ("panel", 7000, 8000, 128), ("panel", 2560, 16384, 384)]
 # any rows: streams, the tiled kernel; fewer codes than a piece
-ANY = [("stream", 2, 40, 17), ("stream", 16, 4095, 1001), ("stream", 60, 4000, 4093), ("stream", 120, 4096, 1023), ("stream", 256, 4090, 2047), ("tile", 1999, 1001, 2500), ("tile", 1000, 4001, 17),
+ANY = [("stream", 2, 40, 17), ("stream", 16, 4095, 1001), ("stream", 60, 4000, 4093), ("stream", 120, 4096, 1023), ("stream", 256, 4090, 2047), ("tile", 1999, 1001, 2501), ("tile", 1000, 4001, 17),
        ("tile", 3000, 3000, 127), ("tile", 2500, 2049, 129), ("tile", 4000, 2500, 385), ("tile", 1500, 3000, 250), ("stream", 100, 900, 15), ("stream", 1, 5000, 1), ("stream", 3000, 70, 8)]
+# whole 4-byte words: streams, panels (64, 128, 256)
+WORDS = [("stream", 150, 1000, 1500), ("stream", 700, 300, 300), ("panel", 300, 4100, 1500), ("panel", 700, 2500, 20), ("panel", 300, 4100, 300), ("panel", 1999, 1001, 2500),
+         ("panel", 1500, 3001, 516), ("panel", 4000, 1000, 132), ("panel", 4003, 4097, 1284), ("panel", 9000, 9001, 252), ("panel", 7000, 8000, 124), ("panel", 2500, 2049, 1148)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("kind,M,N,K", PIECES + ANY)
+@pytest.mark.parametrize("kind,M,N,K", PIECES + ANY + WORDS)
 def test_way(seed, kind, M, N, K, dtype):
     import paper_1609_07061_amd as q
 
@@ -42,13 +45,14 @@ def test_way(seed, kind, M, N, K, dtype):
     assert _kernel(lambda: q.qnn_int8_gemm(A, sA, W, sW, dtype=dtype)) == f"gemm_{kind}_kernel"
 
 
-@pytest.mark.parametrize("kind,M,N,K", [("stream", 60, 4000, 4096), ("panel", 1200, 1024, 1040), ("panel", 1190, 4000, 1008), ("panel", 9000, 9001, 256), ("stream", 60, 4000, 4093), ("tile", 1500, 3000, 250)])
+@pytest.mark.parametrize("kind,M,N,K", [("stream", 60, 4000, 4096), ("panel", 1200, 1024, 1040), ("panel", 1190, 4000, 1008), ("panel", 9000, 9001, 256), ("stream", 60, 4000, 4093), ("tile", 1500, 3000, 250),
+                                        ("panel", 300, 4100, 308), ("panel", 1500, 3001, 260), ("panel", 9000, 9001, 260)])
 def test_way_into_the_middle(seed, kind, M, N, K):
     """Outputs with a pitch, at odd addresses, operands with a pitch: nothing else is written."""
     import paper_1609_07061_amd as q
 
     A, sA, W, sW, bias = _operands(seed, M, N, K)
-    pad = 16 if K % 16 == 0 else 5
+    pad = 16 if K % 16 == 0 else 4 if kind == "panel" else 5
     a, w = placed(A, pad, pad, 99)[1], placed(W, 2 * pad, 3 * pad, 99)[1]
     for dtype, pad_o, at in ((torch.float32, 3, 1), (torch.bfloat16, 7, 3), (torch.float16, 8, 8)):
         whole, out = placed(torch.zeros(M, N, dtype=dtype, device="cuda"), pad_o, at, 7.0)
