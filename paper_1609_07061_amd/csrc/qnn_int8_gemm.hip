@@ -207,33 +207,38 @@ __global__ __launch_bounds__(256, 2) void gemm_tile_kernel(const Args<T> a, cons
 }
 
 // The ways a product can go, by rows and columns of a workgroup's tile, and about how long each takes (us): start + more (R - 1) + k R K / 1024, with R the
-// rounds of one tile a compute unit.  Fitted to 66 products of 8 .. 5000 rows, 256 .. 4096 columns and K of 512 .. 7168 each, where the way that comes out
-// ahead is 1.4 % (any rows: 0.9 %) slower than the fastest in the mean.  (us of the fastest ways at N = K = 4096, M = 16: 16 x 16 5.7, 64 x 16 6.2; 64: 7.2
-// of 64 x 16, 8.3 and 7.7 of those beside it; 128: 64 x 32 8.1, 64 x 64 10.6; 256: 64 x 64 11.5, panels 12.7, 64 x 32 14.1; 512: panels of 64 x 64 17.0, of
-// 128 x 128 24.6; 1200: 36.0 and 28.5; 5000: 128 x 128 86, 256 x 256 90; 8192 x 8192 x 8192: 524 and 417.)
-enum WayId { kStream16x16, kStream64x16, kStream64x32, kStream64x64, kPanel64, kPanel128, kPanel256, kTile128 };
+// rounds of `side` tiles a compute unit.  Fitted to 66 products of 8 .. 5000 rows, 256 .. 4096 columns and K of 512 .. 7168 each (those on 128 x 128 to 28 of
+// 500 .. 4000 rows), where the way that comes out ahead is 1 % slower than the fastest in the mean.  (us of the fastest ways at N = K = 4096, M = 16:
+// 16 x 16 5.7, 64 x 16 6.2; 64: 7.2 of 64 x 16, 8.3 and 7.7 of those beside it; 128: 64 x 32 8.1, 64 x 64 10.6; 256: 64 x 64 11.5, panels 12.7, 64 x 32 14.1;
+// 512: panels of 64 x 64 17.8, of 128 x 128 18.3 on eight waves and 24.8 on four; 1024: 27.5, 23.7 and 28.6; 2000: 43.6 on eight and 38.2 on four; 5000: 86 on
+// four, 256 x 256 90; 8192 x 8192 x 8192: 524 and 417.)
+enum WayId { kStream16x16, kStream64x16, kStream64x32, kStream64x64, kPanel64, kPanel128, kPanel128Pairs, kPanel256, kTile128 };
 struct Way {
     WayId id;
-    int rows, columns;
+    int rows, columns, side;
     double start, more, k;
 };
-constexpr Way kWaysOfPieces[] = {{kStream16x16, 16, 16, 2.7, 0.56, 0.276}, {kStream64x16, 64, 16, 3.1, 1.95, 0.743}, {kStream64x32, 64, 32, 3.3, 2.37, 0.924},
-                                 {kStream64x64, 64, 64, 4.3, 3.93, 1.306}, {kPanel64, 64, 64, 3.6, 0.03, 1.838},     {kPanel128, 128, 128, 4.1, 0.0, 4.254},
-                                 {kPanel256, 256, 256, 6.4, 9.10, 8.518}};
-constexpr Way kWaysOfAny[] = {{kStream16x16, 16, 16, 2.8, 0.25, 0.706}, {kStream64x16, 64, 16, 3.8, 0.98, 1.650}, {kStream64x32, 64, 32, 4.4, 3.44, 2.090},
-                              {kStream64x64, 64, 64, 6.1, 5.48, 2.843}, {kTile128, 128, 128, 7.1, 3.11, 6.853}};
+constexpr Way kWaysOfPieces[] = {{kStream16x16, 16, 16, 1, 2.7, 0.56, 0.276},     {kStream64x16, 64, 16, 1, 3.1, 1.95, 0.743}, {kStream64x32, 64, 32, 1, 3.3, 2.37, 0.924},
+                                 {kStream64x64, 64, 64, 1, 4.3, 3.93, 1.306},     {kPanel64, 64, 64, 1, 3.6, 0.03, 1.838},     {kPanel128, 128, 128, 1, 4.7, 2.51, 4.068},
+                                 {kPanel128Pairs, 128, 128, 2, 4.7, 8.98, 5.945}, {kPanel256, 256, 256, 1, 6.4, 9.10, 8.518}};
+constexpr Way kWaysOfAny[] = {{kStream16x16, 16, 16, 1, 2.8, 0.25, 0.706},
+                              {kStream64x16, 64, 16, 1, 3.8, 0.98, 1.650},
+                              {kStream64x32, 64, 32, 1, 4.4, 3.44, 2.090},
+                              {kStream64x64, 64, 64, 1, 6.1, 5.48, 2.843},
+                              {kTile128, 128, 128, 1, 7.1, 3.11, 6.853}};
 // Rows of whole words: the streams' as above, panels fitted to 75 products of 60 .. 8192 rows, where the way ahead is 1.0 % slower than the fastest in the
 // mean.  (300 x 4100 x 3004: 64 x 64 18.4 us, without panels 25.0; 4000 x 4000 x 4004: 256 x 256 69.5, 128 x 128 94.5, without panels 104; 1999 x 3001 x 2500:
 // 128 x 128 36.9, without panels 37.7.)
-constexpr Way kWaysOfWords[] = {{kStream16x16, 16, 16, 2.8, 0.25, 0.706}, {kStream64x16, 64, 16, 3.8, 0.98, 1.650}, {kStream64x32, 64, 32, 4.4, 3.44, 2.090},
-                                {kStream64x64, 64, 64, 6.1, 5.48, 2.843}, {kPanel64, 64, 64, 5.4, 0.80, 2.486},     {kPanel128, 128, 128, 6.8, 1.21, 5.749},
-                                {kPanel256, 256, 256, 9.8, 11.65, 12.12}};
+constexpr Way kWaysOfWords[] = {{kStream16x16, 16, 16, 1, 2.8, 0.25, 0.706}, {kStream64x16, 64, 16, 1, 3.8, 0.98, 1.650},
+                                {kStream64x32, 64, 32, 1, 4.4, 3.44, 2.090}, {kStream64x64, 64, 64, 1, 6.1, 5.48, 2.843},
+                                {kPanel64, 64, 64, 1, 5.4, 0.80, 2.486},     {kPanel128Pairs, 128, 128, 1, 6.8, 1.21, 5.749},
+                                {kPanel256, 256, 256, 1, 9.8, 11.65, 12.12}};
 template <int kCount>
 const Way &fastest(const Way (&ways)[kCount], int64_t M, int64_t N, int64_t K) {
     const Way *best = nullptr;
     double least = 0.0;
     for (const Way &w : ways) {
-        const double rounds = std::ceil((double)ceil_div(M, w.rows) * (double)ceil_div(N, w.columns) / compute_units());
+        const double rounds = std::ceil((double)ceil_div(M, w.rows) * (double)ceil_div(N, w.columns) / (compute_units() * w.side));
         const double us = w.start + w.more * (rounds - 1.0) + w.k * rounds * (double)K / 1024.0;
         if (!best || us < least) best = &w, least = us;
     }
@@ -255,13 +260,13 @@ int launch(const Args<T> &a, hipStream_t s) {
     const Tiles tiles = make_tiles(tm, tn);
     const dim3 grid((unsigned)(tm * tn));
     auto stream = [&](auto on_pieces, auto on_any) { return QNN_LAUNCH("int8_gemm", (pieces ? on_pieces : on_any), grid, dim3(512), 0, s, a, tiles); };
-    auto panels = [&](auto shape, auto shape_of_words) {
+    auto panels_of = [&](auto shape) {
         typedef decltype(shape) S;
         const int64_t most = (int64_t)compute_units() * S::kPerUnit;
-        auto kernel = words ? panel::gemm_panel_kernel<T, decltype(shape_of_words)> : panel::gemm_panel_kernel<T, S>;
-        return QNN_LAUNCH("int8_gemm", kernel, dim3((unsigned)(tm * tn < most ? tm * tn : most)), dim3(S::kThreads), 0, s, a, tiles,
+        return QNN_LAUNCH("int8_gemm", (panel::gemm_panel_kernel<T, S>), dim3((unsigned)(tm * tn < most ? tm * tn : most)), dim3(S::kThreads), 0, s, a, tiles,
                           (uint32_t)ceil_div(a.K, panel::kRow));
     };
+    auto panels = [&](auto shape, auto shape_of_words) { return words ? panels_of(shape_of_words) : panels_of(shape); };
     if (!pieces && !any) return QNN_LAUNCH("int8_gemm", (gemm_stream_kernel<T, 1, 1, 8, 1, kShortRows>), grid, dim3(512), 0, s, a, tiles);
     switch (w.id) {
     case kStream16x16: return stream(gemm_stream_kernel<T, 1, 1, 8, 2, kPieces>, gemm_stream_kernel<T, 1, 1, 8, 2, kAny>);
@@ -269,7 +274,8 @@ int launch(const Args<T> &a, hipStream_t s) {
     case kStream64x32: return stream(gemm_stream_kernel<T, 2, 4, 8, 1, kPieces>, gemm_stream_kernel<T, 2, 4, 8, 1, kAny>);
     case kStream64x64: return stream(gemm_stream_kernel<T, 4, 4, 8, 1, kPieces>, gemm_stream_kernel<T, 4, 4, 8, 1, kAny>);
     case kPanel64: return panels(panel::Tiny(), panel::TinyWords());
-    case kPanel128: return panels(panel::Small(), panel::SmallWords());
+    case kPanel128: return panels_of(panel::Eight());
+    case kPanel128Pairs: return panels(panel::Small(), panel::SmallWords());
     case kPanel256: return panels(panel::Large(), panel::LargeWords());
     case kTile128: return QNN_LAUNCH("int8_gemm", gemm_tile_kernel<T>, grid, dim3(256), 0, s, a, tiles);
     }

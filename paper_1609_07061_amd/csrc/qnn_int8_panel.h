@@ -27,8 +27,8 @@ namespace panel {
 
 constexpr int kRow = 128;  // codes of a row in a group
 
-// WM x WN waves, each with 32 BA rows of A and 32 BW rows of W; kRing groups in LDS; kPerUnit workgroups on a compute unit.  (Two such teams of waves on
-// alternate groups of k were no faster than one: 1024 x 4096 x 4096 on 128 x 128 24.0 us, one team with four groups in LDS 24.5.)
+// WM x WN waves, each with 32 BA rows of A and 32 BW rows of W; kRing groups in LDS; kPerUnit workgroups on a compute unit.  (1024 x 4096 x 4096 on 128 x 128:
+// four waves 28.6 us, two such teams on alternate groups of k or four groups in LDS 24.0 to 24.5, eight waves and four groups 23.7.)
 template <int WM_, int WN_, int BA_, int BW_, int kRing_, int kPerUnit_, bool kWords_ = false>
 struct Shape {
     static constexpr int WM = WM_, WN = WN_, BA = BA_, BW = BW_, kRing = kRing_, kPerUnit = kPerUnit_;
@@ -298,7 +298,8 @@ __global__ __launch_bounds__(S::kThreads, S::kThreads / 256 * S::kPerUnit) void 
 }
 
 typedef Shape<2, 4, 4, 2, 2, 1> Large;  // 256 x 256
-typedef Shape<2, 2, 2, 2, 2, 2> Small;  // 128 x 128
+typedef Shape<2, 2, 2, 2, 2, 2> Small;  // 128 x 128, two workgroups on a compute unit
+typedef Shape<2, 4, 2, 1, 4, 1> Eight;  // 128 x 128 on eight waves
 typedef Shape<2, 2, 1, 1, 4, 2> Tiny;   // 64 x 64
 // the same for words (a line of 256 bytes a load: slower by half, but 4000 x 4000 x 4004 104 us through registers, 69.5 like this)
 typedef Shape<2, 4, 4, 2, 2, 1, true> LargeWords;

@@ -25,7 +25,7 @@ def _kernel(call):
 # whole 16-byte pieces: streams (16 x 16, 64 x 16, 64 x 32, 64 x 64), panels (64, 128, 256)
 PIECES = [("stream", 3, 40, 16), ("stream", 16, 4096, 1040), ("stream", 60, 4000, 4096), ("stream", 120, 4096, 4112), ("stream", 256, 4090, 4096), ("stream", 700, 1000, 4096),
           ("panel", 700, 1000, 272), ("panel", 1200, 1024, 1040), ("panel", 5000, 130, 528), ("panel", 300, 4100, 144), ("panel", 1190, 4000, 1008), ("panel", 5000, 1000, 400),
-          ("panel", 130, 20000, 656), ("panel", 5000, 4099, 16), ("panel", 9000, 9001, 256), ("panel", 5003, 4097, 1168), ("panel", 7000, 8000, 128), ("panel", 2560, 16384, 384)]
+          ("panel", 130, 20000, 656), ("panel", 5000, 4099, 16), ("panel", 9000, 9001, 256), ("panel", 5003, 4097, 1168), ("panel", 1023, 4090, 2064), ("panel", 4000, 1025, 592), ("panel", 7000, 8000, 128), ("panel", 2560, 16384, 384)]
 # any rows: streams, the tiled kernel; fewer codes than a piece
 ANY = [("stream", 2, 40, 17), ("stream", 16, 4095, 1001), ("stream", 60, 4000, 4093), ("stream", 120, 4096, 1023), ("stream", 256, 4090, 2047), ("tile", 1999, 1001, 2501), ("tile", 1000, 4001, 17),
        ("tile", 3000, 3000, 127), ("tile", 2500, 2049, 129), ("tile", 4000, 2500, 385), ("tile", 1500, 3000, 250), ("stream", 100, 900, 15), ("stream", 1, 5000, 1), ("stream", 3000, 70, 8)]
