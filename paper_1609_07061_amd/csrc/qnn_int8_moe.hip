@@ -1,11 +1,13 @@
-// Mixture-of-experts layer on int8 codes for a few tokens, in two kernels or three.  What bounds it is reading the chosen experts' weights once.
+// Mixture-of-experts layer on int8 codes for a few tokens, in two to four kernels.  What bounds it is reading the chosen experts' weights once.
+//   moe_route_kernel, for many logits or experts: the choices.
 //   moe_gate_up_kernel: a workgroup has 16 columns of one expert's inner width, that is 32 rows of W1, and all the tokens that chose the expert; which
-//     tokens these are it finds itself from the logits.  The activation goes to the workspace in fp32, beside the largest magnitude of each token's 16
+//     tokens these are it otherwise finds itself from the logits.  The activation goes to the workspace in fp32, beside the largest magnitude of each token's 16
 //     values; the expert's first workgroup also writes the tokens' weights.
 //   quant_rows_kernel (qnn_rows.h), for more than a few choices: the activations to codes.
 //   moe_down_kernel: a workgroup has 16 columns of the output, that is 16 rows of every expert's W2.  For a few choices it quantizes the activations itself
 //     (a row's scale is known once the first kernel has ended).  It multiplies expert by expert and adds the weighted results in the order of the choices.
 // Both products give 16 x 16 blocks of sums to the matrix cores, with the weights on the row side, and split k over their waves.
+// One token, two of 8 experts of 4096 x 2048 (50 MB): 9.0 + 7.0 us, of which 2 and 3.5 pass before the weights flow; 20 tokens (201 MB): 29.6 + 4.2 + 16.6.
 #include "qnn_int8.h"
 
 namespace qnn {
@@ -312,8 +314,8 @@ __device__ __forceinline__ int in_order(const MoeArgs &a, Route *route, int slot
 // (mostly everything at once); then every wave goes through its steps of k of one expert after the other without a break in its loads, and adds what it has
 // of an expert to the results in LDS (whole numbers: in any order).
 // kQuantize: the codes are made here, from the first kernel's activations and maxima, all at once; else they and their scales are in memory.  The first
-// saves a launch, but every workgroup reads four times as much and makes all the codes (7 tokens, three of 5 experts of 1000 x 700: 10.8 us, in two kernels
-// 4.2 + 9.8; 20 tokens, two of 8 experts of 4096 x 2048: 24.6 us, in two kernels 4.3 + 18.6).
+// saves a launch, but every workgroup reads four times as much and makes all the codes (7 tokens, three of 5 experts of 1000 x 700: 10.8 us where two
+// kernels took 4.2 + 9.8; 20 tokens, two of 8 experts of 4096 x 2048: 24.6 where two took 4.3 + 18.6).
 template <typename T, int kSlots, int kCodes, int kStages, Layout kLayout, bool kQuantize>
 __global__ __launch_bounds__(512) void moe_down_kernel(const MoeArgs a, T *out, int chunk) {
     constexpr int kWaves = 8;

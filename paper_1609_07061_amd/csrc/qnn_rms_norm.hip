@@ -4,7 +4,8 @@
 // Forward: h = x + residual, r = 1 / sqrt(mean h^2 + eps), y = h r gamma, codes and scale of y (qnn_rows.h).  r is one positive number a row, so
 // max |y| = r max |h gamma|: the sum and the maximum come from ONE pass over the row, which stays in registers, and the codes need no r at all.
 // The norm and the codes take h in fp32; the sum that is written is rounded once.
-// Bound by memory: 2 reads and a write of a 16-bit float and a write of a byte for each value.
+// Bound by memory: 2 reads and a write of a 16-bit float and a write of a byte for each value (10000 x 4096 bf16 with a residual, 287 MB: 48.8 us, 5.9 TB/s;
+// one row: 4.2 us, a launch).
 #include <type_traits>
 
 #include "qnn_rows.h"
@@ -57,7 +58,8 @@ struct NormSource {
 //   gh = r (gamma g - h r^2 mean(gamma g h)) + z,   ggamma = sum over the rows of g h r.
 // A workgroup takes kGroups rows at a time, every gridDim-th such group, keeps its lanes' part of ggamma in registers over all of them and writes it once;
 // the second kernel adds these partial sums in a fixed order.  Up to kParts of them, so that they are a small part of what is moved.  (10000 x 4096 bf16
-// with a residual's gradient, 328 MB: two rows at a time 61.0 us, one 70.9; with the next row's loads sent ahead 71.5 and 68.3: more registers, fewer waves.)
+// with a residual's gradient, 328 MB: 58.6 us, 5.6 TB/s, and 4.1 for the parts; one row at a time took 70.9 where two took 61.0, and with the next row's loads
+// sent ahead 68.3 and 71.5: more registers, fewer waves.)
 constexpr int kParts = 512;
 
 template <typename T>
