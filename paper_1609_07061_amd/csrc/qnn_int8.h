@@ -19,13 +19,17 @@ __device__ __forceinline__ v4i load_window(const int8_t *row, int64_t k, int64_t
     return v;
 }
 __device__ __forceinline__ v4i in_place(const v4i &v, int64_t k, int64_t K) {
-    const int64_t over = k + 16 - K;  // codes to leave out
-    if (over <= 0) return v;
-    const uint64_t lo = (uint32_t)v[0] | (uint64_t)(uint32_t)v[1] << 32, hi = (uint32_t)v[2] | (uint64_t)(uint32_t)v[3] << 32;
-    const int bits = 8 * (int)(over < 16 ? over : 0);  // 0: all of them
-    const uint64_t a = over >= 16 ? 0u : (bits < 64 ? (lo >> bits) | (hi << (64 - bits)) : hi >> (bits - 64));
-    const uint64_t b = over >= 16 || bits >= 64 ? 0u : hi >> bits;
-    return v4i{(int)a, (int)(a >> 32), (int)b, (int)(b >> 32)};
+    // codes to leave out: a shift by as many bytes, words first, without a branch (1356 x 384 x 767: 8.7 us with branches, 7.7 so)
+    const int64_t over = k + 16 - K;
+    const uint32_t bytes = (uint32_t)(over < 0 ? 0 : (over > 16 ? 16 : over));
+    uint32_t x[5] = {(uint32_t)v[0], (uint32_t)v[1], (uint32_t)v[2], (uint32_t)v[3], 0u};
+    const bool four = (bytes & 16u) != 0u, two = (bytes & 8u) != 0u, one = (bytes & 4u) != 0u;
+    x[0] = two ? x[2] : x[0], x[1] = two ? x[3] : x[1], x[2] = two ? 0u : x[2], x[3] = two ? 0u : x[3];
+    x[0] = one ? x[1] : x[0], x[1] = one ? x[2] : x[1], x[2] = one ? x[3] : x[2], x[3] = one ? 0u : x[3];
+    v4i out;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) out[i] = four ? 0 : (int)__builtin_amdgcn_alignbyte(x[i + 1], x[i], bytes);
+    return out;
 }
 // The same for a row of fewer than 16 codes
 __device__ __forceinline__ v4i load_short(const int8_t *row, int64_t k, int64_t K) {

@@ -141,17 +141,27 @@ __global__ __launch_bounds__(256, 2) void gemm_tile_kernel(const Args<T> a, cons
     fetch(0, even);
     fetch(kGroup, odd);
     put(0, even, 0);
-    // at the top of a turn: group k in buffer 0, the loads of the next in `odd` under way
-    for (int64_t k = 0; k < a.K; k += 2 * kGroup) {
-        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // (written and, the other buffer, read; loads stay under way)
+    auto turn = []() __attribute__((always_inline)) {  // (written and, the other buffer, read; loads stay under way)
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    };
+    // at the top: group k in buffer 0, the loads of the next in `odd` under way
+    int64_t k = 0;
+    for (; k + 2 * kGroup < a.K; k += 2 * kGroup) {
+        turn();
         fetch(k + 2 * kGroup, even);
         multiply(0);
-        if (k + kGroup >= a.K) break;
         put(1, odd, k + kGroup);
-        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        turn();
         fetch(k + 3 * kGroup, odd);
         multiply(1);
-        if (k + 2 * kGroup < a.K) put(0, even, k + 2 * kGroup);
+        put(0, even, k + 2 * kGroup);
+    }
+    turn();
+    multiply(0);
+    if (k + kGroup < a.K) {
+        put(1, odd, k + kGroup);
+        turn();
+        multiply(1);
     }
     __syncthreads();
     // A wave's sums of 32 rows pass through its part of LDS and leave as rows of 64 columns, 8 columns a lane
