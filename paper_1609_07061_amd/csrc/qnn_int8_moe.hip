@@ -334,24 +334,21 @@ __global__ __launch_bounds__(512) void moe_down_kernel(const MoeArgs a, T *out, 
     const int pitch = chunk + 16, most = kCodes / pitch;
     // everything at once: rows of codes are in the order of the choices, else in that of the experts
     const bool at_once = kQuantize || (slots <= most && F <= (uint32_t)chunk);
-    // kQuantize: 1024 activations of a row by a wave, four loads of whole lines; the first kItems of a wave's are on their way from here on
-    constexpr int kItems = 2;
-    float v[kItems][4][4];
-    const uint32_t parts = ((uint32_t)chunk + 1023u) / 1024u, items = (uint32_t)slots * parts;
-    auto fetch = [&](float (&to)[4][4], uint32_t item) __attribute__((always_inline)) {
-        const float *const p = a.act + (int64_t)(item / parts) * a.F;
+    // kQuantize: 256 activations of a row by a wave, a load of whole lines; the first kItems of a wave's are on their way from here on
+    constexpr int kItems = 4;
+    float v[kItems][4];
+    const uint32_t parts = ((uint32_t)chunk + 255u) / 256u, items = (uint32_t)slots * parts;
+    const uint32_t inverse = (65535u + parts) / parts;  // item / parts = item * inverse / 65536: up to 32 rows in 20 KB are less than 128 items
+    auto row_of = [&](uint32_t item) __attribute__((always_inline)) { return (item * inverse) >> 16; };
+    auto fetch = [&](float (&to)[4], uint32_t item) __attribute__((always_inline)) {  // (the rows are followed by more than they lack to a group of four)
+        const uint32_t m = row_of(item), f = (item - m * parts) * 256u + 4u * lane;
+        __builtin_memcpy(to, a.act + (int64_t)m * a.F + min(f, F - 1u), 16);
 #pragma unroll
-        for (uint32_t u = 0; u < 4u; ++u) {
-            const uint32_t f = item % parts * 1024u + 4u * lane + 256u * u;  // (the rows are followed by more than they lack to a group of four)
-            __builtin_memcpy(to[u], p + min(f, F - 1u), 16);
-#pragma unroll
-            for (uint32_t j = 0; j < 4u; ++j) to[u][j] = f + j < F ? to[u][j] : 0.0f;
-        }
+        for (uint32_t j = 0; j < 4u; ++j) to[j] = f + j < F ? to[j] : 0.0f;
     };
     if constexpr (kQuantize) {
 #pragma unroll
-        for (int j = 0; j < kItems; ++j)
-            if ((uint32_t)(wave + kWaves * j) < items) fetch(v[j], (uint32_t)(wave + kWaves * j));
+        for (int j = 0; j < kItems; ++j) fetch(v[j], min((uint32_t)(wave + kWaves * j), items - 1u));
     }
     // One wave finds the order of the choices; the others how each activation is quantized (for a choice that takes no part: nothing that is used).
     if (wave == 0) {
@@ -426,21 +423,18 @@ __global__ __launch_bounds__(512) void moe_down_kernel(const MoeArgs a, T *out, 
             s.start(steps, base, at);
             if constexpr (kQuantize) {  // zeros from an activation's end to a whole step
                 for (uint32_t i0 = wave; i0 < items; i0 += kWaves * kItems) {
+                    if (i0 != (uint32_t)wave) {
 #pragma unroll
-                    for (uint32_t j = 0; j < kItems; ++j)
-                        if (i0 != (uint32_t)wave && i0 + kWaves * j < items) fetch(v[j], i0 + kWaves * j);
+                        for (uint32_t j = 0; j < kItems; ++j) fetch(v[j], min(i0 + kWaves * j, items - 1u));
+                    }
 #pragma unroll
                     for (uint32_t j = 0; j < kItems; ++j) {
                         const uint32_t i = i0 + kWaves * j;
                         if (i >= items) break;
-                        const int m = (int)(i / parts);
+                        const uint32_t m = row_of(i), f = (i - m * parts) * 256u + 4u * lane;
                         Quantizer q(0u, 1.0f);
                         q.mul = mul[m], q.pre = pre[m], q.zero = pre[m] == 0.0f;
-#pragma unroll
-                        for (uint32_t u = 0; u < 4u; ++u) {
-                            const uint32_t f = i % parts * 1024u + 4u * lane + 256u * u;
-                            if (f < (uint32_t)chunk) *reinterpret_cast<uint32_t *>(&codes[m * pitch + (int)f]) = q.four(v[j][u][0], v[j][u][1], v[j][u][2], v[j][u][3]);
-                        }
+                        if (f < (uint32_t)chunk) *reinterpret_cast<uint32_t *>(&codes[m * pitch + f]) = q.four(v[j][0], v[j][1], v[j][2], v[j][3]);
                     }
                 }
             } else {  // 16 codes a lane, whole rows of the part (what lies beyond the inner width meets zeros), eight loads under way
