@@ -460,19 +460,20 @@ __global__ __launch_bounds__(512) void moe_down_kernel(const MoeArgs a, T *out, 
             asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // (weights may still be on their way)
             constexpr int kBlocks = kSlots < 64 ? kSlots / 16 : 4;  // of 16 tokens of an expert
             v4i acc[kBlocks];
-            int row[kBlocks], first = 0, count = 0;
-            bool other = true;
-            s.run(steps, base, at, [&](int, const typename S::Operands &o) __attribute__((always_inline)) {
-                if (other) {
-                    first = __builtin_amdgcn_readfirstlane(start[x]), count = __builtin_amdgcn_readfirstlane(start[x + 1]) - first;
+            int row[kBlocks], choice[kBlocks], count = 0;
+            auto enter = [&]() __attribute__((always_inline)) {  // expert x: asked for at the end of the step before, so that LDS answers while its weights come in
+                const int first = __builtin_amdgcn_readfirstlane(start[x]);
+                count = __builtin_amdgcn_readfirstlane(start[x + 1]) - first;
 #pragma unroll
-                    for (int j = 0; j < kBlocks; ++j) {
-                        const int pos = first + min(16 * j + r, count - 1);
-                        row[j] = (at_once ? order[pos] : pos - first_row) * pitch, acc[j] = v4i{0, 0, 0, 0};
-                    }
+                for (int j = 0; j < kBlocks; ++j) {
+                    const int pos = first + min(16 * j + r, count - 1);
+                    choice[j] = order[pos], row[j] = (at_once ? choice[j] : pos - first_row) * pitch, acc[j] = v4i{0, 0, 0, 0};
                 }
+            };
+            if (steps > 0) enter();
+            s.run(steps, base, at, [&](int i, const typename S::Operands &o) __attribute__((always_inline)) {
                 const int k = 128 * block + 16 * g;
-                other = next(x, block);
+                const bool other = next(x, block);
 #pragma unroll
                 for (int j = 0; j < kBlocks; ++j)
                     if (16 * j < count) {
@@ -480,11 +481,11 @@ __global__ __launch_bounds__(512) void moe_down_kernel(const MoeArgs a, T *out, 
                         for (int h = 0; h < 2; ++h)
                             acc[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(o.w[h][0], *reinterpret_cast<const v4i *>(&codes[row[j] + k + 64 * h]), acc[j], 0, 0, 0);
                         if (other && 16 * j + r < count) {
-                            const int m = order[first + 16 * j + r];
 #pragma unroll
-                            for (int w = 0; w < 4; ++w) atomicAdd(&result[m][4 * g + w], acc[j][w]);
+                            for (int w = 0; w < 4; ++w) atomicAdd(&result[choice[j]][4 * g + w], acc[j][w]);
                         }
                     }
+                if (other && i + 1 < steps) enter();
             });
             asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         }
