@@ -102,3 +102,18 @@ def test_gate_backward_far_out(gate, value):
     x, one = torch.full((3, 40), gate, device="cuda"), torch.ones(3, 40, device="cuda")
     a, b = q.qnn_silu_gate_backward(one, x, one)
     assert (a == value).all() and (b == value * gate).all()
+
+
+def test_offsets_beyond_32_bits(seed):
+    """Rows that lie more than 4 GiB apart."""
+    import paper_1609_07061_amd as q
+
+    F, pitch = 333, (1 << 31) + 72
+    u, grad = _inputs(seed, 3, F, torch.bfloat16)
+    want, want_grad = q.qnn_silu_gate_quant(u[:, :F], u[:, F:]), q.qnn_silu_gate_backward(grad, u[:, :F], u[:, F:])
+    far = torch.empty(2 * pitch + 2 * F, dtype=torch.bfloat16, device="cuda").as_strided((3, 2 * F), (pitch, 1))
+    far.copy_(u)
+    got = q.qnn_silu_gate_quant(far[:, :F], far[:, F:])
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    got = q.qnn_silu_gate_backward(grad, far[:, :F], far[:, F:], far[:, :F], far[:, F:])
+    assert torch.equal(got[0], want_grad[0]) and torch.equal(got[1], want_grad[1])

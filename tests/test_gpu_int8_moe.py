@@ -125,6 +125,23 @@ def test_strides(seed, T, pad, offset):
     assert untouched(whole, out, 7.0) and (workspace[-4096:] == 0xFF).all()
 
 
+@pytest.mark.parametrize("T,log_pitch", [(3, 26), (3, 27), (40, 26)])
+def test_offsets_beyond_32_bits(seed, T, log_pitch):
+    """Experts that lie 4 GiB apart, rows of one that do."""
+    import paper_1609_07061_amd as q
+
+    E, H, F, pitch = 3, 48, 16, 1 << log_pitch
+    layer = _layer(seed, T, E, H, F)
+    want = _call(q, layer, 2, dtype=torch.float32)
+    far = list(layer)
+    for i in (3, 5):
+        w = layer[i]
+        far[i] = torch.empty((E * w.shape[1] - 1) * pitch + w.shape[2], dtype=torch.int8, device="cuda").as_strided(w.shape, (w.shape[1] * pitch, pitch, 1))
+        far[i].copy_(w)
+    assert torch.equal(_call(q, far, 2, dtype=torch.float32), want)
+    _check(want, layer, 2)
+
+
 def test_graph(seed):
     import paper_1609_07061_amd as q
 

@@ -162,3 +162,29 @@ def test_backward_against_differences(seed, K):
     size = _backward(grad.double(), h.double(), gamma.double(), None)
     bound = (2 * sum_error(K) + 10) * U * ((size[2] * dh.double().abs()).sum() + (size[3] * dg.double().abs()).sum())
     assert (got - slope).abs() <= bound + 1e-6 * (1 + slope.abs()) + 1e-8 * rows * K
+
+
+def _far_apart(t, pitch):
+    """The rows of t, `pitch` elements apart."""
+    whole = torch.empty((t.shape[0] - 1) * pitch + t.shape[1], dtype=t.dtype, device="cuda")
+    view = whole.as_strided(t.shape, (pitch, 1))
+    view.copy_(t)
+    return view
+
+
+@pytest.mark.parametrize("K", [256, 333])
+def test_offsets_beyond_32_bits(seed, K):
+    """Rows that lie more than 4 GiB apart."""
+    import paper_1609_07061_amd as q
+
+    g, pitch = generator(seed, K, 9), (1 << 31) + 72
+    x, res, grad, gamma = normal(g, 3, K).bfloat16(), normal(g, 3, K).bfloat16(), normal(g, 3, K).bfloat16(), (1 + normal(g, K) / 4).bfloat16()
+    want, want_grad = q.qnn_rms_norm_quant(x, gamma, EPS, res), q.qnn_rms_norm_backward(grad, x, gamma, EPS, res)
+    far = _far_apart(x, pitch)
+    got = q.qnn_rms_norm_backward(grad, far, gamma, EPS, res)
+    assert torch.equal(got[0], want_grad[0]) and torch.equal(got[1], want_grad[1])
+    codes = _far_apart(torch.zeros(3, K, dtype=torch.int8, device="cuda"), pitch)
+    got = q.qnn_rms_norm_quant(far, gamma, EPS, res, codes, None, far)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and torch.equal(got[2], want[2])
+    got = q.qnn_rms_norm_backward(grad, x, gamma, EPS, res, far)
+    assert torch.equal(got[0], want_grad[0])
