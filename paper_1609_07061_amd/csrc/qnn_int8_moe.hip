@@ -7,7 +7,7 @@
 //   moe_down_kernel: a workgroup has 16 columns of the output, that is 16 rows of every expert's W2.  For a few choices it quantizes the activations itself
 //     (a row's scale is known once the first kernel has ended).  It multiplies expert by expert and adds the weighted results in the order of the choices.
 // Both products give 16 x 16 blocks of sums to the matrix cores, with the weights on the row side, and split k over their waves.
-// One token, two of 8 experts of 4096 x 2048 (50 MB): 9.0 + 7.0 us, of which 2 and 3.5 pass before the weights flow; 20 tokens (201 MB): 29.6 + 4.2 + 16.6.
+// One token, two of 8 experts of 4096 x 2048 (50 MB): 8.9 + 6.9 us, of which 2 and 3 pass before the weights flow; 20 tokens (201 MB): 29.5 + 4.2 + 16.6.
 #include "qnn_int8.h"
 
 namespace qnn {
@@ -547,7 +547,7 @@ int launch_moe(const MoeArgs &a, void *out, int type, hipStream_t s) {
             return QNN_LAUNCH("int8_moe", (pieces2 ? (once ? pieces_once : pieces) : (a.F >= 16 ? any : short_rows)), columns, threads, 0, s, a, o, chunk);
         };
         // (Few steps under way where there is little to do: each one more is code to fetch, which a short kernel waits for.  One token, two of 8 experts of
-        // 4096 x 2048: 7.07 us, with a third 7.45; rows of any length: with four 9.9 us where one takes 9.3.)
+        // 4096 x 2048: 6.8 us, with a third 7.15, with four 7.45; rows of any length, 7 tokens, three of 5 experts of 1000 x 700: four 9.9 where one took 9.3.)
         if (few)
             return launch(moe_down_kernel<T, 32, kFew, 2, kPieces, true>, moe_down_kernel<T, 32, kFew, 2, kPiecesOnce, true>,
                           moe_down_kernel<T, 32, kFew, 1, kAny, true>, moe_down_kernel<T, 32, kFew, 1, kShortRows, true>, (int)whole);
