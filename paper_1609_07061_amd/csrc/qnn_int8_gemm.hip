@@ -231,16 +231,17 @@ struct Way {
 constexpr Way kWaysOfPieces[] = {{kStream16x16, 16, 16, 1, 2.7, 0.56, 0.276},     {kStream64x16, 64, 16, 1, 3.1, 1.95, 0.743}, {kStream64x32, 64, 32, 1, 3.3, 2.37, 0.924},
                                  {kStream64x64, 64, 64, 1, 4.3, 3.93, 1.306},     {kPanel64, 64, 64, 1, 3.6, 0.03, 1.838},     {kPanel128, 128, 128, 1, 4.7, 2.51, 4.068},
                                  {kPanel128Pairs, 128, 128, 2, 4.7, 8.98, 5.945}, {kPanel256, 256, 256, 1, 6.4, 9.10, 8.518}};
-constexpr Way kWaysOfAny[] = {{kStream16x16, 16, 16, 1, 2.8, 0.25, 0.706},
-                              {kStream64x16, 64, 16, 1, 3.8, 0.98, 1.650},
-                              {kStream64x32, 64, 32, 1, 4.4, 3.44, 2.090},
-                              {kStream64x64, 64, 64, 1, 6.1, 5.48, 2.843},
-                              {kTile128, 128, 128, 1, 7.1, 3.11, 6.853}};
+// Rows at any address: fitted to 78 products of 5 .. 4000 rows, of each of which the fastest way comes out ahead.
+constexpr Way kWaysOfAny[] = {{kStream16x16, 16, 16, 1, 2.8, 0.33, 0.671},
+                              {kStream64x16, 64, 16, 1, 3.4, 1.04, 1.610},
+                              {kStream64x32, 64, 32, 1, 3.9, 3.11, 2.022},
+                              {kStream64x64, 64, 64, 1, 5.2, 4.72, 2.982},
+                              {kTile128, 128, 128, 1, 6.2, 4.49, 7.015}};
 // Rows of whole words: the streams' as above, panels fitted to 75 products of 60 .. 8192 rows, where the way ahead is 1.0 % slower than the fastest in the
 // mean.  (300 x 4100 x 3004: 64 x 64 18.4 us, without panels 25.0; 4000 x 4000 x 4004: 256 x 256 69.5, 128 x 128 94.5, without panels 104; 1999 x 3001 x 2500:
 // 128 x 128 36.9, without panels 37.7.)
-constexpr Way kWaysOfWords[] = {{kStream16x16, 16, 16, 1, 2.8, 0.25, 0.706}, {kStream64x16, 64, 16, 1, 3.8, 0.98, 1.650},
-                                {kStream64x32, 64, 32, 1, 4.4, 3.44, 2.090}, {kStream64x64, 64, 64, 1, 6.1, 5.48, 2.843},
+constexpr Way kWaysOfWords[] = {{kStream16x16, 16, 16, 1, 2.8, 0.33, 0.671}, {kStream64x16, 64, 16, 1, 3.4, 1.04, 1.610},
+                                {kStream64x32, 64, 32, 1, 3.9, 3.11, 2.022}, {kStream64x64, 64, 64, 1, 5.2, 4.72, 2.982},
                                 {kPanel64, 64, 64, 1, 5.4, 0.80, 2.486},     {kPanel128Pairs, 128, 128, 1, 6.8, 1.21, 5.749},
                                 {kPanel256, 256, 256, 1, 9.8, 11.65, 12.12}};
 template <int kCount>
