@@ -326,6 +326,7 @@ int qnn_rms_norm_quant(const void *x, int64_t ldx, const void *residual, int64_t
 /* Its gradient, the quantizer taken as the identity (straight through, as Sec. 2.3 takes the sign): with g = grad the gradient at y, r = 1 /
  * sqrt(mean(h^2) + eps) and grad_sum (NULL: none) a gradient that reaches h along the residual path,
  *   grad_h = r (gamma g - h r^2 mean(gamma g h)) + grad_sum,   grad_gamma = sum over the rows of g h r   (DEVICE float32 [K]).
+ * A row that the forward call counts as not finite has NaN for its grad_h, and with it grad_gamma is NaN.
  * h: what the forward call wrote to `sum` (x, without a residual).  grad_h may be grad_sum itself.  rows >= 1; K <= 16384.  workspace: DEVICE,
  * 256-byte aligned, qnn_rms_norm_backward_workspace_bytes(rows, K) bytes.  Sums are formed in a fixed order. */
 int qnn_rms_norm_backward(const void *grad, int64_t ld_grad, const void *h, int64_t ld_h, const void *grad_sum, int64_t ld_grad_sum, int type,

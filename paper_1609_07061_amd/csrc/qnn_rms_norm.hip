@@ -15,6 +15,13 @@ namespace {
 
 using namespace rows;
 
+// r of a row of K whose squares add up to `total`.  NaN for a row whose mean square is beyond fp32 (1 / sqrt would be 0: a row of zeros, and a gradient
+// of zeros) or that has a value that is not finite.
+__device__ __forceinline__ float norm_factor(float total, int64_t K, float eps) {
+    const float mean = total / (float)K;
+    return magnitude(mean) < 0x7F800000u ? 1.0f / sqrtf(mean + eps) : __uint_as_float(0x7FC00000u);
+}
+
 template <typename T, bool kOnce>
 struct NormSource {
     struct Kept {
@@ -43,11 +50,7 @@ struct NormSource {
         for (int i = 0; i < kVec; ++i) v[i] = kept.h[i] * g[i];
     }
     __device__ __forceinline__ float add(const Kept &kept, int i, float sum) const { return __fmaf_rn(kept.h[i], kept.h[i], sum); }
-    __device__ __forceinline__ float factor(float total, int64_t K) const {
-        const float mean = total / (float)K;
-        // (a mean beyond fp32 would give the factor 0 and a row of zeros)
-        return magnitude(mean) < 0x7F800000u ? 1.0f / sqrtf(mean + eps) : __uint_as_float(0x7FC00000u);
-    }
+    __device__ __forceinline__ float factor(float total, int64_t K) const { return norm_factor(total, K, eps); }
     template <bool kShort>
     __device__ __forceinline__ void keep(int64_t row, const Window &w, int64_t K, const Kept &kept) const {
         if (sum) store_values<kOnce, kShort>(sum + row * lds, w, K, kept.h);
@@ -122,7 +125,7 @@ __global__ __launch_bounds__(kThreads *groups_of(kThreads)) void rms_norm_backwa
         s = across<kThreads>(s, TwoSums::join, shared[group], turn);
         turn ^= 1;
         if (row >= a.n_rows) return;
-        const float r = 1.0f / sqrtf(s.a / (float)a.K + a.eps), c = r * r * (s.b / (float)a.K);
+        const float r = norm_factor(s.a, a.K, a.eps), c = r * r * (s.b / (float)a.K);
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             const int64_t k = (int64_t)(i * kThreads + lane) * kVec;
