@@ -319,14 +319,15 @@ size_t qnn_conv2d_dedup_workspace_bytes(int64_t B, int64_t H, int64_t Wd, int64_
 /* Root-mean-square norm with the residual's addition, to codes: h = x + residual, y = h / sqrt(mean(h^2) + eps) * gamma, codes and scale of y.
  * x, residual (NULL: none), sum (NULL: not written; receives h, rounded once; it may be x or residual itself): DEVICE [rows][ld] of `type`.
  * gamma: DEVICE [K] of float32 or `type` (gamma_type).  codes: DEVICE int8 [rows][ld_codes]; scale: DEVICE float32 [rows].  eps >= 0, finite.
- * The norm is formed from h before it is rounded.  A row whose mean square is beyond float32 counts as not finite. */
+ * The norm is formed from h before it is rounded.  A row whose sum of squares (or mean square and eps together) is beyond float32 counts as not finite, and so
+ * does a row other than zeros whose mean square and eps together are below its normal numbers (2^-126: without eps, values of about 1e-19 and less). */
 int qnn_rms_norm_quant(const void *x, int64_t ldx, const void *residual, int64_t ld_residual, int type, const void *gamma, int gamma_type, float eps,
                        int64_t rows, int64_t K, void *sum, int64_t ld_sum, int8_t *codes, int64_t ld_codes, float *scale, void *stream);
 
 /* Its gradient, the quantizer taken as the identity (straight through, as Sec. 2.3 takes the sign): with g = grad the gradient at y, r = 1 /
  * sqrt(mean(h^2) + eps) and grad_sum (NULL: none) a gradient that reaches h along the residual path,
  *   grad_h = r (gamma g - h r^2 mean(gamma g h)) + grad_sum,   grad_gamma = sum over the rows of g h r   (DEVICE float32 [K]).
- * A row that the forward call counts as not finite has NaN for its grad_h, and with it grad_gamma is NaN.
+ * A row that the forward call counts as not finite, or one of zeros without eps, has no finite gradient: its grad_h and all of grad_gamma are NaN or infinite.
  * h: what the forward call wrote to `sum` (x, without a residual).  grad_h may be grad_sum itself.  rows >= 1; K <= 16384.  workspace: DEVICE,
  * 256-byte aligned, qnn_rms_norm_backward_workspace_bytes(rows, K) bytes.  Sums are formed in a fixed order. */
 int qnn_rms_norm_backward(const void *grad, int64_t ld_grad, const void *h, int64_t ld_h, const void *grad_sum, int64_t ld_grad_sum, int type,

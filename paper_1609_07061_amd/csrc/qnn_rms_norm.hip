@@ -15,11 +15,13 @@ namespace {
 
 using namespace rows;
 
-// r of a row of K whose squares add up to `total`.  NaN for a row whose mean square is beyond fp32 (1 / sqrt would be 0: a row of zeros, and a gradient
-// of zeros) or that has a value that is not finite.
+// r of a row of K whose squares add up to `total`.  NaN for a row whose sum is beyond fp32 (1 / sqrt would be 0: a row of zeros, and a gradient of zeros) or that
+// has a value that is not finite.  Infinite where mean and eps together are below the normal numbers, whose squares have lost their digits: such a row counts as
+// not finite too, unless it holds nothing but zeros.  (Sums in units of a power of two would hold both; in the gradient they take a fourth of the waves.)
 __device__ __forceinline__ float norm_factor(float total, int64_t K, float eps) {
-    const float mean = total / (float)K;
-    return magnitude(mean) < 0x7F800000u ? 1.0f / sqrtf(mean + eps) : __uint_as_float(0x7FC00000u);
+    const float mean = total / (float)K + eps;
+    if (mean < 0x1p-126f) return __uint_as_float(0x7F800000u);
+    return magnitude(mean) < 0x7F800000u ? 1.0f / sqrtf(mean) : __uint_as_float(0x7FC00000u);
 }
 
 template <typename T, bool kOnce>

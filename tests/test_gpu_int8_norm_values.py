@@ -4,7 +4,7 @@ import math
 import pytest
 import torch
 
-from int8_testlib import U, assert_near, generator, normal, sum_error
+from int8_testlib import U, assert_near, assert_quantized, generator, normal, sum_error
 
 pytestmark = pytest.mark.gpu
 EPS = 1e-5
@@ -71,3 +71,44 @@ def test_gradient_that_is_not_finite(seed, K):
         rows, columns = [0, 1, 3], [k for k in range(K) if k != K - 2]
         assert torch.equal(gh[rows], want[0][rows]) and torch.equal(gw[columns], want[1][columns])
         assert not torch.isfinite(gh[2]).any() and not torch.isfinite(gw[K - 2])
+
+
+@pytest.mark.parametrize("K", [10, 700, 3000, 33000])
+def test_squares_out_of_range(seed, K):
+    """Rows whose squares fp32 does not hold: exact or marked, never an approximation."""
+    import paper_1609_07061_amd as q
+
+    x, gamma = normal(generator(seed, K, 6), 10, K), torch.ones(K, device="cuda")
+    sizes = [1e-18, 1e-21, 1e-23, 1e-25, 1e-30, 1e-40, 0.0, 1e17, 3e19, 1.0]
+    x *= torch.tensor(sizes, device="cuda")[:, None]
+    x[9] = 0
+    x[9, K // 2] = 1e-22  # one value only
+    codes, scale, _ = q.qnn_rms_norm_quant(x, gamma, 0.0)
+    marked = [1, 2, 3, 4, 5, 8, 9]
+    assert torch.isnan(scale[marked]).all() and (codes[marked] == 0).all()
+    assert scale[6] == 0 and (codes[6] == 0).all()
+    y = x.double() / torch.sqrt(x.double().square().mean(dim=1, keepdim=True))
+    assert_quantized(codes[[0, 7]], scale[[0, 7]], y[[0, 7]], (sum_error(K) / 2 + 9) * U)  # (a square's rounding is up to 2 U at 2^-126)
+    # nothing left of any of them, whatever the sum is
+    codes, scale, _ = q.qnn_rms_norm_quant(x[[1, 4, 5, 6]], 0 * gamma, 0.0)
+    assert (scale == 0).all() and (codes == 0).all()
+    # a mean square and an eps that fp32 holds one by one
+    big = torch.zeros(1, K, device="cuda")
+    big[0, 0] = 1.8e19
+    assert torch.isfinite(q.qnn_rms_norm_quant(big, gamma, 1e-5)[1]).all()
+    assert torch.isnan(q.qnn_rms_norm_quant(big[:, :1], gamma[:1], 3e38)[1]).all()
+
+
+@pytest.mark.parametrize("K", BACKWARD_WIDTHS)
+def test_gradient_of_squares_out_of_range(seed, K):
+    import paper_1609_07061_amd as q
+
+    g = generator(seed, K, 7)
+    h, grad, gamma = normal(g, 7, K), normal(g, 7, K), 1 + normal(g, K) / 4
+    h *= torch.tensor([1e-18, 1e-21, 1e-25, 1e-40, 0.0, 1e17, 1.0], device="cuda")[:, None]
+    fine = [0, 5, 6]
+    gh, gw = q.qnn_rms_norm_backward(grad, h, gamma, 0.0)
+    assert not torch.isfinite(gh[1:5]).any() and not torch.isfinite(gw).any()
+    rest = q.qnn_rms_norm_backward(grad[fine], h[fine], gamma, 0.0)
+    assert torch.equal(rest[0], gh[fine])
+    check_backward(rest, grad[fine], h[fine], gamma, 0.0, sum_error(K) + 2)
