@@ -168,7 +168,7 @@ __global__ __launch_bounds__(kThreads >= 256 ? kThreads : 256) void quant_rows_k
                                                                                      int64_t ld_codes, float *scale) {
     __shared__ SumTop shared[2][kThreads / 64];
     const int lane = threadIdx.x % kThreads;
-    const int64_t row = (int64_t)blockIdx.x * rows_per_block(kThreads) + threadIdx.x / kThreads;
+    const int64_t row = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * rows_per_block(kThreads) + threadIdx.x / kThreads;
     if (row >= n_rows) return;  // (the same for all lanes of a row, and a workgroup with a barrier has one)
     constexpr int kHeld = kPer > 0 ? kPer : 1;
     float v[kHeld][kVec];
@@ -214,12 +214,19 @@ __global__ __launch_bounds__(kThreads >= 256 ? kThreads : 256) void quant_rows_k
     }
 }
 
+// `blocks` workgroups of up to 1024 threads and less than a row of them more, blockIdx.y * gridDim.x + blockIdx.x the number of each: HIP launches fewer than 2^32
+// threads along a dimension
+inline dim3 grid_of(int64_t blocks) {
+    constexpr int64_t kLine = 1 << 21;
+    return blocks <= kLine ? dim3((unsigned)blocks) : dim3((unsigned)kLine, (unsigned)ceil_div(blocks, kLine));
+}
+
 template <typename Source, int kThreads, int kPer, bool kShort = false>
 int launch_shape(const char *what, const Source &src, int64_t n_rows, int64_t K, int8_t *codes, int64_t ld_codes, float *scale, hipStream_t s) {
     const int64_t blocks = ceil_div(n_rows, rows_per_block(kThreads));
     if (blocks > 0x7FFFFFFFLL) return fail(QNN_ERR_SHAPE, "%s: %lld rows", what, (long long)n_rows);
-    return QNN_LAUNCH(what, (quant_rows_kernel<Source, kThreads, kPer, kShort>), dim3((unsigned)blocks), dim3(kThreads >= 256 ? kThreads : 256), 0, s, src, n_rows,
-                      K, codes, ld_codes, scale);
+    return QNN_LAUNCH(what, (quant_rows_kernel<Source, kThreads, kPer, kShort>), grid_of(blocks), dim3(kThreads >= 256 ? kThreads : 256), 0, s, src, n_rows, K, codes,
+                      ld_codes, scale);
 }
 // Lanes and groups by the length of a row
 template <typename Source>
