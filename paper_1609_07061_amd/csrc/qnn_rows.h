@@ -158,6 +158,11 @@ struct TwoSums {
     static __device__ __forceinline__ TwoSums join(const TwoSums &x, const TwoSums &y) { return {x.a + y.a, x.b + y.b}; }
 };
 
+// `blocks` workgroups of up to 1024 threads, and less than a line of them more, in lines of kLine: HIP launches fewer than 2^32 threads along a dimension
+constexpr int64_t kLine = 1 << 21;
+inline dim3 grid_of(int64_t blocks) { return blocks <= kLine ? dim3((unsigned)blocks) : dim3((unsigned)kLine, (unsigned)ceil_div(blocks, kLine)); }
+__device__ __forceinline__ uint32_t block_number() { return blockIdx.y * (uint32_t)kLine + blockIdx.x; }
+
 constexpr int rows_per_block(int threads) { return threads >= 256 ? 1 : 256 / threads; }
 
 // One row per kThreads lanes.  Source: `load<kShort>(row, window, K, values, kept)` the values to be quantized, up to the factor `factor(sum)`;
@@ -168,7 +173,7 @@ __global__ __launch_bounds__(kThreads >= 256 ? kThreads : 256) void quant_rows_k
                                                                                      int64_t ld_codes, float *scale) {
     __shared__ SumTop shared[2][kThreads / 64];
     const int lane = threadIdx.x % kThreads;
-    const int64_t row = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * rows_per_block(kThreads) + threadIdx.x / kThreads;
+    const int64_t row = (int64_t)block_number() * rows_per_block(kThreads) + threadIdx.x / kThreads;
     if (row >= n_rows) return;  // (the same for all lanes of a row, and a workgroup with a barrier has one)
     constexpr int kHeld = kPer > 0 ? kPer : 1;
     float v[kHeld][kVec];
@@ -212,13 +217,6 @@ __global__ __launch_bounds__(kThreads >= 256 ? kThreads : 256) void quant_rows_k
             give(q, 0, Window(k, K));
         }
     }
-}
-
-// `blocks` workgroups of up to 1024 threads and less than a row of them more, blockIdx.y * gridDim.x + blockIdx.x the number of each: HIP launches fewer than 2^32
-// threads along a dimension
-inline dim3 grid_of(int64_t blocks) {
-    constexpr int64_t kLine = 1 << 21;
-    return blocks <= kLine ? dim3((unsigned)blocks) : dim3((unsigned)kLine, (unsigned)ceil_div(blocks, kLine));
 }
 
 template <typename Source, int kThreads, int kPer, bool kShort = false>
