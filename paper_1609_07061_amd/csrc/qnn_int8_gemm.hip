@@ -256,6 +256,8 @@ const Way &fastest(const Way (&ways)[kCount], int64_t M, int64_t N, int64_t K) {
     return *best;
 }
 
+constexpr int64_t kMostTiles = 1 << 22;  // of 512 threads: HIP launches fewer than 2^32 along a dimension
+
 template <typename T>
 int launch(const Args<T> &a, hipStream_t s) {
     const bool pieces = in_pieces(a.A, a.lda, a.M, a.K) && in_pieces(a.W, a.ldw, a.N, a.K), any = !pieces && a.K >= 16;
@@ -265,9 +267,18 @@ int launch(const Args<T> &a, hipStream_t s) {
                    : any   ? fastest(kWaysOfAny, a.M, a.N, a.K)
                            : kWaysOfAny[0];
     const int64_t tm = ceil_div(a.M, w.rows), tn = ceil_div(a.N, w.columns);
-    // (8 columns of tiles and what lies in them have 32 bits)
-    if (tm > 0x7FFFFFFFLL || tn > 0x0FFFFFFFLL || tm * tn > 0x7FFFFFFFLL)
-        return fail(QNN_ERR_SHAPE, "int8_gemm: M = %lld, N = %lld", (long long)a.M, (long long)a.N);
+    if ((double)tm * (double)tn > kMostTiles) {  // in two parts
+        Args<T> one = a, two = a;
+        if (tm >= tn) {
+            const int64_t m = tm / 2 * w.rows;
+            one.M = m, two.M -= m, two.A += m * a.lda, two.scaleA += m, two.out += m * a.ldo;
+        } else {
+            const int64_t n = tn / 2 * w.columns;
+            one.N = n, two.N -= n, two.W += n * a.ldw, two.scaleW += n, two.bias += a.bias ? n : 0, two.out += n;
+        }
+        const int rc = launch(one, s);
+        return rc ? rc : launch(two, s);
+    }
     const Tiles tiles = make_tiles(tm, tn);
     const dim3 grid((unsigned)(tm * tn));
     auto stream = [&](auto on_pieces, auto on_any) { return QNN_LAUNCH("int8_gemm", (pieces ? on_pieces : on_any), grid, dim3(512), 0, s, a, tiles); };

@@ -29,3 +29,29 @@ def test_rows(seed, K):
     q.qnn_silu_gate_quant(x[:, :K], x[:, K:], codes, scale)
     want = q.qnn_silu_gate_quant(base[:, :K], base[:, K:])
     assert _all_equal(codes, want[0]) and _all_equal(scale, want[1])
+
+
+def test_products_of_short_rows():
+    """More than 2^31 outputs in tiles of 16 x 16 on 512 threads each."""
+    import paper_1609_07061_amd as q
+
+    g, n, times = torch.Generator(device="cuda").manual_seed(5), 64, 725
+    A, W, sA, sW = codes_of(g, n, 3), codes_of(g, n, 3), normal(g, n), normal(g, n) * 0.01
+    want = q.qnn_int8_gemm(A, sA, W, sW, dtype=torch.float16)
+    assert ((want.double() - (A.double() @ W.double().t()) * sA.double()[:, None] * sW.double()).abs() <= 2.0 ** -10 * want.double().abs() + 2.0 ** -24).all()
+    got = q.qnn_int8_gemm(A.repeat(times, 1), sA.repeat(times), W.repeat(times, 1), sW.repeat(times), dtype=torch.float16)
+    assert _all_equal(got, want.repeat(1, times))
+
+
+@pytest.mark.parametrize("K", [16, 17])
+def test_products_of_many_rows(K):
+    """2^29 rows and more, in tiles of 64 x 16 on 512 threads each."""
+    import paper_1609_07061_amd as q
+
+    g, few, rows = torch.Generator(device="cuda").manual_seed(K), 4099, (1 << 29) + 4321
+    A, W, sA, sW = codes_of(g, few, K), codes_of(g, 3, K), normal(g, few), normal(g, 3) * 0.01
+    want = q.qnn_int8_gemm(A, sA, W, sW, dtype=torch.float16)
+    assert ((want.double() - (A.double() @ W.double().t()) * sA.double()[:, None] * sW.double()).abs() <= 2.0 ** -10 * want.double().abs() + 2.0 ** -24).all()
+    times = rows // few + 1
+    got = q.qnn_int8_gemm(A.repeat(times, 1)[:rows], sA.repeat(times)[:rows], W, sW, dtype=torch.float16)
+    assert _all_equal(got, want)
