@@ -5,6 +5,8 @@
 // y and nothing is clipped.  a = 0: scale and codes 0.  A value that is not finite: scale NaN and codes 0, so that whatever is formed from the row is
 // NaN too.  (LinearQuant of Sec. 3 has one step for a whole tensor; activations of a language model differ in size from token to token.)
 #pragma once
+#include <type_traits>
+
 #include "qnn_internal.h"
 
 namespace qnn {
@@ -50,7 +52,13 @@ template <bool kOnce, bool kShort, typename T>
 __device__ __forceinline__ void store_values(T *row, const Window &w, int64_t K, const float (&v)[kVec]) {
     Raw<T> r;
 #pragma unroll
-    for (int i = 0; i < kVec; ++i) r.e[i] = (T)v[i];  // to nearest, ties to even
+    for (int i = 0; i < kVec; ++i) {
+        float x = v[i];
+        // From the value in fp32.  (A product that the compiler rounds to fp16 in one instruction now and then differs in the last place from one that it rounds
+        // twice, and which it takes depends on the variant and on the place in a window.)
+        if constexpr (std::is_same<T, f16>::value) asm("" : "+v"(x));
+        r.e[i] = (T)x;  // to nearest, ties to even
+    }
     if (!kShort && w.skip == 0) {
         if constexpr (kOnce) {
             Words4 u[sizeof r / 16];
