@@ -15,9 +15,12 @@ EPS = 1e-5
 
 
 def codes_of_rows(w):
-    """Weights as int8 codes with a scale for every output channel, laid out once per change of the weights."""
-    scale = w.abs().amax(dim=-1) / 127
-    return (w / scale[..., None]).round_().to(torch.int8), scale.float()
+    """Weights as int8 codes with a scale for every output channel, laid out once per change of the weights.  A channel of zeros has scale 0, one with a value that
+    is not finite scale NaN, both codes 0."""
+    scale = w.abs().amax(dim=-1).float() / 127
+    fine = torch.isfinite(scale) & (scale > 0)
+    codes = (w / torch.where(fine, scale, 1.0)[..., None]).round_()
+    return torch.where(fine[..., None], codes, 0.0).to(torch.int8), torch.where(torch.isfinite(scale), scale, math.nan)
 
 
 class FeedForward:
