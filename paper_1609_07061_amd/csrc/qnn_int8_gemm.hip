@@ -216,12 +216,14 @@ __global__ __launch_bounds__(256, 2) void gemm_tile_kernel(const Args<T> a, cons
     }
 }
 
-// The ways a product can go, by rows and columns of a workgroup's tile, and about how long each takes (us): start + more (R - 1) + k R K / 1024, with R the
-// rounds of `side` tiles a compute unit.  Fitted to 66 products of 8 .. 5000 rows, 256 .. 4096 columns and K of 512 .. 7168 each (those on 128 x 128 to 28 of
-// 500 .. 4000 rows), where the way that comes out ahead is 1 % slower than the fastest in the mean.  (us of the fastest ways at N = K = 4096, M = 16:
-// 16 x 16 5.7, 64 x 16 6.2; 64: 7.2 of 64 x 16, 8.3 and 7.7 of those beside it; 128: 64 x 32 8.1, 64 x 64 10.6; 256: 64 x 64 11.5, panels 12.7, 64 x 32 14.1;
-// 512: panels of 64 x 64 17.8, of 128 x 128 18.3 on eight waves and 24.8 on four; 1024: 27.5, 23.7 and 28.6; 2000: 43.6 on eight and 38.2 on four; 5000: 86 on
-// four, 256 x 256 90; 8192 x 8192 x 8192: 524 and 417.)
+// The ways a product can go, by rows and columns of a workgroup's tile.  The least start + more (R - 1) + k R K / 1024 is taken, with R the rounds of `side` tiles
+// a compute unit: formed like a time in us, but it only ranks the ways (one round or many, and what overlaps, share one line; 2000 x 4096 x 4096 on the pairs comes
+// out as 28 and takes 35).  Fitted to products of all three kinds of rows, judged on others: 200 of each kind drawn over 1 .. 20000 rows, 64 .. 12000 columns and
+// K of 16 .. 9000, where the way that comes out ahead takes in the mean 1.6 % (pieces), 1.8 % (words) and 0.7 % (any rows) longer than the fastest of all, and 22,
+// 32 and 31 % at most.  (us at N = K = 4096, bf16 out, inputs in the caches: M = 16: 16 x 16 3.8, 64 x 16 5.3; 64: 64 x 16 6.1, 64 x 32 6.5, 16 x 16 8.3;
+// 128: 64 x 32 6.9, 64 x 64 9.1, 64 x 16 10.1; 256: 64 x 64 10.5, panels of 64 x 64 11.1, 64 x 32 12.2; 512: panels of 64 x 64 15.3, of 128 x 128 on eight waves
+// 16.9 and in pairs 22.3, streams 19.3; 1024: 29.4, 21.5, 26.1; 2000: 56.1, 39.6, 35.1, 256 x 256 42.2; 5000: 137, 95, 86, 89; 8192 x 8192 x 8192: 824, 553, 507,
+// 386.)  The pairs are two workgroups on a compute unit: counted as one round of two tiles, since with rounds of one the choice costs 3.9 % where this costs 1.9.
 enum WayId { kStream16x16, kStream64x16, kStream64x32, kStream64x64, kPanel64, kPanel128, kPanel128Pairs, kPanel256, kTile128 };
 struct Way {
     WayId id;
@@ -229,17 +231,16 @@ struct Way {
     double start, more, k;
 };
 constexpr Way kWaysOfPieces[] = {{kStream16x16, 16, 16, 1, 2.7, 0.56, 0.276},     {kStream64x16, 64, 16, 1, 3.1, 1.95, 0.743}, {kStream64x32, 64, 32, 1, 3.3, 2.37, 0.924},
-                                 {kStream64x64, 64, 64, 1, 4.3, 3.93, 1.306},     {kPanel64, 64, 64, 1, 3.6, 0.03, 1.838},     {kPanel128, 128, 128, 1, 4.7, 2.51, 4.068},
+                                 {kStream64x64, 64, 64, 1, 4.3, 3.93, 1.306},     {kPanel64, 64, 64, 1, 3.6, 0.80, 1.600},     {kPanel128, 128, 128, 1, 4.7, 2.51, 4.068},
                                  {kPanel128Pairs, 128, 128, 2, 4.7, 8.98, 5.945}, {kPanel256, 256, 256, 1, 6.4, 9.10, 8.518}};
-// Rows at any address: fitted to 78 products of 5 .. 4000 rows, of each of which the fastest way comes out ahead.
+// Rows at any address
 constexpr Way kWaysOfAny[] = {{kStream16x16, 16, 16, 1, 2.8, 0.33, 0.671},
                               {kStream64x16, 64, 16, 1, 3.4, 1.04, 1.610},
                               {kStream64x32, 64, 32, 1, 3.9, 3.11, 2.022},
                               {kStream64x64, 64, 64, 1, 5.2, 4.72, 2.982},
                               {kTile128, 128, 128, 1, 6.2, 4.49, 7.015}};
-// Rows of whole words: the streams' as above, panels fitted to 75 products of 60 .. 8192 rows, where the way ahead is 1.0 % slower than the fastest in the
-// mean.  (300 x 4100 x 3004: 64 x 64 18.4 us, without panels 25.0; 4000 x 4000 x 4004: 256 x 256 69.5, 128 x 128 94.5, without panels 104; 1999 x 3001 x 2500:
-// 128 x 128 36.9, without panels 37.7.)
+// Rows of whole words: streams as above, panels.  (300 x 4100 x 3004: panels of 64 x 64 16.7 us, streams of 64 x 64 18.0; 4000 x 4000 x 4004: 256 x 256 69,
+// 128 x 128 96; 1999 x 3001 x 2500: 128 x 128 29.5, 256 x 256 43.6.  Counting the pairs two tiles a round changes nothing here: 2.6 and 2.5 %.)
 constexpr Way kWaysOfWords[] = {{kStream16x16, 16, 16, 1, 2.8, 0.33, 0.671}, {kStream64x16, 64, 16, 1, 3.4, 1.04, 1.610},
                                 {kStream64x32, 64, 32, 1, 3.9, 3.11, 2.022}, {kStream64x64, 64, 64, 1, 5.2, 4.72, 2.982},
                                 {kPanel64, 64, 64, 1, 5.4, 0.80, 2.486},     {kPanel128Pairs, 128, 128, 1, 6.8, 1.21, 5.749},

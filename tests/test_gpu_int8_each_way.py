@@ -26,15 +26,15 @@ WAYS = {
 # Sizes at which the rule (for 256 compute units) takes each way: the first for operands and outputs with a pitch too
 SIZES = [
     ("pieces 16 x 16", 63, 65, 16), ("pieces 16 x 16", 3, 1001, 4112), ("pieces 64 x 16", 129, 500, 16), ("pieces 64 x 16", 63, 2049, 16), ("pieces 64 x 16", 60, 4000, 4096),
-    ("pieces 64 x 32", 257, 1001, 16), ("pieces 64 x 32", 120, 4096, 4112), ("pieces 64 x 64", 129, 3001, 2048), ("pieces 64 x 64", 256, 4090, 4096),
+    ("pieces 64 x 32", 257, 1001, 16), ("pieces 64 x 32", 120, 4096, 4112), ("pieces 64 x 64", 256, 4090, 4096), ("pieces 64 x 64", 190, 3901, 4112),
     ("any 16 x 16", 63, 65, 21), ("any 16 x 16", 16, 4095, 1001), ("any 64 x 16", 257, 500, 21), ("any 64 x 16", 60, 4000, 4093), ("any 64 x 32", 257, 1001, 21),
     ("any 64 x 32", 120, 4096, 1023), ("any 64 x 64", 129, 3001, 261), ("any 64 x 64", 256, 4090, 2047),
     ("any 128 x 128", 1500, 3000, 250), ("any 128 x 128", 6000, 130, 21), ("any 128 x 128", 129, 8001, 21), ("any 128 x 128", 2500, 2049, 129), ("any 128 x 128", 1999, 1001, 2501),
     ("short", 100, 900, 15), ("short", 1, 5000, 1),
-    ("panel 64", 129, 3001, 16), ("panel 64", 700, 1000, 272), ("panel 64", 9000, 9001, 256), ("panel 64", 1200, 1024, 1040),
+    ("panel 64", 129, 3001, 16), ("panel 64", 700, 1000, 272), ("panel 64", 5000, 130, 528), ("panel 64", 1200, 1024, 1040),
     ("panel 128, eight waves", 1500, 2049, 400), ("panel 128, eight waves", 500, 8001, 400), ("panel 128, eight waves", 500, 4097, 1024), ("panel 128, eight waves", 1023, 4090, 2064),
     ("panel 128", 1500, 4097, 144), ("panel 128", 1000, 8001, 128), ("panel 128", 4000, 1025, 592), ("panel 128", 1190, 4000, 1008),
-    ("panel 256", 3000, 5000, 128), ("panel 256", 2000, 8001, 128), ("panel 256", 2000, 4097, 400), ("panel 256", 5003, 4097, 1168),
+    ("panel 256", 3000, 5000, 128), ("panel 256", 2000, 8001, 128), ("panel 256", 2000, 4097, 400), ("panel 256", 5003, 4097, 1168), ("panel 256", 9000, 9001, 256), ("panel 256", 5000, 4099, 16),
     ("words 64", 129, 3001, 516), ("words 64", 6000, 130, 20), ("words 64", 129, 8001, 20), ("words 64", 300, 4100, 1500),
     ("words 128", 500, 4097, 20), ("words 128", 257, 8001, 20), ("words 128", 1500, 3001, 516), ("words 128", 2500, 2049, 1148),
     ("words 256", 2000, 4097, 132), ("words 256", 3000, 4097, 20), ("words 256", 2000, 8001, 20), ("words 256", 4003, 4001, 1284), ("words 256", 4000, 4000, 4004),
