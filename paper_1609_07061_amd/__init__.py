@@ -635,7 +635,7 @@ def _vector(t: torch.Tensor, n: int, name: str) -> torch.Tensor:
 
 
 def _new_codes(rows: int, cols: int, like: torch.Tensor) -> torch.Tensor:
-    """Codes whose rows start at multiples of 16 bytes, which the products read fastest."""
+    """Codes whose rows start at multiples of 16 bytes: the products read them fastest where the rows are also a multiple of 16 codes long."""
     return torch.empty((rows, (cols + 15) // 16 * 16), dtype=torch.int8, device=like.device)[:, :cols]
 
 

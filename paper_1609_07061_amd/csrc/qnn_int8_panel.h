@@ -6,7 +6,7 @@
 // one's operands in flight.  What is different is the way out (floats, half as wide or as wide as the sums) and that nothing pads the operands: codes of k
 // beyond the rows are loaded from the rows' beginning and zeroed on one side behind LDS.
 //
-// What bounds it: at 8192 x 8192 x 8192 the card's power (codes of a normal distribution: 403 - 417 us, 2.6 - 2.7 P op/s, the matrix cores busy 73 % of
+// What bounds it: at 8192 x 8192 x 8192 the card's power (codes of a normal distribution: 386 - 417 us, 2.6 - 2.8 P op/s, the matrix cores busy 73 % of
 // 710 k cycles at 1.76 GHz; all zeros run at 2.44 GHz).  16 x 16 x 64 instead of 32 x 32 x 32 matrix instructions: half as many updates of sums a product,
 // 484 -> 425 us.  At middle sizes the fixed part and LDS: 64 x 64 sums a wave read 64 KB and write 32 KB of LDS for 512 cycles of matrix instructions.
 #pragma once
@@ -28,7 +28,7 @@ namespace panel {
 constexpr int kRow = 128;  // codes of a row in a group
 
 // WM x WN waves, each with 32 BA rows of A and 32 BW rows of W; kRing groups in LDS; kPerUnit workgroups on a compute unit.  (1024 x 4096 x 4096 on 128 x 128:
-// four waves 28.6 us, two such teams on alternate groups of k or four groups in LDS 24.0 to 24.5, eight waves and four groups 23.7.)
+// four waves 26.1 us, eight waves and four groups 21.5; two teams of four on alternate groups of k, or four groups in LDS for four waves, lay between.)
 template <int WM_, int WN_, int BA_, int BW_, int kRing_, int kPerUnit_, bool kWords_ = false>
 struct Shape {
     static constexpr int WM = WM_, WN = WN_, BA = BA_, BW = BW_, kRing = kRing_, kPerUnit = kPerUnit_;
@@ -301,7 +301,8 @@ typedef Shape<2, 4, 4, 2, 2, 1> Large;  // 256 x 256
 typedef Shape<2, 2, 2, 2, 2, 2> Small;  // 128 x 128, two workgroups on a compute unit
 typedef Shape<2, 4, 2, 1, 4, 1> Eight;  // 128 x 128 on eight waves
 typedef Shape<2, 2, 1, 1, 4, 2> Tiny;   // 64 x 64
-// the same for words (a line of 256 bytes a load: slower by half, but 4000 x 4000 x 4004 104 us through registers, 69.5 like this)
+// the same for words (a line of 256 bytes a load: slower by half, but 4000 x 4000 x 4004 104 us through registers, 69 like this; the largest spills 7 to 9 registers in the
+// way out, none in the loop over k)
 typedef Shape<2, 4, 4, 2, 2, 1, true> LargeWords;
 typedef Shape<2, 2, 2, 2, 2, 2, true> SmallWords;
 typedef Shape<2, 2, 1, 1, 4, 2, true> TinyWords;
