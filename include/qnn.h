@@ -365,6 +365,78 @@ int qnn_int8_moe(const int8_t *x, int64_t ldx, const float *scale_x, const float
                  int64_t ldo, int type, void *workspace, size_t workspace_bytes, void *stream);
 size_t qnn_int8_moe_workspace_bytes(int64_t tokens, int top, int64_t F);
 
+/* Attention half of a decoder block on int8 codes.  Keys and values of earlier tokens lie as codes, one float32 scale for each token and head (a code stands for
+ * code * scale, as above), in PAGES of `page` tokens that sequences take in any order. */
+
+/* Positions of tokens and the rotation that they stand for: pair i of a head turns by the angle positions[axis[i]][token] * freq[i], formed in 64 bits. */
+typedef struct {
+    const int32_t *positions; /* DEVICE [axes][ld_positions]: one row, or one for time, height, width and so on */
+    int64_t ld_positions;
+    const double *freq;       /* DEVICE [pairs], radians a position */
+    const int32_t *axis;      /* DEVICE [pairs] (NULL: the first axis for all); numbers outside 0 .. axes - 1 count as the nearest of these */
+    int32_t axes, pairs;      /* the first 2 * pairs values of a head are rotated; pairs is a multiple of 8; 0: no rotation, and the pointers may be NULL */
+    int32_t neighbours;       /* 0: values i and i + pairs are a pair; otherwise values 2 i and 2 i + 1 */
+} qnn_rotation;
+
+/* A paged cache and the sequences of one call.  Of sequence b the table's row b names the pages, page after page; lengths[b] tokens of it are in the cache or being
+ * appended, and the last starts[b + 1] - starts[b] of these are the call's tokens starts[b] .. starts[b + 1] - 1: its NEW tokens.  Tokens of the call that no
+ * sequence has (before starts[0], from starts[sequences] on) are left alone.  A page number outside 0 .. pages - 1, or a token beyond the table's width, names no
+ * page: such a token is not stored, and not seen.  Lengths are at most 2^31 - 4096. */
+typedef struct {
+    int8_t *k, *v;                   /* DEVICE [pages][heads][page][D], dense, 16-byte aligned */
+    float *k_scale, *v_scale;        /* DEVICE [pages][heads][page] */
+    int64_t pages, heads, page, D;   /* pages * heads * page < 2^32; D a multiple of 16, at most 256 */
+    const int32_t *table;            /* DEVICE [sequences][ld_table], `width` entries of a row */
+    int64_t ld_table, width;
+    const int32_t *starts, *lengths; /* DEVICE [sequences + 1], not decreasing; [sequences] */
+    int64_t sequences;
+} qnn_paged_cache;
+
+/* Norm of every head of queries and keys and the rotation by the tokens' positions, in one pass.  Of a head h of D values:
+ *   n = h / sqrt(mean(h^2) + eps) * gamma   (gamma NULL: n = h),   then of every pair  y_a = n_a cos - n_b sin,  y_b = n_b cos + n_a sin.
+ * q, k: DEVICE, value d of head h of token t at t * ld + h * step + d, of `type`; q_out, k_out likewise, and they may be q, k themselves (same strides).
+ * heads_k may be 0 (k, k_out NULL).  gamma_q, gamma_k: DEVICE [D] of float32 or `type` (gamma_type), both or neither.  D a multiple of 16, at most 256.
+ * What counts as not finite is as in qnn_rms_norm_quant: such a head is NaN or infinite. */
+int qnn_qk_norm_rotate(const void *q, int64_t ld_q, int64_t step_q, int64_t heads_q, const void *k, int64_t ld_k, int64_t step_k, int64_t heads_k, int type,
+                       const void *gamma_q, const void *gamma_k, int gamma_type, float eps, const qnn_rotation *rotation, int64_t tokens, int64_t D, void *q_out,
+                       int64_t ld_q_out, int64_t step_q_out, void *k_out, int64_t ld_k_out, int64_t step_k_out, void *stream);
+
+/* Its gradient.  With g = grad turned back by the same angles and r = 1 / sqrt(mean(h^2) + eps):
+ *   out = r (gamma g - h r^2 mean(gamma g h)),   grad_gamma = sum over tokens and heads of g h r   (DEVICE float32 [D]);   gamma NULL: out = g.
+ * q, k: what the forward call read.  out_q may be grad_q, out_k grad_k (same strides).  tokens >= 1 where there is a gamma.  workspace: DEVICE, 256-byte aligned,
+ * qnn_qk_norm_rotate_backward_workspace_bytes(...) bytes (without gamma none).  Sums are formed in a fixed order. */
+int qnn_qk_norm_rotate_backward(const void *grad_q, int64_t ld_grad_q, int64_t step_grad_q, const void *grad_k, int64_t ld_grad_k, int64_t step_grad_k, const void *q,
+                                int64_t ld_q, int64_t step_q, int64_t heads_q, const void *k, int64_t ld_k, int64_t step_k, int64_t heads_k, int type,
+                                const void *gamma_q, const void *gamma_k, int gamma_type, float eps, const qnn_rotation *rotation, int64_t tokens, int64_t D,
+                                void *out_q, int64_t ld_out_q, int64_t step_out_q, void *out_k, int64_t ld_out_k, int64_t step_out_k, float *grad_gamma_q,
+                                float *grad_gamma_k, void *workspace, size_t workspace_bytes, void *stream);
+size_t qnn_qk_norm_rotate_backward_workspace_bytes(int64_t tokens, int64_t heads_q, int64_t heads_k, int64_t D);
+
+/* Keys and values of new tokens into the cache: keys normed and rotated as above, keys and values then to codes with a scale for each token and head, as
+ * qnn_rms_norm_quant forms them of a row.  k, v: DEVICE [tokens][cache->heads][D] with strides as above.  q (heads_q 0: none): the queries beside them, normed and
+ * rotated to q_out in the same launch.  No two tokens of a call may have the same place in the cache. */
+int qnn_cache_append(const qnn_paged_cache *cache, const void *q, int64_t ld_q, int64_t step_q, int64_t heads_q, const void *k, int64_t ld_k, int64_t step_k,
+                     const void *v, int64_t ld_v, int64_t step_v, int type, const void *gamma_q, const void *gamma_k, int gamma_type, float eps,
+                     const qnn_rotation *rotation, int64_t tokens, void *q_out, int64_t ld_q_out, int64_t step_q_out, void *stream);
+
+/* Attention of the new tokens' queries over the cache, after their own keys and values are in it.  heads_q is a multiple of cache->heads; query head h reads
+ * head h / (heads_q / cache->heads).  Of query i and key j of a sequence of n tokens, m of them new:
+ *   s = scale * q_i . k_j;  with cap > 0: s = cap * tanh(s / cap);  with slopes: s -= slopes[h] * (place(i) - place(j));   out_i = sum_j softmax_j(s) v_j.
+ * A query sees the tokens up to itself.  With a tree it sees the first n - m tokens and, of the new ones, those whose bit is set in its mask tree[i] (bit t: new
+ * token t of the sequence; new tokens from the 65th on are seen by none).  A query that sees nothing gets zeros.
+ * place is the index in the sequence; with a tree that of a new token is n - m - 1 + (bits set in its mask).
+ * q, out: DEVICE [tokens][heads_q][D] with strides as above, of `type`; slopes: DEVICE float32 [heads_q] or NULL; tree: DEVICE uint64 [tokens] or NULL.
+ * most_new, longest: the most new tokens of a sequence and the longest sequence, as far as the host knows; they set how the work is split, so that results depend
+ * on them in the last places, and any numbers >= 1 are right.  workspace: DEVICE, 256-byte aligned, qnn_cache_attention_workspace_bytes(...) bytes (0: none).
+ * A scale of the cache that is NaN makes every query NaN that sees it, and no other.  A query that is not finite gets NaN.  Sums are formed in a fixed order. */
+int qnn_cache_attention(const qnn_paged_cache *cache, const void *q, int64_t ld_q, int64_t step_q, int64_t heads_q, int type, float scale, float cap,
+                        const float *slopes, const uint64_t *tree, int64_t tokens, int64_t most_new, int64_t longest, void *out, int64_t ld_out,
+                        int64_t step_out, void *workspace, size_t workspace_bytes, void *stream);
+size_t qnn_cache_attention_workspace_bytes(int64_t tokens, int64_t sequences, int64_t heads_q, int64_t heads, int64_t D, int64_t most_new, int64_t longest);
+
+/* Rows to codes with a scale each, without a norm or an activation: what an output product takes.  x: DEVICE [rows][ldx] of `type`. */
+int qnn_rows_quant(const void *x, int64_t ldx, int type, int64_t rows, int64_t K, int8_t *codes, int64_t ld_codes, float *scale, void *stream);
+
 /* Engine (QNN_ENGINE_VALU, QNN_ENGINE_MFMA, QNN_ENGINE_MFMA_FP4 or QNN_ENGINE_MFMA_LDS) that ran the calling thread's last successful
  * multiply call; 0 before any.  QNN_ENGINE_MFMA_FP4 covers every kernel on the FP4 matrix cores: with QNN_ENGINE_AUTO also those for
  * products of several planes and of any size, which the engine asked for by name does not take.  For reports: results never depend on

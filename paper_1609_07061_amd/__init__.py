@@ -73,6 +73,12 @@ _SIGS = {
     "qnn_int8_gemm": [_vp, _i64, _vp, _vp, _i64, _vp, _vp, _vp, _i64, _int, _i64, _i64, _i64, _vp],
     "qnn_int8_moe": [_vp, _i64, _vp, _vp, _i64, _i64, _int, _int, _i64, _i64, _vp, _i64, _vp, _vp, _i64, _vp, _vp, _i64, _int, _vp,
                      _sz, _vp],
+    "qnn_qk_norm_rotate": [_vp, _i64, _i64, _i64, _vp, _i64, _i64, _i64, _int, _vp, _vp, _int, C.c_float, _vp, _i64, _i64, _vp, _i64, _i64, _vp, _i64, _i64, _vp],
+    "qnn_qk_norm_rotate_backward": [_vp, _i64, _i64, _vp, _i64, _i64, _vp, _i64, _i64, _i64, _vp, _i64, _i64, _i64, _int, _vp, _vp, _int, C.c_float, _vp, _i64, _i64,
+                                    _vp, _i64, _i64, _vp, _i64, _i64, _vp, _vp, _vp, _sz, _vp],
+    "qnn_cache_append": [_vp, _vp, _i64, _i64, _i64, _vp, _i64, _i64, _vp, _i64, _i64, _int, _vp, _vp, _int, C.c_float, _vp, _i64, _vp, _i64, _i64, _vp],
+    "qnn_cache_attention": [_vp, _vp, _i64, _i64, _i64, _int, C.c_float, C.c_float, _vp, _vp, _i64, _i64, _i64, _vp, _i64, _i64, _vp, _sz, _vp],
+    "qnn_rows_quant": [_vp, _i64, _int, _i64, _i64, _vp, _i64, _vp, _vp],
 }
 for _name, _args in _SIGS.items():
     _f = getattr(_lib, _name)
@@ -91,6 +97,10 @@ _lib.qnn_rms_norm_backward_workspace_bytes.argtypes = [_i64, _i64]
 _lib.qnn_rms_norm_backward_workspace_bytes.restype = _sz
 _lib.qnn_int8_moe_workspace_bytes.argtypes = [_i64, _int, _i64]
 _lib.qnn_int8_moe_workspace_bytes.restype = _sz
+_lib.qnn_qk_norm_rotate_backward_workspace_bytes.argtypes = [_i64, _i64, _i64, _i64]
+_lib.qnn_qk_norm_rotate_backward_workspace_bytes.restype = _sz
+_lib.qnn_cache_attention_workspace_bytes.argtypes = [_i64] * 7
+_lib.qnn_cache_attention_workspace_bytes.restype = _sz
 _lib.qnn_last_engine.restype = C.c_int
 _lib.qnn_last_error.restype = C.c_char_p
 _lib.qnn_version.restype = C.c_char_p
@@ -125,7 +135,8 @@ _lib.qnn_last_engines.restype = C.c_int
 
 EXPORTS = sorted(list(_SIGS) + ["qnn_binary_mlp_workspace_bytes", "qnn_static_scratch_bytes", "qnn_binary_convnet_workspace_bytes",
                                "qnn_binary_backward_workspace_bytes", "qnn_conv2d_dedup_workspace_bytes", "qnn_rms_norm_backward_workspace_bytes",
-                               "qnn_int8_moe_workspace_bytes", "qnn_last_engine",
+                               "qnn_int8_moe_workspace_bytes", "qnn_qk_norm_rotate_backward_workspace_bytes",
+                               "qnn_cache_attention_workspace_bytes", "qnn_last_engine",
                                "qnn_last_engines", "qnn_last_error", "qnn_version"])
 
 
@@ -795,3 +806,208 @@ def qnn_int8_moe(x: torch.Tensor, scale_x: torch.Tensor, logits: torch.Tensor, t
                              _dev(scale2, torch.float32, "scale2"), _dev(out, out.dtype, "out"), _shaped(out, T, H, "out"),
                              _float_type(out, "out"), _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream()))
     return out
+
+
+# ----------------------------------------------------------------------------------- attention half of a decoder block on int8 codes
+class _Rotation(C.Structure):  # qnn_rotation
+    _fields_ = [("positions", _vp), ("ld_positions", _i64), ("freq", _vp), ("axis", _vp), ("axes", C.c_int32), ("pairs", C.c_int32), ("neighbours", C.c_int32)]
+
+
+class _PagedCache(C.Structure):  # qnn_paged_cache
+    _fields_ = [("k", _vp), ("v", _vp), ("k_scale", _vp), ("v_scale", _vp), ("pages", _i64), ("heads", _i64), ("page", _i64), ("D", _i64), ("table", _vp),
+                ("ld_table", _i64), ("width", _i64), ("starts", _vp), ("lengths", _vp), ("sequences", _i64)]
+
+
+def _here(t: Optional[torch.Tensor], dtype, name: str) -> Optional[int]:
+    """Address of a tensor on the current device, where the call is going to run."""
+    p = _dev(t, dtype, name)
+    if t is not None and t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, the current device is {torch.cuda.current_device()}")
+    return p
+
+
+def _heads(t: torch.Tensor, tokens: int, heads: int, D: int, dtype, name: str):
+    """(address, stride of a token, stride of a head) of a [tokens][heads][D] tensor with contiguous heads."""
+    shape, stride = t.shape, t.stride()
+    if tuple(shape) != (tokens, heads, D) or (D > 1 and stride[2] != 1):
+        raise ValueError(f"{name} must be [{tokens}][{heads}][{D}] with contiguous heads, got {list(shape)}")
+    step = stride[1] if heads > 1 else D
+    return _here(t, dtype, name), stride[0] if tokens > 1 else heads * step, step
+
+
+def _heads_shape(t: torch.Tensor, name: str):
+    if t.dim() != 3:
+        raise ValueError(f"{name} must be [tokens][heads][D]")
+    return t.shape
+
+
+def _rotation(positions: Optional[torch.Tensor], freq: Optional[torch.Tensor], axis: Optional[torch.Tensor], neighbours: bool, tokens: int) -> _Rotation:
+    if freq is None:
+        return _Rotation(None, 0, None, None, 0, 0, 0)
+    if positions is None:
+        raise ValueError("a rotation needs positions")
+    if positions.dim() == 1:
+        positions = positions[None]
+    axes, n, ld = _rows_ld(positions, "positions")
+    if n != tokens:
+        raise ValueError(f"positions must be [axes][{tokens}], got [{axes}][{n}]")
+    if freq.dim() != 1:
+        raise ValueError("freq must be dense [pairs]")
+    pairs = freq.shape[0]
+    return _Rotation(_here(positions, torch.int32, "positions"), ld, _here(_vector(freq, pairs, "freq"), torch.float64, "freq"),
+                     None if axis is None else _here(_vector(axis, pairs, "axis"), torch.int32, "axis"), axes, pairs, 1 if neighbours else 0)
+
+
+def _gammas(gamma_q: Optional[torch.Tensor], gamma_k: Optional[torch.Tensor], D: int):
+    """Addresses and the type that they share."""
+    kind = 0
+    for g, name in ((gamma_q, "gamma_q"), (gamma_k, "gamma_k")):
+        if g is not None:
+            kind = _float_type(_vector(g, D, name), name)
+    if gamma_q is not None and gamma_k is not None and gamma_q.dtype != gamma_k.dtype:
+        raise ValueError(f"gamma_q and gamma_k must have one type, got {gamma_q.dtype} and {gamma_k.dtype}")
+    return (None if gamma_q is None else _here(gamma_q, gamma_q.dtype, "gamma_q"), None if gamma_k is None else _here(gamma_k, gamma_k.dtype, "gamma_k"), kind)
+
+
+def qnn_qk_norm_rotate(q: torch.Tensor, k: torch.Tensor, gamma_q: Optional[torch.Tensor], gamma_k: Optional[torch.Tensor], eps: float,
+                       positions: Optional[torch.Tensor], freq: Optional[torch.Tensor], axis: Optional[torch.Tensor] = None, neighbours: bool = False,
+                       q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
+    """Norm of every head of queries and keys (none where the gammas are None) and the rotation by the tokens' positions (none where freq is None).
+    q, k: [tokens][heads][D], also parts of one product's rows; positions: int32 [axes][tokens] (or [tokens]); freq: float64 [pairs], radians a position; axis: int32
+    [pairs], which row of positions a pair takes; neighbours: pairs are values 2 i, 2 i + 1 instead of i, i + pairs -> (q_out, k_out), which may be q, k."""
+    T, Hq, D = _heads_shape(q, "q")
+    Hk = _heads_shape(k, "k")[1]
+    kind = _float_type(q, "q")
+    if q_out is None:
+        q_out = torch.empty((T, Hq, D), dtype=q.dtype, device=q.device)
+    if k_out is None:
+        k_out = torch.empty((T, Hk, D), dtype=q.dtype, device=q.device)
+    gq, gk, gamma_kind = _gammas(gamma_q, gamma_k, D)
+    _check(_lib.qnn_qk_norm_rotate(*_heads(q, T, Hq, D, q.dtype, "q"), Hq, *_heads(k, T, Hk, D, q.dtype, "k"), Hk, kind, gq, gk, gamma_kind, eps,
+                                   C.byref(_rotation(positions, freq, axis, neighbours, T)), T, D, *_heads(q_out, T, Hq, D, q.dtype, "q_out"),
+                                   *_heads(k_out, T, Hk, D, q.dtype, "k_out"), _stream()))
+    return q_out, k_out
+
+
+def qnn_qk_norm_rotate_backward_workspace_bytes(tokens: int, heads_q: int, heads_k: int, D: int) -> int:
+    return int(_lib.qnn_qk_norm_rotate_backward_workspace_bytes(tokens, heads_q, heads_k, D))
+
+
+def qnn_qk_norm_rotate_backward(grad_q: torch.Tensor, grad_k: torch.Tensor, q: torch.Tensor, k: torch.Tensor, gamma_q: Optional[torch.Tensor],
+                                gamma_k: Optional[torch.Tensor], eps: float, positions: Optional[torch.Tensor], freq: Optional[torch.Tensor],
+                                axis: Optional[torch.Tensor] = None, neighbours: bool = False, out_q: Optional[torch.Tensor] = None,
+                                out_k: Optional[torch.Tensor] = None, grad_gamma_q: Optional[torch.Tensor] = None,
+                                grad_gamma_k: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """Gradient of qnn_qk_norm_rotate.  q, k: what the forward call read (so not outputs in their place) -> (out_q, out_k of the type of q, which may be grad_q,
+    grad_k, grad_gamma_q, grad_gamma_k float32 [D], None without gammas)."""
+    T, Hq, D = _heads_shape(q, "q")
+    Hk = _heads_shape(k, "k")[1]
+    kind = _float_type(q, "q")
+    if out_q is None:
+        out_q = torch.empty((T, Hq, D), dtype=q.dtype, device=q.device)
+    if out_k is None:
+        out_k = torch.empty((T, Hk, D), dtype=q.dtype, device=q.device)
+    gq, gk, gamma_kind = _gammas(gamma_q, gamma_k, D)
+    norm = gamma_q is not None or gamma_k is not None
+    need = qnn_qk_norm_rotate_backward_workspace_bytes(T, Hq, Hk, D) if norm else 0
+    if norm:
+        if gamma_q is not None and grad_gamma_q is None:
+            grad_gamma_q = torch.empty(D, dtype=torch.float32, device=q.device)
+        if gamma_k is not None and grad_gamma_k is None:
+            grad_gamma_k = torch.empty(D, dtype=torch.float32, device=q.device)
+        if workspace is None:
+            workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=q.device)
+    sums = [None if g is None or not norm else _here(_vector(g, D, name), torch.float32, name)
+            for g, name in ((grad_gamma_q, "grad_gamma_q"), (grad_gamma_k, "grad_gamma_k"))]
+    _check(_lib.qnn_qk_norm_rotate_backward(
+        *_heads(grad_q, T, Hq, D, q.dtype, "grad_q"), *_heads(grad_k, T, Hk, D, q.dtype, "grad_k"), *_heads(q, T, Hq, D, q.dtype, "q"), Hq,
+        *_heads(k, T, Hk, D, q.dtype, "k"), Hk, kind, gq, gk, gamma_kind, eps, C.byref(_rotation(positions, freq, axis, neighbours, T)), T, D,
+        *_heads(out_q, T, Hq, D, q.dtype, "out_q"), *_heads(out_k, T, Hk, D, q.dtype, "out_k"), *sums,
+        None if workspace is None else _here(workspace, torch.uint8, "workspace"), 0 if workspace is None else workspace.numel(), _stream()))
+    return (out_q, out_k, grad_gamma_q, grad_gamma_k) if norm else (out_q, out_k, None, None)
+
+
+def qnn_new_cache(pages: int, heads: int, page: int, D: int, device="cuda"):
+    """An empty paged cache: (codes of keys int8 [pages][heads][page][D], their scales float32 [pages][heads][page], codes of values, their scales), zeros."""
+    return tuple(torch.zeros((pages, heads, page) + ((D,) if i % 2 == 0 else ()), dtype=torch.int8 if i % 2 == 0 else torch.float32, device=device) for i in range(4))
+
+
+def _paged(cache, table: torch.Tensor, starts: torch.Tensor, lengths: torch.Tensor) -> _PagedCache:
+    k, k_scale, v, v_scale = cache
+    if k.dim() != 4 or not k.is_contiguous() or v.shape != k.shape or not v.is_contiguous():
+        raise ValueError("codes of the cache must be dense [pages][heads][page][D], keys and values alike")
+    for t, name in ((k_scale, "keys"), (v_scale, "values")):
+        if t.shape != k.shape[:3] or not t.is_contiguous():
+            raise ValueError(f"scales of the cache's {name} must be dense [pages][heads][page]")
+    sequences, width, ld = _rows_ld(table, "table")
+    _vector(lengths, sequences, "lengths"), _vector(starts, sequences + 1, "starts")
+    return _PagedCache(_here(k, torch.int8, "codes of keys"), _here(v, torch.int8, "codes of values"), _here(k_scale, torch.float32, "scales of keys"),
+                       _here(v_scale, torch.float32, "scales of values"), *k.shape, _here(table, torch.int32, "table"), ld, width,
+                       _here(starts, torch.int32, "starts"), _here(lengths, torch.int32, "lengths"), sequences)
+
+
+def qnn_cache_append(cache, table: torch.Tensor, starts: torch.Tensor, lengths: torch.Tensor, k: torch.Tensor, v: torch.Tensor, gamma_k: Optional[torch.Tensor],
+                     eps: float, positions: Optional[torch.Tensor], freq: Optional[torch.Tensor], axis: Optional[torch.Tensor] = None, neighbours: bool = False,
+                     q: Optional[torch.Tensor] = None, gamma_q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """Keys and values of new tokens into a paged cache (qnn_new_cache), keys normed and rotated as in qnn_qk_norm_rotate; with q its heads likewise, to q_out (which
+    may be q) -> q_out.  table: int32 [sequences][pages of a sequence]; starts: int32 [sequences + 1], where each sequence's new tokens begin among the call's;
+    lengths: int32 [sequences], all tokens of a sequence, the new ones among them."""
+    c = _paged(cache, table, starts, lengths)
+    T, Hk, D = _heads_shape(k, "k")
+    if (Hk, D) != (c.heads, c.D):
+        raise ValueError(f"k must have {c.heads} heads of {c.D}, got {Hk} of {D}")
+    kind = _float_type(k, "k")
+    gq, gk, gamma_kind = _gammas(gamma_q, gamma_k, D)
+    Hq, queries, results = 0, (None, 0, 0), (None, 0, 0)
+    if q is not None:
+        Hq = _heads_shape(q, "q")[1]
+        if q_out is None:
+            q_out = torch.empty((T, Hq, D), dtype=q.dtype, device=q.device)
+        queries, results = _heads(q, T, Hq, D, k.dtype, "q"), _heads(q_out, T, Hq, D, k.dtype, "q_out")
+    _check(_lib.qnn_cache_append(C.byref(c), *queries, Hq, *_heads(k, T, Hk, D, k.dtype, "k"), *_heads(v, T, Hk, D, k.dtype, "v"), kind, gq, gk, gamma_kind, eps,
+                                 C.byref(_rotation(positions, freq, axis, neighbours, T)), T, *results, _stream()))
+    return None if q is None else q_out
+
+
+def qnn_cache_attention_workspace_bytes(tokens: int, sequences: int, heads_q: int, heads: int, D: int, most_new: int, longest: int) -> int:
+    return int(_lib.qnn_cache_attention_workspace_bytes(tokens, sequences, heads_q, heads, D, most_new, longest))
+
+
+def qnn_cache_attention(q: torch.Tensor, cache, table: torch.Tensor, starts: torch.Tensor, lengths: torch.Tensor, scale: Optional[float] = None, cap: float = 0.0,
+                        slopes: Optional[torch.Tensor] = None, tree: Optional[torch.Tensor] = None, most_new: Optional[int] = None,
+                        longest: Optional[int] = None, out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of the new tokens' queries [tokens][heads][D] over a paged cache that has their keys and values already (cache, table, starts, lengths as in
+    qnn_cache_append).  scale: 1 / sqrt(D) if None; cap > 0: scores become cap * tanh(score / cap); slopes: float32 [heads], times the distance taken off a score;
+    tree: int64 [tokens], bit t of a token's mask: it sees new token t of its sequence (without one it sees all tokens up to itself).  most_new, longest: the most
+    new tokens of a sequence and the longest sequence, as far as the host knows; they set how the work is split, and any numbers are right."""
+    c = _paged(cache, table, starts, lengths)
+    T, Hq, D = _heads_shape(q, "q")
+    if D != c.D:
+        raise ValueError(f"q must have heads of {c.D}, got {D}")
+    kind = _float_type(q, "q")
+    if out is None:
+        out = torch.empty((T, Hq, D), dtype=q.dtype, device=q.device)
+    most_new = max(T, 1) if most_new is None else most_new
+    longest = max(c.width * c.page, 1) if longest is None else longest
+    if workspace is None:
+        need = qnn_cache_attention_workspace_bytes(T, c.sequences, Hq, c.heads, D, most_new, longest)
+        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=q.device)
+    _check(_lib.qnn_cache_attention(
+        C.byref(c), *_heads(q, T, Hq, D, q.dtype, "q"), Hq, kind, 1.0 / D ** 0.5 if scale is None else scale, cap,
+        None if slopes is None else _here(_vector(slopes, Hq, "slopes"), torch.float32, "slopes"),
+        None if tree is None else _here(_vector(tree, T, "tree"), torch.int64, "tree"), T, most_new, longest, *_heads(out, T, Hq, D, q.dtype, "out"),
+        _here(workspace, torch.uint8, "workspace"), workspace.numel(), _stream()))
+    return out
+
+
+def qnn_rows_quant(x: torch.Tensor, codes: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None):
+    """Codes int8 [rows][K] and scale float32 [rows] of the rows of x -> (codes, scale)."""
+    rows, K, ldx = _rows_ld(x, "x")
+    kind = _float_type(x, "x")
+    if codes is None:
+        codes = _new_codes(rows, K, x)
+    if scale is None:
+        scale = torch.empty(rows, dtype=torch.float32, device=x.device)
+    _check(_lib.qnn_rows_quant(_here(x, x.dtype, "x"), ldx, kind, rows, K, _here(codes, torch.int8, "codes"), _shaped(codes, rows, K, "codes"),
+                               _here(_vector(scale, rows, "scale"), torch.float32, "scale"), _stream()))
+    return codes, scale

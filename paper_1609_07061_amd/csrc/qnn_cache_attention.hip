@@ -1,0 +1,445 @@
+// Attention over the paged cache for few rows: a workgroup has 16 NB rows (queries of one sequence and the heads that share one of the cache), and its four waves
+// take 32 keys at a time in turn; the grid splits long sequences further.  A wave's products are S^T = K Q^T and O^T = V^T P^T (16 x 16 x 32, float16): of the
+// first result a lane has keys 4 g + 0 .. 3 of either 16 for query lane mod 16, which is the second's right operand as it is once the rows of V are taken in that
+// order; the sums over keys of a query are per lane until the end.  Codes go from memory to registers, 16 bytes of K a lane and D / 16 of V (whole rows a load), and
+// become float16 there; V's transposition is the choice of bytes in that step.
+#include "qnn_attention.h"
+
+namespace qnn {
+namespace attention {
+namespace {
+
+constexpr int kStep = 32, kWaves = 4;
+
+// Keys of a step, as a wave needs them: by the lane in memory order, in LDS
+struct __attribute__((aligned(16))) Keys {
+    uint32_t row[kStep];
+    float k_scale[kStep], v_scale[kStep];
+    float bias[kStep];   // 0, or -infinity for a key that is not there
+    float log_v[kStep];  // log2 of the values' scale, rounded up
+    int32_t place[kStep];
+};
+
+template <int DP>
+struct Codes {
+    static constexpr int kV = DP / 64;  // words of V a lane and key: DP / 16 codes
+    v4u k[2][DP / 64];
+    uint32_t v[8][kV];
+};
+
+template <int DP, int NB, int kParts, bool kMore>
+__global__ __launch_bounds__(64 * kWaves) void few_rows_kernel(const Args a) {
+    constexpr int kRows = 16 * NB, kPitch = DP + 4, kV = DP / 64;
+    __shared__ Keys keys[kWaves][2];
+    __shared__ float2 states[kWaves][kRows];
+    __shared__ __attribute__((aligned(16))) float sums[2][kRows][kPitch];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    uint32_t head, split, block, b;
+    {
+        const uint32_t id = rows::block_number();
+        uint32_t rest = quotient(id, a.pages.heads, a.heads_inverse, head);
+        rest = quotient(rest, (uint32_t)a.splits, a.splits_inverse, split);
+        b = quotient(rest, (uint32_t)a.blocks, a.blocks_inverse, block);
+    }
+    if ((int64_t)b >= a.sequences) return;  // (of the launch's last line)
+    const Sequence s = sequence_at(a, b);
+    const uint32_t n_rows = (uint32_t)s.fresh * (uint32_t)a.group;
+    for (uint32_t first = block * kRows; first < n_rows; first += (uint32_t)a.blocks * kRows) {
+        uint32_t in_group;
+        const uint32_t last = min(first + kRows, n_rows) - 1u;
+        const int32_t i0 = (int32_t)quotient(first, (uint32_t)a.group, a.group_inverse, in_group), i1 = (int32_t)quotient(last, (uint32_t)a.group, a.group_inverse, in_group);
+        // keys below `end` are looked at, those below `open` are seen by all rows
+        const int32_t end = min(a.tree ? s.n : max(s.base + i1 + 1, 0), s.in_table), open = a.tree ? s.base : s.base + i0 + 1;
+        const int64_t steps = (end + (int64_t)kStep - 1) / kStep;
+        const int32_t lo = (int32_t)(steps * split / a.splits), hi = (int32_t)(steps * (split + 1) / a.splits);
+
+        Query<DP, kParts> query[NB];
+        Sight sight[NB];
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
+            const Row row = row_at(a, s, min(first + 16u * n + r, last), head);
+            query[n].load(a, row);
+            sight[n].load(a, s, row);
+            if constexpr (!kMore) query[n].mult *= kLog2e;
+        }
+        v4f out[DP / 16][NB] = {};
+        float level[NB], total[NB];  // R; the sum of 2^(t - R) over this lane's keys
+#pragma unroll
+        for (int n = 0; n < NB; ++n) level[n] = -INFINITY, total[n] = 0.0f;
+
+        // ---- loads.  Of a step: the page numbers, then rows and scales, then codes
+        const int at = lane & 31;
+        struct Ahead {
+            uint32_t row;
+            float k_scale, v_scale;
+            int32_t place;
+        };
+        auto find = [&](int32_t step) __attribute__((always_inline)) -> uint32_t {
+            const int32_t key = step * kStep + at;
+            const uint32_t row = step < hi && key < end ? paged::row_of(a.pages, b, (uint32_t)key) : paged::kNoRow;
+            return row == paged::kNoRow ? row : row + head * a.pages.page;
+        };
+        auto scales = [&](int32_t step, uint32_t row, Ahead &x) __attribute__((always_inline)) {
+            x.row = row;
+            x.k_scale = row != paged::kNoRow ? a.k_scale[row] : 0.0f, x.v_scale = row != paged::kNoRow ? a.v_scale[row] : 0.0f;
+            x.place = step * kStep + at;
+            if (kMore && a.tree && x.place >= s.base && row != paged::kNoRow && x.place - s.base < s.fresh)
+                x.place = s.base - 1 + __popcll(a.tree[s.first + (x.place - s.base)]);
+        };
+        auto note = [&](const Ahead &x, Keys &k) __attribute__((always_inline)) {
+            const bool there = x.row != paged::kNoRow;
+            if (lane < kStep) {
+                k.row[at] = there ? x.row : 0u;
+                k.k_scale[at] = x.k_scale, k.v_scale[at] = x.v_scale;
+                k.bias[at] = there ? 0.0f : -INFINITY;
+                k.log_v[at] = x.v_scale != 0.0f ? fmaxf((float)__builtin_amdgcn_frexp_expf(x.v_scale), kLowest) : kLowest;
+                if constexpr (kMore) k.place[at] = x.place;
+            }
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        };
+        auto fetch = [&](const Keys &k, Codes<DP> &c) __attribute__((always_inline)) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int8_t *const from = a.k + (int64_t)k.row[16 * h + r] * a.D;
+#pragma unroll
+                for (int i = 0; i < DP / 64; ++i) {
+                    const int d = 64 * i + 16 * g;
+                    c.k[h][i] = *reinterpret_cast<const v4u *>(from + (d < a.D ? d : 0));  // (beyond the head the query is zero)
+                }
+            }
+            const int d = r * (DP / 16) < a.D ? r * (DP / 16) : 0;  // (beyond the head nothing is stored)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int8_t *const from = a.v + (int64_t)k.row[16 * (e >> 2) + 4 * g + (e & 3)] * a.D + d;
+                __builtin_memcpy(c.v[e], __builtin_assume_aligned(from, 4 * kV), 4 * kV);
+            }
+        };
+        auto use = [&](int32_t step, const Keys &k, const Codes<DP> &c) __attribute__((always_inline)) {
+            v4f dots[2][NB] = {};
+#pragma unroll
+            for (int i = 0; i < DP / 64; ++i)
+#pragma unroll
+                for (int f = 0; f < 2; ++f)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const h8 codes = eight_codes(c.k[h][i][2 * f], c.k[h][i][2 * f + 1]);
+#pragma unroll
+                        for (int n = 0; n < NB; ++n)
+#pragma unroll
+                            for (int p = 0; p < kParts; ++p)
+                                dots[h][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes, query[n].part[p][i][f], dots[h][n], 0, 0, 0);
+                    }
+            v4f k_scale[2], v_scale[2], bias[2], log_v[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int from = 16 * h + 4 * g;
+                k_scale[h] = *reinterpret_cast<const v4f *>(&k.k_scale[from]), v_scale[h] = *reinterpret_cast<const v4f *>(&k.v_scale[from]);
+                bias[h] = *reinterpret_cast<const v4f *>(&k.bias[from]), log_v[h] = *reinterpret_cast<const v4f *>(&k.log_v[from]);
+            }
+            const bool masked = (step + 1) * (int64_t)kStep > open;
+            h8 weights[NB][kParts];
+#pragma unroll
+            for (int n = 0; n < NB; ++n) {
+                float t[2][4], most = -INFINITY;
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        // (the scales first: a key that is not there has 0, and no product with it may overflow)
+                        float x = dots[h][n][e] * (query[n].mult * k_scale[h][e]);
+                        if constexpr (kMore) {
+                            if (a.cap > 0.0f) x = a.cap * tanh_of(x / a.cap);
+                            x *= kLog2e;
+                            if (a.slopes) x -= sight[n].slope * (float)(sight[n].place - k.place[16 * h + 4 * g + e]);
+                        }
+                        t[h][e] = x + bias[h][e];
+                    }
+                if (masked) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (!sight[n].sees(a, s, step * kStep + 16 * h + 4 * g + e)) t[h][e] = -INFINITY;
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) most = fmaxf(most, t[h][e] + log_v[h][e]);
+                most = fmaxf(most, __shfl_xor(most, 16));
+                most = fmaxf(most, __shfl_xor(most, 32));
+                const bool moves = most > level[n] + 15.0f;
+                if (__any(moves)) {
+                    const float now = moves ? most - 8.0f : level[n], factor = level[n] == now ? 1.0f : __builtin_amdgcn_exp2f(level[n] - now);
+                    level[n] = now;
+                    total[n] *= factor;
+#pragma unroll
+                    for (int d = 0; d < DP / 16; ++d) out[d][n] *= factor;
+                }
+                const float from = level[n] == -INFINITY ? 0.0f : level[n];
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float p = __builtin_amdgcn_exp2f(t[h][e] - from);
+                        total[n] += p;
+                        const float w = t[h][e] == -INFINITY ? 0.0f : p * v_scale[h][e];  // (a scale that is NaN is only for those who see it)
+                        const _Float16 hi = (_Float16)w;
+                        weights[n][0][4 * h + e] = hi;
+                        if constexpr (kParts == 2) weights[n][1][4 * h + e] = (_Float16)(w - (float)hi);
+                    }
+            }
+            // V: byte d mod 4 of word d / 4 of the eight keys' rows
+#pragma unroll
+            for (int x = 0; x < kV; ++x)
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    h2 codes[2][4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint32_t pair = __builtin_amdgcn_perm(c.v[2 * e + 1][x] ^ kBias, c.v[2 * e][x] ^ kBias, half ? 0x07030602u : 0x05010400u);
+                        codes[0][e] = halves(__builtin_amdgcn_perm(kExponents, pair, 0x04010400u));
+                        codes[1][e] = halves(__builtin_amdgcn_perm(kExponents, pair, 0x04030402u));
+                    }
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        const h8 operand = {codes[y][0][0], codes[y][0][1], codes[y][1][0], codes[y][1][1], codes[y][2][0], codes[y][2][1], codes[y][3][0], codes[y][3][1]};
+                        const int d = 4 * x + 2 * half + y;
+#pragma unroll
+                        for (int n = 0; n < NB; ++n)
+#pragma unroll
+                            for (int p = 0; p < kParts; ++p) out[d][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(operand, weights[n][p], out[d][n], 0, 0, 0);
+                    }
+                }
+        };
+
+        // ---- steps lo + wave, lo + wave + 4, ...: codes one step ahead, scales two, page numbers three
+        {
+            Codes<DP> even, odd;
+            Ahead ahead;
+            const int32_t step0 = lo + wave;
+            uint32_t row = find(step0);
+            scales(step0, row, ahead);
+            row = find(step0 + kWaves);
+            note(ahead, keys[wave][0]);
+            if (step0 < hi) fetch(keys[wave][0], even);
+            scales(step0 + kWaves, row, ahead);
+            row = find(step0 + 2 * kWaves);
+            for (int32_t step = step0; step < hi; step += 2 * kWaves) {
+                note(ahead, keys[wave][1]);
+                fetch(keys[wave][1], odd);
+                scales(step + 2 * kWaves, row, ahead);
+                row = find(step + 3 * kWaves);
+                use(step, keys[wave][0], even);
+                if (step + kWaves >= hi) break;
+                note(ahead, keys[wave][0]);
+                fetch(keys[wave][0], even);
+                scales(step + 3 * kWaves, row, ahead);
+                row = find(step + 4 * kWaves);
+                use(step + kWaves, keys[wave][1], odd);
+            }
+        }
+
+        // ---- the waves' sums
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
+            total[n] += __shfl_xor(total[n], 16);
+            total[n] += __shfl_xor(total[n], 32);
+            if (g == 0) states[wave][16 * n + r] = make_float2(level[n], total[n]);
+        }
+        __syncthreads();
+        auto most_of = [&](int row) __attribute__((always_inline)) {
+            float most = states[0][row].x;
+#pragma unroll
+            for (int w = 1; w < kWaves; ++w) most = fmaxf(most, states[w][row].x);
+            return most;
+        };
+        auto factor_of = [](float level, float most) __attribute__((always_inline)) { return level == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(level - most); };
+        auto put = [&](bool add) __attribute__((always_inline)) {
+#pragma unroll
+            for (int n = 0; n < NB; ++n) {
+                const float f = factor_of(level[n], most_of(16 * n + r));
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+#pragma unroll
+                    for (int d4 = 0; d4 < DP / 64; ++d4) {
+                        v4f *const to = reinterpret_cast<v4f *>(&sums[wave & 1][16 * n + r][(4 * g + e) * (DP / 16) + 4 * d4]);
+                        v4f x = {out[4 * d4][n][e] * f, out[4 * d4 + 1][n][e] * f, out[4 * d4 + 2][n][e] * f, out[4 * d4 + 3][n][e] * f};
+                        if (add) x += *to;
+                        *to = x;
+                    }
+            }
+        };
+        if (wave >= 2) put(false);
+        __syncthreads();
+        if (wave < 2) put(true);
+        __syncthreads();
+        for (uint32_t x = threadIdx.x; x < (uint32_t)(kRows * (DP / 8)); x += 64 * kWaves) {
+            const uint32_t row = x / (DP / 8), d = x % (DP / 8) * 8;
+            if (first + row > last || (int32_t)d >= a.D) continue;
+            const Row at_row = row_at(a, s, first + row, head);
+            const float most = most_of(row);
+            float sum = 0.0f, y[8];
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) sum += states[w][row].y * factor_of(states[w][row].x, most);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = sums[0][row][d + e] + sums[1][row][d + e];
+            if (a.splits == 1) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[e] = sum == 0.0f ? 0.0f : y[e] / sum;
+                store_values(a.out, at_row.token * a.ld_out + at_row.head * a.step_out + d, a.type, y);
+            } else {
+                const int64_t to = ((int64_t)split * a.tokens + at_row.token) * a.heads_q + at_row.head;
+                if (d == 0) a.state[to] = make_float2(most, sum);
+                if (!(sum == 0.0f)) {
+                    float *const p = a.part + to * a.D + d;
+                    __builtin_memcpy(p, y, sizeof y);
+                }
+            }
+        }
+        __syncthreads();  // (before the next rows)
+    }
+}
+
+// Parts of the keys joined: a workgroup for each query and head.  32 lanes (64 where a head is longer than 128) have a part's sums, 4 values a lane.
+constexpr int kMostSplits = 128;
+
+__global__ __launch_bounds__(256) void join_kernel(const Args a) {
+    __shared__ float factors[kMostSplits], totals[4], tops[4];
+    __shared__ v4f sums[8][64];
+    const int tid = threadIdx.x;
+    const int64_t id = rows::block_number(), rows_all = a.tokens * a.heads_q;
+    if (id >= rows_all) return;
+    const int64_t token = id / a.heads_q, head = id % a.heads_q;
+    if (token < a.starts[0] || token >= a.starts[a.sequences]) return;
+    float level = -INFINITY, total = 0.0f;
+    if (tid < a.splits) {
+        const float2 x = a.state[tid * rows_all + id];
+        level = x.x, total = x.y;
+    }
+    float top = level;
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    if ((tid & 63) == 0) tops[tid >> 6] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+    const float factor = level == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(level - top);
+    if (tid < a.splits) factors[tid] = total == 0.0f ? -1.0f : factor;  // (nothing there, and no sums written)
+    float sum = total * factor;
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) sum += __shfl_xor(sum, d);
+    if ((tid & 63) == 0) totals[tid >> 6] = sum;
+    __syncthreads();
+    sum = (totals[0] + totals[1]) + (totals[2] + totals[3]);
+    const int lanes = a.D > 128 ? 64 : 32, parts = 256 / lanes, part = tid / lanes, at = tid % lanes;
+    v4f y = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (4 * at < a.D)
+        for (int s = part; s < a.splits; s += parts)
+            if (!(factors[s] < 0.0f)) y += factors[s] * *reinterpret_cast<const v4f *>(a.part + (s * rows_all + id) * a.D + 4 * at);
+    sums[part][at] = y;
+    __syncthreads();
+    if (8 * tid < a.D) {
+        float z[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            float x = 0.0f;
+            for (int p = 0; p < parts; ++p) x += sums[p][2 * tid + e / 4][e % 4];
+            z[e] = sum == 0.0f ? 0.0f : x / sum;
+        }
+        store_values(a.out, token * a.ld_out + head * a.step_out + 8 * tid, a.type, z);
+    }
+}
+
+// How a call is split: blocks of rows for each sequence and head of the cache, and parts of the keys
+struct Plan {
+    int rows;
+    int64_t blocks, splits;
+};
+Plan plan_of(int64_t sequences, int64_t heads_q, int64_t heads, int64_t most_new, int64_t longest) {
+    Plan p;
+    const int64_t rows = most_new * (heads_q / heads);
+    p.rows = rows <= 16 ? 16 : 32;
+    p.blocks = ceil_div(rows, p.rows);
+    // two workgroups a compute unit, as long as a part has a step for every wave
+    const int64_t have = sequences * heads * p.blocks, want = ceil_div(2 * (int64_t)compute_units(), have), most = ceil_div(longest, kStep * kWaves);
+    p.splits = want < 1 ? 1 : (want < most ? want : most);
+    if (p.splits > kMostSplits) p.splits = kMostSplits;
+    return p;
+}
+bool plannable(int64_t tokens, int64_t sequences, int64_t heads_q, int64_t heads, int64_t D, int64_t most_new, int64_t longest) {
+    return tokens >= 1 && sequences >= 1 && heads >= 1 && heads_q >= 1 && heads_q % heads == 0 && heads_q <= 65535 && D >= 16 && D <= paged::kMostD && most_new >= 1 &&
+           longest >= 1;
+}
+// (numbers above what there can be do no more than these)
+int64_t at_most(int64_t x, int64_t limit) { return x < limit ? x : limit; }
+
+template <int DP, int kParts, bool kMore>
+int launch_few(const Args &a, const Plan &p, dim3 grid, hipStream_t s) {
+    if (p.rows == 16) return QNN_LAUNCH("cache_attention", (few_rows_kernel<DP, 1, kParts, kMore>), grid, dim3(64 * kWaves), 0, s, a);
+    return QNN_LAUNCH("cache_attention", (few_rows_kernel<DP, 2, kParts, kMore>), grid, dim3(64 * kWaves), 0, s, a);
+}
+template <int DP>
+int launch(const Args &a, const Plan &p, dim3 grid, hipStream_t s) {
+    const bool more = a.cap > 0.0f || a.slopes;
+    if (a.type == QNN_F32) return more ? launch_few<DP, 2, true>(a, p, grid, s) : launch_few<DP, 2, false>(a, p, grid, s);
+    return more ? launch_few<DP, 1, true>(a, p, grid, s) : launch_few<DP, 1, false>(a, p, grid, s);
+}
+
+}  // namespace
+}  // namespace attention
+}  // namespace qnn
+
+using namespace qnn;
+
+extern "C" size_t qnn_cache_attention_workspace_bytes(int64_t tokens, int64_t sequences, int64_t heads_q, int64_t heads, int64_t D, int64_t most_new,
+                                                      int64_t longest) {
+    if (!attention::plannable(tokens, sequences, heads_q, heads, D, most_new, longest)) return 0;
+    const attention::Plan p = attention::plan_of(sequences, heads_q, heads, attention::at_most(most_new, tokens), attention::at_most(longest, 0x7FFFFFFF));
+    return p.splits == 1 ? 0 : (size_t)p.splits * (size_t)tokens * (size_t)heads_q * ((size_t)D * 4 + 8);
+}
+
+extern "C" int qnn_cache_attention(const qnn_paged_cache *cache, const void *q, int64_t ld_q, int64_t step_q, int64_t heads_q, int type, float scale, float cap,
+                                   const float *slopes, const uint64_t *tree, int64_t tokens, int64_t most_new, int64_t longest, void *out, int64_t ld_out,
+                                   int64_t step_out, void *workspace, size_t workspace_bytes, void *stream) {
+    const char *const what = "cache_attention";
+    if (int rc = paged::check_cache(what, cache)) return rc;
+    const int64_t D = cache->D;
+    if (tokens < 0 || tokens > 0x7FFFFFFF || heads_q < 1 || heads_q > 65535 || heads_q % cache->heads || most_new < 1 || longest < 1)
+        return fail(QNN_ERR_SHAPE, "%s: %lld tokens, %lld heads on %lld of the cache, most_new = %lld, longest = %lld", what, (long long)tokens, (long long)heads_q,
+                    (long long)cache->heads, (long long)most_new, (long long)longest);
+    if (!rows::known_type(type)) return fail(QNN_ERR_SHAPE, "%s: type %d", what, type);
+    if (!(cap >= 0.0f) || cap > 3.0e38f || !(scale >= -3.0e38f && scale <= 3.0e38f)) return fail(QNN_ERR_SHAPE, "%s: scale = %g, cap = %g", what, (double)scale, (double)cap);
+    if (tokens == 0 || cache->sequences == 0) return QNN_OK;
+    if ((double)tokens * (double)(heads_q / cache->heads) > 2147483647.0) return fail(QNN_ERR_UNSUPPORTED, "%s: %lld tokens", what, (long long)tokens);
+    if (!paged::heads_fit(ld_q, step_q, heads_q, D, tokens) || !paged::heads_fit(ld_out, step_out, heads_q, D, tokens))
+        return fail(QNN_ERR_SHAPE, "%s: heads of %lld values at strides %lld, %lld or %lld, %lld overlap", what, (long long)D, (long long)ld_q, (long long)step_q,
+                    (long long)ld_out, (long long)step_out);
+    if (!q || !out) return fail(QNN_ERR_NULL, "%s: NULL pointer", what);
+    if (int rc = paged::check_cache_pointers(what, cache)) return rc;
+    const int w = rows::value_bytes(type);
+    if (!rows::aligned_to(q, w) || !rows::aligned_to(out, w) || !rows::aligned_to(slopes, 4) || !rows::aligned_to(tree, 8))
+        return fail(QNN_ERR_ALIGN, "%s: pointer not aligned to its type", what);
+    most_new = attention::at_most(most_new, tokens), longest = attention::at_most(longest, 0x7FFFFFFF);
+    const attention::Plan p = attention::plan_of(cache->sequences, heads_q, cache->heads, most_new, longest);
+    const size_t need = qnn_cache_attention_workspace_bytes(tokens, cache->sequences, heads_q, cache->heads, D, most_new, longest);
+    if (need > 0 && (!workspace || !rows::aligned_to(workspace, 256) || workspace_bytes < need))
+        return fail(QNN_ERR_WORKSPACE, "%s: workspace NULL, misaligned or smaller than %zu bytes", what, need);
+    const double blocks = (double)cache->sequences * (double)cache->heads * (double)p.blocks * (double)p.splits;
+    if (blocks > 1073741823.0 || (double)tokens * (double)heads_q > 2147483647.0) return fail(QNN_ERR_UNSUPPORTED, "%s: %.0f workgroups", what, blocks);
+    const int64_t queries = tokens * heads_q;
+    float *const part = static_cast<float *>(workspace);
+    attention::Args a = {};
+    a.q = q, a.out = out, a.ld_q = ld_q, a.step_q = step_q, a.ld_out = ld_out, a.step_out = step_out;
+    a.k = cache->k, a.v = cache->v, a.k_scale = cache->k_scale, a.v_scale = cache->v_scale;
+    a.pages = paged::pages_of(*cache), a.starts = cache->starts, a.lengths = cache->lengths, a.slopes = slopes, a.tree = tree, a.scale = scale, a.cap = cap;
+    a.tokens = tokens, a.sequences = cache->sequences, a.type = type, a.D = (int32_t)D, a.heads_q = (int32_t)heads_q;
+    a.group = (int32_t)(heads_q / cache->heads), a.splits = (int32_t)p.splits, a.blocks = (int32_t)p.blocks;
+    a.group_inverse = inverse_of(a.group), a.heads_inverse = inverse_of(cache->heads), a.splits_inverse = inverse_of(p.splits), a.blocks_inverse = inverse_of(p.blocks);
+    a.part = part, a.state = reinterpret_cast<float2 *>(part + p.splits * queries * D);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const dim3 grid = rows::grid_of((int64_t)blocks);
+    const int rc = D <= 64 ? attention::launch<64>(a, p, grid, s) : (D <= 128 ? attention::launch<128>(a, p, grid, s) : attention::launch<256>(a, p, grid, s));
+    if (rc || p.splits == 1) return rc;
+    return QNN_LAUNCH(what, attention::join_kernel, rows::grid_of(queries), dim3(256), 0, s, a);
+}

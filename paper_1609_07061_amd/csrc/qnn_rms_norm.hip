@@ -15,15 +15,6 @@ namespace {
 
 using namespace rows;
 
-// r of a row of K whose squares add up to `total`.  NaN for a row whose sum is beyond fp32 (1 / sqrt would be 0: a row of zeros, and a gradient of zeros) or that
-// has a value that is not finite.  Infinite where mean and eps together are below the normal numbers, whose squares have lost their digits: such a row counts as
-// not finite too, unless it holds nothing but zeros.  (Sums in units of a power of two would hold both; in the gradient they take a fourth of the waves.)
-__device__ __forceinline__ float norm_factor(float total, int64_t K, float eps) {
-    const float mean = total / (float)K + eps;
-    if (mean < 0x1p-126f) return __uint_as_float(0x7F800000u);
-    return magnitude(mean) < 0x7F800000u ? 1.0f / sqrtf(mean) : __uint_as_float(0x7FC00000u);
-}
-
 template <typename T, bool kOnce>
 struct NormSource {
     struct Kept {
@@ -178,29 +169,6 @@ __global__ __launch_bounds__(kThreads *groups_of(kThreads)) void rms_norm_backwa
     }
 }
 
-// ggamma[k] = sum of n_parts rows of `parts`: 32 columns a workgroup, 32 lanes a column, eight loads of each under way
-__global__ __launch_bounds__(1024) void add_parts_kernel(const float *parts, int n_parts, int64_t K, float *out) {
-    __shared__ float sums[32][33];
-    const int c = threadIdx.x & 31, g = threadIdx.x >> 5;
-    const int64_t k = (int64_t)blockIdx.x * 32 + c;
-    float s = 0.0f;
-    if (k < K)
-        for (int p0 = g; p0 < n_parts; p0 += 256) {
-            float v[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = p0 + 32 * j < n_parts ? parts[(int64_t)(p0 + 32 * j) * K + k] : 0.0f;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) s += v[j];
-        }
-    sums[g][c] = s;
-    __syncthreads();
-    float t = sums[c][g];  // column g, part c
-#pragma unroll
-    for (int d = 16; d >= 1; d >>= 1) t += __shfl_xor(t, d);
-    const int64_t to = (int64_t)blockIdx.x * 32 + g;
-    if (c == 0 && to < K) out[to] = t;
-}
-
 constexpr int64_t kWidest = 2048 * kVec;  // of the gradient, whose rows stay in registers
 int64_t parts_of(int64_t rows) { return rows < kParts ? rows : kParts; }
 
@@ -210,7 +178,8 @@ int launch_backward(const NormGradArgs<T> &a, float *grad_gamma, hipStream_t s) 
     const bool once = beyond_caches((a.grad_sum ? 4.0 : 3.0) * sizeof(T) * (double)a.n_rows * (double)a.K);
     auto kernel = once ? rms_norm_backward_kernel<T, kThreads, kPer, !kShort, kShort> : rms_norm_backward_kernel<T, kThreads, kPer, false, kShort>;
     if (int rc = QNN_LAUNCH("rms_norm_backward", kernel, dim3((unsigned)parts), dim3(kThreads * groups_of(kThreads)), 0, s, a)) return rc;
-    return QNN_LAUNCH("rms_norm_backward", add_parts_kernel, dim3((unsigned)ceil_div(a.K, 32)), dim3(1024), 0, s, a.parts, (int)parts, a.K, grad_gamma);
+    const AddParts all = {a.parts, (int32_t)parts, grad_gamma};
+    return QNN_LAUNCH("rms_norm_backward", add_parts_kernel, dim3((unsigned)ceil_div(a.K, 32)), dim3(1024), 0, s, all, all, a.K);
 }
 
 }  // namespace

@@ -171,6 +171,47 @@ constexpr int64_t kLine = 1 << 21;
 inline dim3 grid_of(int64_t blocks) { return blocks <= kLine ? dim3((unsigned)blocks) : dim3((unsigned)kLine, (unsigned)ceil_div(blocks, kLine)); }
 __device__ __forceinline__ uint32_t block_number() { return blockIdx.y * (uint32_t)kLine + blockIdx.x; }
 
+// r of a row of K whose squares add up to `total`.  NaN for a row whose sum is beyond fp32 (1 / sqrt would be 0: a row of zeros, and a gradient of zeros) or that
+// has a value that is not finite.  Infinite where mean and eps together are below the normal numbers, whose squares have lost their digits: such a row counts as
+// not finite too, unless it holds nothing but zeros.  (Sums in units of a power of two would hold both; in the gradient they take a fourth of the waves.)
+__device__ __forceinline__ float norm_factor(float total, int64_t K, float eps) {
+    const float mean = total / (float)K + eps;
+    if (mean < 0x1p-126f) return __uint_as_float(0x7F800000u);
+    return magnitude(mean) < 0x7F800000u ? 1.0f / sqrtf(mean) : __uint_as_float(0x7FC00000u);
+}
+
+// out[k] = sum of n_parts rows of `parts`, of one such sum or, with two lines of workgroups, of two: 32 columns a workgroup, 32 lanes a column, eight loads of each
+// under way
+struct AddParts {
+    const float *parts;
+    int32_t n_parts;
+    float *out;
+};
+static __global__ __launch_bounds__(1024) void add_parts_kernel(const AddParts one, const AddParts two, int64_t K) {
+    const float *const parts = blockIdx.y ? two.parts : one.parts;
+    float *const out = blockIdx.y ? two.out : one.out;
+    const int n_parts = blockIdx.y ? two.n_parts : one.n_parts;
+    __shared__ float sums[32][33];
+    const int c = threadIdx.x & 31, g = threadIdx.x >> 5;
+    const int64_t k = (int64_t)blockIdx.x * 32 + c;
+    float s = 0.0f;
+    if (k < K)
+        for (int p0 = g; p0 < n_parts; p0 += 256) {
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = p0 + 32 * j < n_parts ? parts[(int64_t)(p0 + 32 * j) * K + k] : 0.0f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s += v[j];
+        }
+    sums[g][c] = s;
+    __syncthreads();
+    float t = sums[c][g];  // column g, part c
+#pragma unroll
+    for (int d = 16; d >= 1; d >>= 1) t += __shfl_xor(t, d);
+    const int64_t to = (int64_t)blockIdx.x * 32 + g;
+    if (c == 0 && to < K) out[to] = t;
+}
+
 constexpr int rows_per_block(int threads) { return threads >= 256 ? 1 : 256 / threads; }
 
 // One row per kThreads lanes.  Source: `load<kShort>(row, window, K, values, kept)` the values to be quantized, up to the factor `factor(sum)`;

@@ -1,0 +1,130 @@
+"""Keys and values into a paged cache against the definition in 64 bits."""
+import math
+
+import pytest
+import torch
+
+from attention_testlib import Paged, Rotation, heads_of, norm_rotate, strided, untouched
+from int8_testlib import TYPES, U, assert_near, assert_quantized, generator, normal
+
+pytestmark = pytest.mark.gpu
+EPS = 1e-6
+# lengths, new tokens, heads of queries, heads of the cache, D, page, before, behind
+CASES = [([1], [1], 0, 1, 16, 1, 0, 0), ([5, 0, 200, 33], [1, 0, 1, 1], 8, 2, 64, 16, 0, 0), ([70, 19, 300], [70, 3, 65], 4, 4, 128, 20, 2, 3),
+          ([17], [40], 2, 1, 80, 7, 0, 0), ([5000], [4999], 3, 1, 32, 64, 1, 0), ([9] * 130, [1] * 130, 5, 1, 256, 16, 0, 5), ([40, 3], [40, 3], 10, 5, 112, 128, 0, 0)]
+
+
+def _expect(p, rows, values, error):
+    """Checks the cache's rows of every new token against `values` and everything else against `before`."""
+    codes, scale = p.cache[2 * rows], p.cache[2 * rows + 1]
+    for b, (n, m) in enumerate(zip(p.n, p.fresh)):
+        page, off, there = p.places(b)
+        for i in range(m):
+            at = n - m + i
+            if at < 0 or not there[at]:
+                continue
+            y = values[p.first[b] + i]
+            top = y.abs().amax(dim=1)
+            wrong = error[p.first[b] + i]
+            relative = (wrong.amax(dim=1) / top).max().item() if rows == 0 else 0.0
+            assert_quantized(codes[page[at], :, off[at]], scale[page[at], :, off[at]], y, relative + 4 * U)
+
+
+def _written(p):
+    """Which rows of the cache the call writes."""
+    mark = torch.zeros(p.cache[1].shape, dtype=torch.bool, device="cuda")
+    for b, (n, m) in enumerate(zip(p.n, p.fresh)):
+        page, off, there = p.places(b)
+        new = torch.arange(n, device="cuda") >= n - m
+        mark[page[new & there], :, off[new & there]] = True
+    return mark
+
+
+@pytest.mark.parametrize("case", CASES)
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("norm", [True, False])
+def test_append(seed, case, dtype, norm):
+    import paper_1609_07061_amd as q
+
+    lengths, fresh, Hq, Hk, D, page, before, behind = case
+    p = Paged(seed, lengths, fresh, Hk, D, page, before=before, behind=behind)
+    T = p.tokens
+    rotation = Rotation(seed, T, D, D // 32 * 8 if D % 32 == 0 else D // 2)
+    x, k, v = (heads_of(seed + i, T, H, D, dtype) for i, H in enumerate((Hq, Hk, Hk)))
+    g = generator(seed, 9)
+    gq, gk = ((1 + 0.3 * normal(g, D)).to(dtype) if norm else None for _ in range(2))
+    old = [t.clone() for t in p.cache]
+    whole, out = strided(torch.full_like(x, 5.0), fill=7.0)
+    got = q.qnn_cache_append(*p.args, strided(k)[1], strided(v)[1], gk, EPS, *rotation.args, *((strided(x)[1], gq, out) if Hq else ()))
+    _expect(p, 0, *norm_rotate(k, gk, EPS, rotation))
+    _expect(p, 1, v.double(), torch.zeros_like(v, dtype=torch.float64))
+    mark = _written(p)
+    for t, o in zip(p.cache, old):
+        assert torch.equal(t[~mark], o[~mark])
+    if Hq:
+        assert got is out
+        inside = slice(p.first[0], p.first[-1])
+        want, error = norm_rotate(x, gq, EPS, rotation)
+        assert_near(out[inside], want[inside], error[inside])
+        assert (out[:before] == 5).all() and (out[p.first[-1]:] == 5).all() and untouched(whole, out, 7.0)
+    else:
+        assert got is None
+
+
+def test_codes_and_scales_are_the_rows(seed):
+    """Values: as qnn_rows_quant of the same rows; a row that is not finite has scale NaN and codes 0, one of zeros scale 0."""
+    import paper_1609_07061_amd as q
+
+    p = Paged(seed, [50], [50], 3, 64, 16)
+    k, v = heads_of(seed, 50, 3, 64, torch.bfloat16), heads_of(seed + 1, 50, 3, 64, torch.bfloat16)
+    v[3, 1, 7], v[4, 2, 0], v[5, 0] = math.nan, -math.inf, 0.0
+    k[6, 2, 9] = math.nan
+    rotation = Rotation(seed, 50, 64)
+    q.qnn_cache_append(*p.args, k, v, None, EPS, *rotation.args)
+    page, off, _ = p.places(0)
+    codes, scale = q.qnn_rows_quant(v.reshape(150, 64))
+    assert torch.equal(p.cache[2][page, :, off].reshape(150, 64), codes)
+    assert torch.equal(p.cache[3][page, :, off].reshape(150).nan_to_num(-1.0), scale.nan_to_num(-1.0))
+    assert torch.isnan(p.cache[1][page[6], 2, off[6]]) and (p.cache[0][page[6], 2, off[6]] == 0).all()
+    assert int(torch.isnan(p.cache[1]).sum()) == 1
+
+
+def test_pages_that_are_none(seed):
+    """Numbers outside the cache and tokens beyond the table name no page: nothing is written for them."""
+    import paper_1609_07061_amd as q
+
+    p = Paged(seed, [100, 40], [100, 40], 2, 32, 16)
+    p.table[0, 1], p.table[0, 3], p.table[1, 0] = -1, p.cache[0].shape[0], 2 ** 31 - 1
+    p.table = p.table[:, :5].clone()  # (the first sequence needs 7)
+    old = [t.clone() for t in p.cache]
+    x, k, v = (heads_of(seed + i, 140, 2, 32, torch.float16) for i in range(3))
+    rotation = Rotation(seed, 140, 32)
+    out = q.qnn_cache_append(*p.args, k, v, None, EPS, *rotation.args, x)
+    _expect(p, 0, *norm_rotate(k, None, EPS, rotation))
+    mark = _written(p)
+    assert int(mark.sum()) == 2 * (3 * 16 + 24)
+    for t, o in zip(p.cache, old):
+        assert torch.equal(t[~mark], o[~mark])
+    assert_near(out, *norm_rotate(x, None, EPS, rotation))
+
+
+def test_offsets_beyond_32_bits(seed):
+    """A cache of more than 4 GiB of keys: pages at its end."""
+    import paper_1609_07061_amd as q
+
+    D, page, pages = 256, 128, 140000
+    codes = torch.zeros(pages, 1, page, D, dtype=torch.int8, device="cuda")  # 4.6e9 bytes
+    scale = torch.zeros(pages, 1, page, device="cuda")
+    cache = (codes, scale, codes.clone(), scale.clone())
+    ints = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")
+    k, v = heads_of(seed, 130, 1, D, torch.bfloat16), heads_of(seed + 1, 130, 1, D, torch.bfloat16)
+    rotation = Rotation(seed, 130, D)
+    q.qnn_cache_append(cache, ints(pages - 1, pages - 2)[None], ints(0, 130), ints(130), k, v, None, EPS, *rotation.args)
+    want, error = norm_rotate(k, None, EPS, rotation)
+    got = torch.cat([codes[-1, 0], codes[-2, 0, :2]])
+    assert_quantized(got, torch.cat([scale[-1, 0], scale[-2, 0, :2]]), want[:, 0], (error[:, 0] / want.abs().amax(dim=2)).max().item() + 4 * U)
+    assert not codes[:-2].any() and not scale[:-2].any() and not codes[-2, 0, 2:].any()
+    x = heads_of(seed + 2, 130, 2, D, torch.bfloat16)
+    out = q.qnn_cache_attention(x, cache, ints(pages - 1, pages - 2)[None], ints(0, 130), ints(130))
+    small = [torch.stack([t[-1], t[-2]]) for t in cache]
+    assert torch.equal(out, q.qnn_cache_attention(x, small, ints(0, 1)[None], ints(0, 130), ints(130)))

@@ -1,0 +1,224 @@
+"""Attention over a paged cache against the definition in 64 bits."""
+import math
+import random
+
+import pytest
+import torch
+
+from attention_testlib import Paged, attention, heads_of, strided, untouched
+from int8_testlib import TYPES, assert_near, generator, normal
+
+pytestmark = pytest.mark.gpu
+# lengths, new tokens, heads of queries, heads of the cache, D, page
+CASES = [([1], [1], 1, 1, 16, 16), ([33], [1], 8, 1, 64, 16), ([5, 0, 700, 128, 1], [1, 0, 1, 1, 1], 8, 2, 128, 16), ([2049], [1], 4, 4, 256, 64), ([300, 77], [1, 1], 5, 1, 80, 20),
+         ([31, 32, 64, 65], [31, 32, 1, 65], 6, 3, 64, 7), ([1000], [100], 4, 2, 128, 32), ([130, 9], [17, 9], 20, 2, 112, 16), ([70], [70], 3, 3, 240, 128),
+         ([5000, 200], [2, 1], 16, 2, 128, 1), ([600], [600], 8, 1, 64, 64)]
+EACH = [("f16", "plain"), ("bf16", "plain"), ("f32", "plain"), ("bf16", "cap"), ("f32", "cap"), ("f16", "slopes"), ("f32", "both"), ("bf16", "both")]
+NAMES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+
+
+def _options(kind, H):
+    return dict(cap=7.0 if kind in ("cap", "both") else 0.0,
+                slopes=2.0 ** (-8.0 * torch.arange(1, H + 1, device="cuda", dtype=torch.float32) / H) if kind in ("slopes", "both") else None)
+
+
+def _tree(seed, p):
+    """Masks of drafted tokens: a token and those it follows; some see nothing, some another's branch, one bits beyond the sequence's tokens."""
+    rng, out = random.Random(seed), [0] * p.first[0]
+    for m in p.fresh:
+        masks = []
+        for i in range(m):
+            parent = rng.randint(-1, i - 1)
+            masks.append((masks[parent] if parent >= 0 else 0) | (1 << i if i < 64 else 0))
+        for i in range(m):
+            if rng.random() < 0.1:
+                masks[i] = rng.choice([0, rng.getrandbits(64), 1 << 63])
+        out += masks
+    out += [0] * (p.tokens - len(out))
+    return torch.tensor([x - (1 << 64) if x >> 63 else x for x in out], dtype=torch.int64, device="cuda")
+
+
+def _near(got, want, error, written):
+    assert_near(got[written], want[written], error[written])
+
+
+@pytest.mark.parametrize("case", CASES)
+@pytest.mark.parametrize("type,kind", EACH)
+@pytest.mark.parametrize("with_tree", [False, True])
+def test_attention(seed, case, type, kind, with_tree):
+    import paper_1609_07061_amd as q
+
+    lengths, fresh, H, heads, D, page = case
+    p = Paged(seed, lengths, fresh, heads, D, page, before=1, behind=2)
+    x = heads_of(seed, p.tokens, H, D, NAMES[type], 2.0)
+    options = _options(kind, H)
+    if with_tree:
+        options["tree"] = _tree(seed, p)
+    whole, out = strided(torch.full_like(x, 3.0), fill=9.0)
+    got = q.qnn_cache_attention(strided(x)[1], *p.args, None, **options, out=out)
+    want, error, written = attention(p, x, D ** -0.5, **options)
+    assert got is out
+    _near(out, want, error, written)
+    assert (out[~written] == 3).all() and untouched(whole, out, 9.0)
+    # however the work is split
+    for most_new, longest in ((1, 1), (max(fresh), max(lengths)), (1 << 40, 1 << 40)):
+        again = q.qnn_cache_attention(x, *p.args, None, **options, most_new=most_new, longest=longest)
+        _near(again, want, error, written)
+        assert torch.equal(again[written], q.qnn_cache_attention(x, *p.args, None, **options, most_new=most_new, longest=longest)[written])
+
+
+@pytest.mark.parametrize("type", ["f32", "bf16"])
+@pytest.mark.parametrize("lengths,fresh,H,heads,D,page", [([20000], [1], 8, 2, 128, 16), ([9000, 3, 4000], [1, 1, 1], 2, 1, 256, 64), ([3000, 2500], [64, 40], 8, 2, 64, 16),
+                                                          ([5000], [700], 8, 2, 128, 64)])
+def test_long(seed, lengths, fresh, H, heads, D, page, type):
+    import paper_1609_07061_amd as q
+
+    p = Paged(seed, lengths, fresh, heads, D, page)
+    x = heads_of(seed, p.tokens, H, D, NAMES[type], 2.0)
+    got = q.qnn_cache_attention(x, *p.args, 0.1, most_new=max(fresh), longest=max(lengths))
+    _near(got, *attention(p, x, 0.1))
+
+
+@pytest.mark.parametrize("type", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("fresh", [1, 40, 200])
+def test_what_is_not_seen_does_not_matter(seed, fresh, type):
+    """Scales that are NaN or infinite at later tokens, behind the sequence's end, on other pages and in pages that are none; and what a query that sees one gets."""
+    import paper_1609_07061_amd as q
+
+    p = Paged(seed, [500, 90], [fresh, 1], 2, 64, 32)
+    x = heads_of(seed, p.tokens, 4, 64, NAMES[type])
+    want = q.qnn_cache_attention(x, *p.args)
+    mark = torch.zeros(p.cache[1].shape, dtype=torch.bool, device="cuda")
+    for b in range(2):
+        page, off, _ = p.places(b)
+        mark[page, :, off] = True
+    for i, bad in ((1, math.nan), (3, math.inf)):
+        p.cache[i][~mark] = bad
+    assert torch.equal(q.qnn_cache_attention(x, *p.args), want)
+    # the last token of the first sequence: seen by its own query alone
+    page, off, _ = p.places(0)
+    for i in (1, 3):
+        kept = p.cache[i][page[-1], 1, off[-1]].clone()
+        p.cache[i][page[-1], 1, off[-1]] = math.nan
+        got = q.qnn_cache_attention(x, *p.args)
+        assert torch.isnan(got[fresh - 1, 2:]).all()
+        got[fresh - 1, 2:] = want[fresh - 1, 2:]
+        assert torch.equal(got, want)
+        p.cache[i][page[-1], 1, off[-1]] = kept
+    # a query that is not finite
+    y = x.clone()
+    y[0, 0, 3], y[0, 3, 63] = math.inf, math.nan
+    got = q.qnn_cache_attention(y, *p.args)
+    assert torch.isnan(got[0, 0]).all() and torch.isnan(got[0, 3]).all()
+    got[0, 0], got[0, 3] = want[0, 0], want[0, 3]
+    assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("fresh", [1, 30, 300])
+def test_pages_that_are_none(seed, fresh):
+    """Tokens whose page is outside the cache or beyond the table are not seen; a query left with nothing gets zeros."""
+    import paper_1609_07061_amd as q
+
+    p = Paged(seed, [400, 60, 20], [fresh, 1, 20], 2, 64, 16)
+    p.table[0, 3], p.table[0, 11], p.table[1] = -1, p.cache[0].shape[0], 2 ** 31 - 1
+    p.table[2, 0] = -7
+    p.table = p.table[:, :20].clone()
+    x = heads_of(seed, p.tokens, 4, 64, torch.bfloat16)
+    got = q.qnn_cache_attention(x, *p.args)
+    want, error, written = attention(p, x, 0.125)
+    _near(got, want, error, written)
+    assert (got[fresh] == 0).all() and (got[fresh + 1:fresh + 17] == 0).all()
+
+
+def test_lengths_that_do_not_fit(seed):
+    """Fewer tokens than new ones: the first of these have no place and see nothing.  No sequences, no tokens, an empty table."""
+    import paper_1609_07061_amd as q
+
+    p = Paged(seed, [6, 0], [10, 3], 1, 32, 4)
+    x = heads_of(seed, 13, 2, 32, torch.float32)
+    got = q.qnn_cache_attention(x, *p.args)
+    assert (got[:4] == 0).all() and (got[10:] == 0).all()
+    _near(got, *attention(p, x, 32 ** -0.5))
+    out = torch.full_like(x, 4.0)
+    q.qnn_cache_attention(x, p.cache, p.table[:0], p.starts[:1], p.lengths[:0], out=out)
+    assert (out == 4).all()
+    assert (q.qnn_cache_attention(x, p.cache, p.table[:, :0], p.starts, p.lengths) == 0).all()
+    assert q.qnn_cache_attention(x[:0], *p.args).shape == (0, 2, 32)
+
+
+@pytest.mark.parametrize("type", ["f32", "f16", "bf16"])
+def test_values_of_all_sizes(seed, type):
+    """Scores that the softmax tells apart by thousands, scales of values from 1e-30 to 1e4, heads of zeros, tiny and large queries."""
+    import paper_1609_07061_amd as q
+
+    p = Paged(seed, [900] * 6, [1] * 6, 1, 64, 16)
+    g = generator(seed, 3)
+    p.cache[3].copy_(10.0 ** (torch.rand(p.cache[3].shape, generator=g, device="cuda") * 34 - 30))
+    p.cache[3][:, :, ::5] = 0
+    x = heads_of(seed, 6, 2, 64, NAMES[type])
+    x[0] *= 100
+    x[1] *= 1e-3
+    x[2] = 0
+    x[3, :, ::2] *= 1e-4
+    if type != "f16":
+        x[4] *= 1e-30
+        x[5] *= 1e4
+    got = q.qnn_cache_attention(x, *p.args)
+    _near(got, *attention(p, x, 0.125))
+
+
+def test_nothing_but_zeros_in_the_cache(seed):
+    import paper_1609_07061_amd as q
+
+    cache = q.qnn_new_cache(4, 2, 16, 64)
+    ints = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")
+    x = heads_of(seed, 3, 4, 64, torch.bfloat16)
+    out = q.qnn_cache_attention(x, cache, ints([[0, 1, 2]]), ints([0, 3]), ints([40]))
+    assert (out == 0).all()
+
+
+def test_scores_and_their_cap(seed):
+    """Small scores keep their digits through the cap, large ones end at it."""
+    import paper_1609_07061_amd as q
+
+    p = Paged(seed, [300], [1], 1, 64, 16)
+    for factor in (1e-4, 1e-2, 0.3, 1.0, 30.0):
+        x = heads_of(seed, 1, 1, 64, torch.float32, factor)
+        for cap in (0.5, 30.0):
+            _near(q.qnn_cache_attention(x, *p.args, 0.2, cap), *attention(p, x, 0.2, cap))
+
+
+def test_graphs_and_streams(seed):
+    """One graph for all steps: lengths, tables and tokens change between replays; two graphs share a workspace; a stream of its own."""
+    import paper_1609_07061_amd as q
+
+    p = Paged(seed, [700, 300, 1], [1, 1, 1], 2, 64, 16)
+    x = heads_of(seed, 3, 8, 64, torch.bfloat16)
+    most, longest = 1, 700
+    ws = torch.empty(q.qnn_cache_attention_workspace_bytes(3, 3, 8, 2, 64, most, longest), dtype=torch.uint8, device="cuda")
+    assert ws.numel() > 0
+    outs = [torch.empty_like(x), torch.empty_like(x)]
+    scales = (0.125, 0.3)
+    call = lambda i, out: q.qnn_cache_attention(x, *p.args, scales[i], most_new=most, longest=longest, out=out, workspace=ws)
+    call(0, outs[0])
+    torch.cuda.synchronize()
+    graphs = []
+    for i in range(2):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[i]):
+            call(i, outs[i])
+    for lengths in ([700, 300, 1], [5, 700, 64], [0, 33, 699], [1, 1, 1]):
+        p.lengths.copy_(torch.tensor(lengths, dtype=torch.int32))
+        x.copy_(heads_of(seed + lengths[0], 3, 8, 64, torch.bfloat16))
+        want = [call(i, torch.empty_like(x)).clone() for i in range(2)]
+        torch.cuda.synchronize()
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        again = call(1, torch.empty_like(x))
+    side.synchronize()
+    assert torch.equal(again, want[1])
