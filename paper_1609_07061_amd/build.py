@@ -17,7 +17,7 @@ SOURCES = ["qnn_api.hip", "qnn_probe.hip", "qnn_pack.hip", "qnn_quant.hip", "qnn
            "qnn_gemm_mfma_k1.hip", "qnn_gemm_mfma_k2.hip", "qnn_gemm_mfma_k3.hip", "qnn_gemm_mfma_k4.hip", "qnn_gemm_stage_k0.hip",
            "qnn_gemm_stage_k1.hip", "qnn_gemm_stage_k2.hip", "qnn_gemm_panel_k0.hip", "qnn_gemm_bytes_panel_k0.hip",
            "qnn_gemm_mixed.hip", "qnn_gemm_codes.hip", "qnn_gemm_image.hip", "qnn_rms_norm.hip", "qnn_silu_gate.hip", "qnn_int8_gemm.hip", "qnn_int8_moe.hip",
-           "qnn_heads.hip", "qnn_cache_attention.hip", "qnn_rows_quant.hip"]
+           "qnn_heads.hip", "qnn_cache_attention.hip", "qnn_cache_attention_many.hip", "qnn_rows_quant.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc", "-ffp-contract=off",

@@ -3,8 +3,9 @@
 // Of a query q (a row of D floats) and the keys it sees, code rows c_j with scales a_j and value codes v_j with scales b_j:
 //   s_j = scale a_j (q . c_j), capped and biased as asked;   out = sum_j 2^(t_j - R) b_j v_j / sum_j 2^(t_j - R),   t_j = s_j log2(e).
 // One pass over the keys.  Both products are matrix instructions on float16 operands with sums in fp32: a code is exact in float16; q is brought to 2^13 .. 2^14 by a
-// power of two, so that values 2^-28 of its largest still have all of their digits; the weight w_j = 2^(t_j - R) b_j is what meets the value codes.  fp32 queries
-// and their weights are held in two parts, 22 digits; of 16-bit ones the weight's rounding is 2^-12, an eighth of the bf16 result's.
+// power of two, so that values 2^-28 of its largest still have all of their digits; the weight w_j = 2^(t_j - R) b_j is what meets the value codes.  Of bf16 results
+// an eighth of their own rounding is the weights' (half a step is 2^-11 of a weight, 2^-8 of a result); for fp16 and fp32 results weights are held in two parts, 22
+// digits, and so are fp32 queries.
 // R follows the largest of t_j + log2(b_j) seen, so that w_j is at most 2^15 and the largest about 2^8: small weights keep their digits down to 2^-22 of it, however
 // the scales b_j differ.  It moves only when a weight would pass 2^15: the sums are multiplied by a power then, and nothing else.  Sums that belong to different R
 // (of waves, of parts of the keys) are joined in a fixed order.
@@ -26,6 +27,16 @@ typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 constexpr float kLog2e = 1.44269504f;
 constexpr float kLowest = -100.0f;  // log2 of the least scale of values that R follows (zeros have none)
 
+// A lane's number that the compiler cannot see through: what follows from it is worked out where it is needed.  (Worked out once before the loops, addresses take
+// some 100 registers, and the sums are spilled.)
+__device__ __forceinline__ int opaque(int x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
+// log2 of a scale of values, rounded up, for R to follow
+__device__ __forceinline__ float log_scale(float v) { return v != 0.0f ? fmaxf((float)__builtin_amdgcn_frexp_expf(v), kLowest) : kLowest; }
+
 struct Args {
     const void *q;
     void *out;
@@ -38,7 +49,7 @@ struct Args {
     const uint64_t *tree;
     float scale, cap;
     int64_t tokens, sequences;
-    int32_t type, D, heads_q, group, splits, blocks;  // blocks: of rows, for each sequence and head of the cache
+    int32_t D, heads_q, group, splits, blocks;  // blocks: of rows, for each sequence and head of the cache
     uint32_t group_inverse, heads_inverse, splits_inverse, blocks_inverse;
     float *part;   // [splits][tokens][heads_q][D]: sums, where splits > 1
     float2 *state;  // [splits][tokens][heads_q]: R, sum of 2^(t - R)
@@ -98,88 +109,65 @@ __device__ __forceinline__ Row row_at(const Args &a, const Sequence &s, uint32_t
     return {(int32_t)i, s.first + i, (int64_t)head * a.group + in_group};
 }
 
-// 16 floats of a query at p (fp32, fp16 or bf16)
-__device__ __forceinline__ void load_values(const void *p, int64_t at, int type, float (&x)[16]) {
-    auto take = [&](auto tag) __attribute__((always_inline)) {
-        typedef decltype(tag) T;
-        T e[16];
-        __builtin_memcpy(e, static_cast<const T *>(p) + at, sizeof e);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = (float)e[i];
-    };
-    if (type == QNN_F32)
-        take(0.0f);
-    else if (type == QNN_F16)
-        take((rows::f16)0.0f);
-    else
-        take((rows::bf16)0.0f);
-}
-__device__ __forceinline__ void store_values(void *p, int64_t at, int type, const float (&x)[8]) {
-    const rows::Window w(0, 8);
-    if (type == QNN_F32)
-        rows::store_values<false, false>(static_cast<float *>(p) + at, w, 8, x);
-    else if (type == QNN_F16)
-        rows::store_values<false, false>(static_cast<rows::f16 *>(p) + at, w, 8, x);
-    else
-        rows::store_values<false, false>(static_cast<rows::bf16 *>(p) + at, w, 8, x);
-}
-
-// A query's lanes: DP / 64 runs of 16 values, 64 c + 16 g + 0 .. 15 with g = lane / 16, as float16 operands for the products with 16 bytes of code each
-template <int DP, int kParts>
-struct Query {
-    h8 part[kParts][DP / 64][2];
-    float mult;  // scale of the sums: scale * 2^(what was taken out)
-    __device__ __forceinline__ void load(const Args &a, const Row &row) {
-        const int g = (threadIdx.x & 63) >> 4;
-        float x[DP / 64][16];
-        uint32_t top = 0u;
-#pragma unroll
-        for (int c = 0; c < DP / 64; ++c) {
-            const int d = 64 * c + 16 * g;
-            if (d < a.D) {
-                load_values(a.q, row.token * a.ld_q + row.head * a.step_q + d, a.type, x[c]);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) x[c][i] = 0.0f;
-            }
-#pragma unroll
-            for (int i = 0; i < 16; ++i) top = max(top, rows::magnitude(x[c][i]));
-        }
-        top = max(top, (uint32_t)__shfl_xor((int)top, 16));
-        top = max(top, (uint32_t)__shfl_xor((int)top, 32));
-        const bool fine = top < 0x7F800000u;
-        const int e = fine && top ? __builtin_amdgcn_frexp_expf(__uint_as_float(top)) : 0;
-        mult = __builtin_amdgcn_ldexpf(a.scale, e - 14);
-#pragma unroll
-        for (int c = 0; c < DP / 64; ++c)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float y = fine ? __builtin_amdgcn_ldexpf(x[c][i], 14 - e) : __uint_as_float(0x7FC00000u);
-                const _Float16 hi = (_Float16)y;
-                part[0][c][i >> 3][i & 7] = hi;
-                if constexpr (kParts == 2) part[1][c][i >> 3][i & 7] = (_Float16)(y - (float)hi);
-            }
-    }
+template <typename T>
+struct Parts {
+    static constexpr int kQuery = std::is_same<T, float>::value ? 2 : 1, kWeight = std::is_same<T, rows::bf16>::value ? 1 : 2;
 };
 
-// What a row sees beyond the keys that all rows of a block see
+// A row of queries from the power of two that brings its largest value to 2^13 .. 2^14.  `top`: the largest magnitude, as rows::magnitude has it
+struct Scaling {
+    int exponent;
+    bool fine;
+    __device__ __forceinline__ explicit Scaling(uint32_t top)
+        : exponent(top > 0u && top < 0x7F800000u ? __builtin_amdgcn_frexp_expf(__uint_as_float(top)) - 14 : -14), fine(top < 0x7F800000u) {}
+    __device__ __forceinline__ float of(float x) const { return fine ? __builtin_amdgcn_ldexpf(x, -exponent) : __uint_as_float(0x7FC00000u); }
+    __device__ __forceinline__ float mult(float scale) const { return __builtin_amdgcn_ldexpf(scale, exponent); }  // of the sums
+};
+template <int kParts>
+__device__ __forceinline__ void split(float y, _Float16 (&part)[kParts]) {
+    part[0] = (_Float16)y;
+    if constexpr (kParts == 2) part[1] = (_Float16)(y - (float)part[0]);
+}
+
+template <typename T>
+__device__ __forceinline__ void store_eight(void *p, int64_t at, const float (&x)[8]) {
+    rows::store_values<false, false>(static_cast<T *>(p) + at, rows::Window(0, 8), 8, x);
+}
+
+// What a row sees beyond the keys that all rows of a block see: those up to `last`, and of a tree's drafted ones those in `mask`
 struct Sight {
-    int32_t last;     // causal: the last key
-    uint64_t mask;    // tree
-    float slope;      // times log2(e)
+    int32_t last;
+    uint64_t mask;
+    float slope;  // times log2(e)
     int32_t place;
     __device__ __forceinline__ void load(const Args &a, const Sequence &s, const Row &row) {
-        last = s.base + row.i;
         mask = a.tree ? a.tree[row.token] : 0ull;
+        last = a.tree ? s.base - 1 : s.base + row.i;
         place = a.tree ? s.base - 1 + __popcll(mask) : last;
         slope = a.slopes ? a.slopes[row.head] * kLog2e : 0.0f;
     }
-    __device__ __forceinline__ bool sees(const Args &a, const Sequence &s, int32_t key) const {
-        if (!a.tree) return key <= last;
-        const int32_t drafted = key - s.base;
-        return drafted < 0 || (drafted < 64 && (mask >> (drafted & 63) & 1ull));
+    // kTree: whether there are masks.  (Without branches: sixteen keys' branches one after the other take longer than the products.)
+    template <bool kTree>
+    __device__ __forceinline__ bool sees(const Sequence &s, int32_t key) const {
+        const bool before = key <= last;
+        if constexpr (!kTree) return before;
+        const uint32_t drafted = (uint32_t)(key - s.base);
+        return before | ((drafted < 64u) & (bool)(mask >> (drafted & 63u) & 1ull));
     }
 };
+
+// How a call is split: rows of a workgroup, blocks of rows for each sequence and head of the cache, and parts of the keys
+struct Plan {
+    int rows;
+    int64_t blocks, splits;
+};
+constexpr int kMostSplits = 128;
+
+// qnn_cache_attention_many.hip: the kernel for many rows
+constexpr int many_rows(int64_t D) { return D <= 128 ? 256 : 128; }  // of a workgroup
+// (two parts of a query of 256 values and its sums are more than a lane's registers)
+constexpr bool takes_many(int64_t D, int type) { return D <= 128 || type != QNN_F32; }
+int launch_many(const Args &a, int type, dim3 grid, hipStream_t s);
 
 }  // namespace attention
 }  // namespace qnn

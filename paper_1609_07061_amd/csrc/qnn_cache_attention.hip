@@ -27,9 +27,50 @@ struct Codes {
     uint32_t v[8][kV];
 };
 
-template <int DP, int NB, int kParts, bool kMore>
-__global__ __launch_bounds__(64 * kWaves) void few_rows_kernel(const Args a) {
-    constexpr int kRows = 16 * NB, kPitch = DP + 4, kV = DP / 64;
+// A query's lanes: DP / 64 runs of 16 values, 64 c + 16 g + 0 .. 15 with g = lane / 16, as operands for the products with 16 bytes of code each
+template <typename T, int DP>
+struct Query {
+    static constexpr int kParts = Parts<T>::kQuery;
+    h8 part[kParts][DP / 64][2];
+    float mult;
+    __device__ __forceinline__ void load(const Args &a, const Row &row) {
+        const int g = (threadIdx.x & 63) >> 4;
+        T x[DP / 64][16];
+        uint32_t top = 0u;
+#pragma unroll
+        for (int c = 0; c < DP / 64; ++c) {
+            const int d = 64 * c + 16 * g;
+            __builtin_memcpy(x[c], static_cast<const T *>(a.q) + row.token * a.ld_q + row.head * a.step_q + (d < a.D ? d : 0), sizeof x[c]);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[c][i] = d < a.D ? x[c][i] : (T)0.0f;
+        }
+#pragma unroll
+        for (int c = 0; c < DP / 64; ++c) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = max(top, rows::magnitude((float)x[c][i]));
+        }
+        top = max(top, (uint32_t)__shfl_xor((int)top, 16));
+        top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+        const Scaling scaling(top);
+        mult = scaling.mult(a.scale);
+#pragma unroll
+        for (int c = 0; c < DP / 64; ++c)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                _Float16 y[kParts];
+                split(scaling.of((float)x[c][i]), y);
+#pragma unroll
+                for (int p = 0; p < kParts; ++p) part[p][c][i >> 3][i & 7] = y[p];
+            }
+    }
+};
+
+// (waves that a SIMD is to hold: what is in flight grows with them)
+constexpr int waves_of(int DP, int NB, int parts) { return DP == 64 ? (NB == 1 ? 4 : 2) : (DP == 128 && NB == 1 ? 3 : (parts == 2 ? 1 : 2)); }
+
+template <typename T, int DP, int NB, bool kMore>
+__global__ __launch_bounds__(64 * kWaves, waves_of(DP, NB, Parts<T>::kQuery)) void few_rows_kernel(const Args a) {
+    constexpr int kRows = 16 * NB, kPitch = DP + 4, kV = DP / 64, kQuery = Parts<T>::kQuery, kWeight = Parts<T>::kWeight;
     __shared__ Keys keys[kWaves][2];
     __shared__ float2 states[kWaves][kRows];
     __shared__ __attribute__((aligned(16))) float sums[2][kRows][kPitch];
@@ -53,7 +94,7 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_kernel(const Args a) {
         const int64_t steps = (end + (int64_t)kStep - 1) / kStep;
         const int32_t lo = (int32_t)(steps * split / a.splits), hi = (int32_t)(steps * (split + 1) / a.splits);
 
-        Query<DP, kParts> query[NB];
+        Query<T, DP> query[NB];
         Sight sight[NB];
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
@@ -63,6 +104,7 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_kernel(const Args a) {
             if constexpr (!kMore) query[n].mult *= kLog2e;
         }
         v4f out[DP / 16][NB] = {};
+        const float inverse_cap = kMore && a.cap > 0.0f ? 1.0f / a.cap : 0.0f;
         float level[NB], total[NB];  // R; the sum of 2^(t - R) over this lane's keys
 #pragma unroll
         for (int n = 0; n < NB; ++n) level[n] = -INFINITY, total[n] = 0.0f;
@@ -92,14 +134,16 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_kernel(const Args a) {
                 k.row[at] = there ? x.row : 0u;
                 k.k_scale[at] = x.k_scale, k.v_scale[at] = x.v_scale;
                 k.bias[at] = there ? 0.0f : -INFINITY;
-                k.log_v[at] = x.v_scale != 0.0f ? fmaxf((float)__builtin_amdgcn_frexp_expf(x.v_scale), kLowest) : kLowest;
+                k.log_v[at] = log_scale(x.v_scale);
                 if constexpr (kMore) k.place[at] = x.place;
             }
             __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
             __builtin_amdgcn_wave_barrier();
             __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
         };
-        auto fetch = [&](const Keys &k, Codes<DP> &c) __attribute__((always_inline)) {
+        Codes<DP> c;
+        auto fetch_k = [&](const Keys &k) __attribute__((always_inline)) {
+            const int lane = opaque(threadIdx.x & 63), r = lane & 15, g = lane >> 4;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int8_t *const from = a.k + (int64_t)k.row[16 * h + r] * a.D;
@@ -109,6 +153,9 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_kernel(const Args a) {
                     c.k[h][i] = *reinterpret_cast<const v4u *>(from + (d < a.D ? d : 0));  // (beyond the head the query is zero)
                 }
             }
+        };
+        auto fetch_v = [&](const Keys &k) __attribute__((always_inline)) {
+            const int lane = opaque(threadIdx.x & 63), r = lane & 15, g = lane >> 4;
             const int d = r * (DP / 16) < a.D ? r * (DP / 16) : 0;  // (beyond the head nothing is stored)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -116,8 +163,12 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_kernel(const Args a) {
                 __builtin_memcpy(c.v[e], __builtin_assume_aligned(from, 4 * kV), 4 * kV);
             }
         };
-        auto use = [&](int32_t step, const Keys &k, const Codes<DP> &c) __attribute__((always_inline)) {
-            v4f dots[2][NB] = {};
+        v4f dots[2][NB];
+        auto use_k = [&]() __attribute__((always_inline)) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int n = 0; n < NB; ++n) dots[h][n] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int i = 0; i < DP / 64; ++i)
 #pragma unroll
@@ -128,21 +179,24 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_kernel(const Args a) {
 #pragma unroll
                         for (int n = 0; n < NB; ++n)
 #pragma unroll
-                            for (int p = 0; p < kParts; ++p)
+                            for (int p = 0; p < kQuery; ++p)
                                 dots[h][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes, query[n].part[p][i][f], dots[h][n], 0, 0, 0);
                     }
-            v4f k_scale[2], v_scale[2], bias[2], log_v[2];
+        };
+        auto use_v = [&](int32_t step, const Keys &k) __attribute__((always_inline)) {
+            const int g = opaque(threadIdx.x & 63) >> 4;
+            v4f k_scale[2], v_scale[2], bias[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int from = 16 * h + 4 * g;
                 k_scale[h] = *reinterpret_cast<const v4f *>(&k.k_scale[from]), v_scale[h] = *reinterpret_cast<const v4f *>(&k.v_scale[from]);
-                bias[h] = *reinterpret_cast<const v4f *>(&k.bias[from]), log_v[h] = *reinterpret_cast<const v4f *>(&k.log_v[from]);
+                bias[h] = *reinterpret_cast<const v4f *>(&k.bias[from]);
             }
             const bool masked = (step + 1) * (int64_t)kStep > open;
-            h8 weights[NB][kParts];
+            h8 weights[NB][kWeight];
 #pragma unroll
             for (int n = 0; n < NB; ++n) {
-                float t[2][4], most = -INFINITY;
+                float t[2][4];
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -150,45 +204,63 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_kernel(const Args a) {
                         // (the scales first: a key that is not there has 0, and no product with it may overflow)
                         float x = dots[h][n][e] * (query[n].mult * k_scale[h][e]);
                         if constexpr (kMore) {
-                            if (a.cap > 0.0f) x = a.cap * tanh_of(x / a.cap);
+                            if (a.cap > 0.0f) x = a.cap * tanh_of(x * inverse_cap);
                             x *= kLog2e;
                             if (a.slopes) x -= sight[n].slope * (float)(sight[n].place - k.place[16 * h + 4 * g + e]);
                         }
                         t[h][e] = x + bias[h][e];
                     }
-                if (masked) {
+                auto mask = [&](auto tree) __attribute__((always_inline)) {
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (!sight[n].sees(a, s, step * kStep + 16 * h + 4 * g + e)) t[h][e] = -INFINITY;
+                        for (int e = 0; e < 4; ++e) t[h][e] = sight[n].template sees<decltype(tree)::value>(s, step * kStep + 16 * h + 4 * g + e) ? t[h][e] : -INFINITY;
+                };
+                if (masked) {
+                    if (a.tree)
+                        mask(std::true_type{});
+                    else
+                        mask(std::false_type{});
                 }
+                float sum, largest;
+                auto weigh = [&]() __attribute__((always_inline)) {
+                    const float from = level[n] == -INFINITY ? 0.0f : level[n];
+                    sum = 0.0f, largest = 0.0f;
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
+                    for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) most = fmaxf(most, t[h][e] + log_v[h][e]);
-                most = fmaxf(most, __shfl_xor(most, 16));
-                most = fmaxf(most, __shfl_xor(most, 32));
-                const bool moves = most > level[n] + 15.0f;
-                if (__any(moves)) {
+                        for (int e = 0; e < 4; ++e) {
+                            const float p = __builtin_amdgcn_exp2f(t[h][e] - from), w = t[h][e] == -INFINITY ? 0.0f : p * v_scale[h][e];
+                            sum += p, largest = fmaxf(largest, fabsf(w));  // (and a scale that is NaN is only for those who see it)
+                            _Float16 x[kWeight];
+                            attention::split(w, x);
+#pragma unroll
+                            for (int i = 0; i < kWeight; ++i) weights[n][i][4 * h + e] = x[i];
+                        }
+                };
+                weigh();
+                if (__any(level[n] == -INFINITY || largest > 32768.0f)) {
+                    float most = -INFINITY;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const v4f log_v = *reinterpret_cast<const v4f *>(&k.log_v[16 * h + 4 * g]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) most = fmaxf(most, t[h][e] + log_v[e]);
+                    }
+                    most = fmaxf(most, __shfl_xor(most, 16));
+                    most = fmaxf(most, __shfl_xor(most, 32));
+                    largest = fmaxf(largest, __shfl_xor(largest, 16));
+                    largest = fmaxf(largest, __shfl_xor(largest, 32));
+                    // (whether a query's R moves depends on that query alone)
+                    const bool moves = (level[n] == -INFINITY || largest > 32768.0f) && most > level[n];
                     const float now = moves ? most - 8.0f : level[n], factor = level[n] == now ? 1.0f : __builtin_amdgcn_exp2f(level[n] - now);
                     level[n] = now;
                     total[n] *= factor;
 #pragma unroll
                     for (int d = 0; d < DP / 16; ++d) out[d][n] *= factor;
+                    weigh();
                 }
-                const float from = level[n] == -INFINITY ? 0.0f : level[n];
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float p = __builtin_amdgcn_exp2f(t[h][e] - from);
-                        total[n] += p;
-                        const float w = t[h][e] == -INFINITY ? 0.0f : p * v_scale[h][e];  // (a scale that is NaN is only for those who see it)
-                        const _Float16 hi = (_Float16)w;
-                        weights[n][0][4 * h + e] = hi;
-                        if constexpr (kParts == 2) weights[n][1][4 * h + e] = (_Float16)(w - (float)hi);
-                    }
+                total[n] += sum;
             }
             // V: byte d mod 4 of word d / 4 of the eight keys' rows
 #pragma unroll
@@ -209,35 +281,36 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_kernel(const Args a) {
 #pragma unroll
                         for (int n = 0; n < NB; ++n)
 #pragma unroll
-                            for (int p = 0; p < kParts; ++p) out[d][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(operand, weights[n][p], out[d][n], 0, 0, 0);
+                            for (int p = 0; p < kWeight; ++p) out[d][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(operand, weights[n][p], out[d][n], 0, 0, 0);
                     }
                 }
         };
 
-        // ---- steps lo + wave, lo + wave + 4, ...: codes one step ahead, scales two, page numbers three
+        // ---- steps lo + wave, lo + wave + 4, ...: of the next one, K's codes are asked for as soon as this one's are used, and V's likewise; scales two steps ahead,
+        // page numbers three
         {
-            Codes<DP> even, odd;
             Ahead ahead;
             const int32_t step0 = lo + wave;
             uint32_t row = find(step0);
             scales(step0, row, ahead);
             row = find(step0 + kWaves);
-            note(ahead, keys[wave][0]);
-            if (step0 < hi) fetch(keys[wave][0], even);
+            if (step0 < hi) {
+                note(ahead, keys[wave][0]);
+                fetch_k(keys[wave][0]);
+                fetch_v(keys[wave][0]);
+            }
             scales(step0 + kWaves, row, ahead);
             row = find(step0 + 2 * kWaves);
-            for (int32_t step = step0; step < hi; step += 2 * kWaves) {
-                note(ahead, keys[wave][1]);
-                fetch(keys[wave][1], odd);
+            int turn = 0;
+            for (int32_t step = step0; step < hi; step += kWaves) {
+                use_k();
+                note(ahead, keys[wave][turn ^ 1]);
+                if (step + kWaves < hi) fetch_k(keys[wave][turn ^ 1]);
+                use_v(step, keys[wave][turn]);
+                turn ^= 1;
+                if (step + kWaves < hi) fetch_v(keys[wave][turn]);
                 scales(step + 2 * kWaves, row, ahead);
                 row = find(step + 3 * kWaves);
-                use(step, keys[wave][0], even);
-                if (step + kWaves >= hi) break;
-                note(ahead, keys[wave][0]);
-                fetch(keys[wave][0], even);
-                scales(step + 3 * kWaves, row, ahead);
-                row = find(step + 4 * kWaves);
-                use(step + kWaves, keys[wave][1], odd);
             }
         }
 
@@ -288,7 +361,7 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_kernel(const Args a) {
             if (a.splits == 1) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) y[e] = sum == 0.0f ? 0.0f : y[e] / sum;
-                store_values(a.out, at_row.token * a.ld_out + at_row.head * a.step_out + d, a.type, y);
+                store_eight<T>(a.out, at_row.token * a.ld_out + at_row.head * a.step_out + d, y);
             } else {
                 const int64_t to = ((int64_t)split * a.tokens + at_row.token) * a.heads_q + at_row.head;
                 if (d == 0) a.state[to] = make_float2(most, sum);
@@ -303,8 +376,7 @@ __global__ __launch_bounds__(64 * kWaves) void few_rows_kernel(const Args a) {
 }
 
 // Parts of the keys joined: a workgroup for each query and head.  32 lanes (64 where a head is longer than 128) have a part's sums, 4 values a lane.
-constexpr int kMostSplits = 128;
-
+template <typename T>
 __global__ __launch_bounds__(256) void join_kernel(const Args a) {
     __shared__ float factors[kMostSplits], totals[4], tops[4];
     __shared__ v4f sums[8][64];
@@ -347,22 +419,18 @@ __global__ __launch_bounds__(256) void join_kernel(const Args a) {
             for (int p = 0; p < parts; ++p) x += sums[p][2 * tid + e / 4][e % 4];
             z[e] = sum == 0.0f ? 0.0f : x / sum;
         }
-        store_values(a.out, token * a.ld_out + head * a.step_out + 8 * tid, a.type, z);
+        store_eight<T>(a.out, token * a.ld_out + head * a.step_out + 8 * tid, z);
     }
 }
 
-// How a call is split: blocks of rows for each sequence and head of the cache, and parts of the keys
-struct Plan {
-    int rows;
-    int64_t blocks, splits;
-};
-Plan plan_of(int64_t sequences, int64_t heads_q, int64_t heads, int64_t most_new, int64_t longest) {
+Plan plan_of(int64_t sequences, int64_t heads_q, int64_t heads, int64_t D, int type, int64_t most_new, int64_t longest) {
     Plan p;
     const int64_t rows = most_new * (heads_q / heads);
-    p.rows = rows <= 16 ? 16 : 32;
+    p.rows = rows <= 64 || !takes_many(D, type) ? (rows <= 16 || D > 128 ? 16 : 32) : many_rows(D);
     p.blocks = ceil_div(rows, p.rows);
-    // two workgroups a compute unit, as long as a part has a step for every wave
-    const int64_t have = sequences * heads * p.blocks, want = ceil_div(2 * (int64_t)compute_units(), have), most = ceil_div(longest, kStep * kWaves);
+    // two workgroups a compute unit (one of the large ones), as long as a part has a step for every wave
+    const int64_t have = sequences * heads * p.blocks, want = ceil_div((p.rows > 32 ? 1 : 2) * (int64_t)compute_units(), have);
+    const int64_t most = ceil_div(longest, p.rows > 32 ? 256 : kStep * kWaves);
     p.splits = want < 1 ? 1 : (want < most ? want : most);
     if (p.splits > kMostSplits) p.splits = kMostSplits;
     return p;
@@ -374,16 +442,17 @@ bool plannable(int64_t tokens, int64_t sequences, int64_t heads_q, int64_t heads
 // (numbers above what there can be do no more than these)
 int64_t at_most(int64_t x, int64_t limit) { return x < limit ? x : limit; }
 
-template <int DP, int kParts, bool kMore>
-int launch_few(const Args &a, const Plan &p, dim3 grid, hipStream_t s) {
-    if (p.rows == 16) return QNN_LAUNCH("cache_attention", (few_rows_kernel<DP, 1, kParts, kMore>), grid, dim3(64 * kWaves), 0, s, a);
-    return QNN_LAUNCH("cache_attention", (few_rows_kernel<DP, 2, kParts, kMore>), grid, dim3(64 * kWaves), 0, s, a);
+template <typename T, int DP, bool kMore>
+int launch_few(const Args &a, int rows, dim3 grid, hipStream_t s) {
+    if (DP > 128 || rows == 16) return QNN_LAUNCH("cache_attention", (few_rows_kernel<T, DP, 1, kMore>), grid, dim3(64 * kWaves), 0, s, a);
+    if constexpr (DP <= 128) return QNN_LAUNCH("cache_attention", (few_rows_kernel<T, DP, 2, kMore>), grid, dim3(64 * kWaves), 0, s, a);
 }
-template <int DP>
-int launch(const Args &a, const Plan &p, dim3 grid, hipStream_t s) {
+template <typename T>
+int launch_few(const Args &a, int rows, dim3 grid, hipStream_t s) {
     const bool more = a.cap > 0.0f || a.slopes;
-    if (a.type == QNN_F32) return more ? launch_few<DP, 2, true>(a, p, grid, s) : launch_few<DP, 2, false>(a, p, grid, s);
-    return more ? launch_few<DP, 1, true>(a, p, grid, s) : launch_few<DP, 1, false>(a, p, grid, s);
+    if (a.D <= 64) return more ? launch_few<T, 64, true>(a, rows, grid, s) : launch_few<T, 64, false>(a, rows, grid, s);
+    if (a.D <= 128) return more ? launch_few<T, 128, true>(a, rows, grid, s) : launch_few<T, 128, false>(a, rows, grid, s);
+    return more ? launch_few<T, 256, true>(a, rows, grid, s) : launch_few<T, 256, false>(a, rows, grid, s);
 }
 
 }  // namespace
@@ -395,8 +464,12 @@ using namespace qnn;
 extern "C" size_t qnn_cache_attention_workspace_bytes(int64_t tokens, int64_t sequences, int64_t heads_q, int64_t heads, int64_t D, int64_t most_new,
                                                       int64_t longest) {
     if (!attention::plannable(tokens, sequences, heads_q, heads, D, most_new, longest)) return 0;
-    const attention::Plan p = attention::plan_of(sequences, heads_q, heads, attention::at_most(most_new, tokens), attention::at_most(longest, 0x7FFFFFFF));
-    return p.splits == 1 ? 0 : (size_t)p.splits * (size_t)tokens * (size_t)heads_q * ((size_t)D * 4 + 8);
+    int64_t splits = 1;  // (enough for any type)
+    for (int type : {QNN_F32, QNN_BF16}) {
+        const attention::Plan p = attention::plan_of(sequences, heads_q, heads, D, type, attention::at_most(most_new, tokens), attention::at_most(longest, 0x7FFFFFFF));
+        if (p.splits > splits) splits = p.splits;
+    }
+    return splits == 1 ? 0 : (size_t)splits * (size_t)tokens * (size_t)heads_q * ((size_t)D * 4 + 8);
 }
 
 extern "C" int qnn_cache_attention(const qnn_paged_cache *cache, const void *q, int64_t ld_q, int64_t step_q, int64_t heads_q, int type, float scale, float cap,
@@ -421,7 +494,7 @@ extern "C" int qnn_cache_attention(const qnn_paged_cache *cache, const void *q, 
     if (!rows::aligned_to(q, w) || !rows::aligned_to(out, w) || !rows::aligned_to(slopes, 4) || !rows::aligned_to(tree, 8))
         return fail(QNN_ERR_ALIGN, "%s: pointer not aligned to its type", what);
     most_new = attention::at_most(most_new, tokens), longest = attention::at_most(longest, 0x7FFFFFFF);
-    const attention::Plan p = attention::plan_of(cache->sequences, heads_q, cache->heads, most_new, longest);
+    const attention::Plan p = attention::plan_of(cache->sequences, heads_q, cache->heads, D, type, most_new, longest);
     const size_t need = qnn_cache_attention_workspace_bytes(tokens, cache->sequences, heads_q, cache->heads, D, most_new, longest);
     if (need > 0 && (!workspace || !rows::aligned_to(workspace, 256) || workspace_bytes < need))
         return fail(QNN_ERR_WORKSPACE, "%s: workspace NULL, misaligned or smaller than %zu bytes", what, need);
@@ -433,13 +506,15 @@ extern "C" int qnn_cache_attention(const qnn_paged_cache *cache, const void *q, 
     a.q = q, a.out = out, a.ld_q = ld_q, a.step_q = step_q, a.ld_out = ld_out, a.step_out = step_out;
     a.k = cache->k, a.v = cache->v, a.k_scale = cache->k_scale, a.v_scale = cache->v_scale;
     a.pages = paged::pages_of(*cache), a.starts = cache->starts, a.lengths = cache->lengths, a.slopes = slopes, a.tree = tree, a.scale = scale, a.cap = cap;
-    a.tokens = tokens, a.sequences = cache->sequences, a.type = type, a.D = (int32_t)D, a.heads_q = (int32_t)heads_q;
+    a.tokens = tokens, a.sequences = cache->sequences, a.D = (int32_t)D, a.heads_q = (int32_t)heads_q;
     a.group = (int32_t)(heads_q / cache->heads), a.splits = (int32_t)p.splits, a.blocks = (int32_t)p.blocks;
     a.group_inverse = inverse_of(a.group), a.heads_inverse = inverse_of(cache->heads), a.splits_inverse = inverse_of(p.splits), a.blocks_inverse = inverse_of(p.blocks);
     a.part = part, a.state = reinterpret_cast<float2 *>(part + p.splits * queries * D);
     hipStream_t s = static_cast<hipStream_t>(stream);
     const dim3 grid = rows::grid_of((int64_t)blocks);
-    const int rc = D <= 64 ? attention::launch<64>(a, p, grid, s) : (D <= 128 ? attention::launch<128>(a, p, grid, s) : attention::launch<256>(a, p, grid, s));
+    const int rc = p.rows > 32
+                       ? attention::launch_many(a, type, grid, s)
+                       : rows::with_type(type, [&](auto tag) { return attention::launch_few<decltype(tag)>(a, p.rows, grid, s); });
     if (rc || p.splits == 1) return rc;
-    return QNN_LAUNCH(what, attention::join_kernel, rows::grid_of(queries), dim3(256), 0, s, a);
+    return rows::with_type(type, [&](auto tag) { return QNN_LAUNCH(what, attention::join_kernel<decltype(tag)>, rows::grid_of(queries), dim3(256), 0, s, a); });
 }

@@ -1,0 +1,395 @@
+// Attention over the paged cache for many rows (drafted trees, prompts): a workgroup has 32 rows a wave, and all its waves meet the same 64 keys at a time, whose codes
+// the workgroup brings from memory to registers two tiles ahead, makes float16 once for all waves and lays into LDS as the matrix instructions (32 x 32 x 16) take them.
+// S^T = K Q^T and O^T = V^T P^T: of the first result a lane has keys 8 a + 4 g + 0 .. 3 (a = 0 .. 3, g = lane / 32) of its query lane mod 32, which is the second's
+// right operand as it is, with the rows of V^T's operand in that order of keys.
+#include "qnn_attention.h"
+
+namespace qnn {
+namespace attention {
+namespace {
+
+typedef float v16f __attribute__((ext_vector_type(16)));
+
+constexpr int kTile = 64;  // keys
+
+// K: [key][DP] in pieces of 8 float16, piece p of key r at p xor (r mod 8).  V: rows of 64 keys, value d at row (d mod 4) (DP / 4) + d / 4: a block of 32 rows is what
+// one quarter of the lanes' words holds; piece 2 s + g has keys 16 s + 4 g + 0 .. 3 and 16 s + 8 + 4 g + 0 .. 3, and lies at (2 s + g) xor (row mod 8).
+template <int DP>
+struct Tile {
+    uint8_t k[kTile * DP * 2];
+    uint8_t v[kTile * DP * 2];
+};
+struct Scales {
+    float k[kTile], v[kTile], log_v[kTile], bias[kTile];  // log_v: log2 of v, rounded up; bias: 0, or -infinity for a key that is not there
+    int32_t place[kTile];
+    int32_t all_there;
+};
+
+template <typename T, int DP, int kWaves, bool kMore>
+__global__ __launch_bounds__(64 * kWaves, kWaves / 4) void many_rows_kernel(const Args a) {
+    constexpr int kThreads = 64 * kWaves, kRows = 32 * kWaves, kQuery = Parts<T>::kQuery, kWeight = Parts<T>::kWeight;
+    constexpr int kUnitsK = kTile * DP / 16, kUnitsV = kTile / 4 * (DP / 4), kLoadsK = (kUnitsK + kThreads - 1) / kThreads, kLoadsV = (kUnitsV + kThreads - 1) / kThreads;
+    constexpr int kAtOnce = DP > 128 || kQuery == 2 || kMore ? 1 : 2;  // (registers)
+    __shared__ __attribute__((aligned(16))) Tile<DP> tiles[2];
+    __shared__ __attribute__((aligned(16))) Scales scales[2];
+    __shared__ uint32_t rows_of[2][kTile];
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r = lane & 31, g = lane >> 5;
+    uint32_t head, split, block, b;
+    {
+        const uint32_t id = rows::block_number();
+        uint32_t rest = quotient(id, a.pages.heads, a.heads_inverse, head);
+        rest = quotient(rest, (uint32_t)a.splits, a.splits_inverse, split);
+        b = quotient(rest, (uint32_t)a.blocks, a.blocks_inverse, block);
+    }
+    if ((int64_t)b >= a.sequences) return;  // (of the launch's last line)
+    const Sequence s = sequence_at(a, b);
+    const uint32_t n_rows = (uint32_t)s.fresh * (uint32_t)a.group;
+    for (uint32_t first = block * kRows; first < n_rows; first += (uint32_t)a.blocks * kRows) {
+        uint32_t in_group;
+        const uint32_t last = min(first + kRows, n_rows) - 1u;
+        const int32_t i0 = (int32_t)quotient(first, (uint32_t)a.group, a.group_inverse, in_group), i1 = (int32_t)quotient(last, (uint32_t)a.group, a.group_inverse, in_group);
+        // keys below `end` are looked at, those below `open` are seen by all rows
+        const int32_t end = min(a.tree ? s.n : max(s.base + i1 + 1, 0), s.in_table), open = a.tree ? s.base : s.base + i0 + 1;
+        const int64_t steps = (end + (int64_t)kTile - 1) / kTile;
+        const int32_t lo = (int32_t)(steps * split / a.splits), hi = (int32_t)(steps * (split + 1) / a.splits);
+        const bool busy = first + 32u * wave <= last;  // (other waves bring codes only)
+        const Row row = row_at(a, s, min(first + 32u * wave + r, last), head);
+
+        // ---- the query: DP / 16 steps of 16 values, 8 g + 0 .. 7 of each in this lane
+        h8 query[kQuery][DP / 16];
+        float mult;
+        Sight sight;
+        {
+            T x[DP / 16][8];
+            uint32_t top = 0u;
+#pragma unroll
+            for (int c = 0; c < DP / 16; ++c) {
+                __builtin_memcpy(x[c], static_cast<const T *>(a.q) + row.token * a.ld_q + row.head * a.step_q + (16 * c < a.D ? 16 * c + 8 * g : 0), sizeof x[c]);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[c][i] = 16 * c < a.D ? x[c][i] : (T)0.0f;
+            }
+#pragma unroll
+            for (int c = 0; c < DP / 16; ++c) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) top = max(top, rows::magnitude((float)x[c][i]));
+            }
+            top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+            const Scaling scaling(top);
+            mult = scaling.mult(a.scale);
+            if constexpr (!kMore) mult *= kLog2e;
+#pragma unroll
+            for (int c = 0; c < DP / 16; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    _Float16 y[kQuery];
+                    attention::split(scaling.of((float)x[c][i]), y);
+#pragma unroll
+                    for (int p = 0; p < kQuery; ++p) query[p][c][i] = y[p];
+                }
+            sight.load(a, s, row);
+        }
+        v16f out[DP / 32] = {};
+        float level = -INFINITY, total = 0.0f;
+        const float inverse_cap = kMore && a.cap > 0.0f ? 1.0f / a.cap : 0.0f;
+
+        // ---- codes: page numbers four tiles ahead, rows and scales three, codes two, float16 one
+        auto find = [&](int32_t tile) __attribute__((always_inline)) -> uint32_t {  // (threads below kTile)
+            const int32_t key = tile * kTile + tid;
+            const uint32_t at = tile < hi && key < end ? paged::row_of(a.pages, b, (uint32_t)key) : paged::kNoRow;
+            return at == paged::kNoRow ? at : at + head * a.pages.page;
+        };
+        struct Ahead {
+            uint32_t row;
+            float k, v;
+            int32_t place;
+        };
+        auto ask = [&](int32_t tile, uint32_t at, Ahead &x) __attribute__((always_inline)) {
+            rows_of[(tile - lo) & 1][tid] = at == paged::kNoRow ? 0u : at;
+            x.row = at;
+            x.k = at != paged::kNoRow ? a.k_scale[at] : 0.0f, x.v = at != paged::kNoRow ? a.v_scale[at] : 0.0f;
+            x.place = tile * kTile + tid;
+            if (kMore && a.tree && x.place >= s.base && at != paged::kNoRow && x.place - s.base < s.fresh)
+                x.place = s.base - 1 + __popcll(a.tree[s.first + (x.place - s.base)]);
+        };
+        auto note = [&](int32_t tile, const Ahead &x) __attribute__((always_inline)) {
+            Scales &to = scales[(tile - lo) & 1];
+            const bool there = x.row != paged::kNoRow;
+            to.k[tid] = x.k, to.v[tid] = x.v, to.bias[tid] = there ? 0.0f : -INFINITY;
+            to.log_v[tid] = log_scale(x.v);
+            if constexpr (kMore) to.place[tid] = x.place;
+            const bool all = __all(there);
+            if (tid == 0) to.all_there = all;
+        };
+        v4u raw_k[kLoadsK];
+        uint32_t raw_v[kLoadsV][4];
+        auto fetch = [&](int32_t tile) __attribute__((always_inline)) {
+            const int tid = opaque(threadIdx.x);
+            const uint32_t *const at = rows_of[(tile - lo) & 1];
+#pragma unroll
+            for (int i = 0; i < kLoadsK; ++i) {
+                const int u = tid + kThreads * i, key = u / (DP / 16), d = u % (DP / 16) * 16;
+                if (kUnitsK % kThreads == 0 || u < kUnitsK) raw_k[i] = *reinterpret_cast<const v4u *>(a.k + (int64_t)at[key] * a.D + (d < a.D ? d : 0));
+            }
+#pragma unroll
+            for (int i = 0; i < kLoadsV; ++i) {
+                const int u = tid + kThreads * i, four = u / (DP / 4), d = u % (DP / 4) * 4;
+                if (kUnitsV % kThreads == 0 || u < kUnitsV) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) raw_v[i][e] = *reinterpret_cast<const uint32_t *>(a.v + (int64_t)at[4 * four + e] * a.D + (d < a.D ? d : 0));
+                }
+            }
+        };
+        auto put = [&](int32_t tile) __attribute__((always_inline)) {
+            const int tid = opaque(threadIdx.x);
+            Tile<DP> &to = tiles[(tile - lo) & 1];
+#pragma unroll
+            for (int i = 0; i < kLoadsK; ++i) {
+                const int u = tid + kThreads * i, key = u / (DP / 16), piece = u % (DP / 16) * 2;
+                if (kUnitsK % kThreads == 0 || u < kUnitsK) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+                        *reinterpret_cast<h8 *>(to.k + key * DP * 2 + 16 * ((piece + h) ^ (key & 7))) = eight_codes(raw_k[i][2 * h], raw_k[i][2 * h + 1]);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < kLoadsV; ++i) {
+                const int u = tid + kThreads * i, four = u / (DP / 4), at = u % (DP / 4);
+                if (kUnitsV % kThreads == 0 || u < kUnitsV) {
+                    h2 codes[4][2];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+#pragma unroll
+                        for (int half = 0; half < 2; ++half) {
+                            const uint32_t pair = __builtin_amdgcn_perm(raw_v[i][2 * e + 1] ^ kBias, raw_v[i][2 * e] ^ kBias, half ? 0x07030602u : 0x05010400u);
+                            codes[2 * half][e] = halves(__builtin_amdgcn_perm(kExponents, pair, 0x04010400u));
+                            codes[2 * half + 1][e] = halves(__builtin_amdgcn_perm(kExponents, pair, 0x04030402u));
+                        }
+                    // keys 4 four .. + 3 = 16 s + 8 h + 4 g + ..
+                    const int piece = (four >> 2) * 2 + (four & 1), h = four >> 1 & 1;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int at_row = j * (DP / 4) + at;
+                        *reinterpret_cast<h4 *>(to.v + at_row * kTile * 2 + 16 * (piece ^ (at_row & 7)) + 8 * h) = h4{codes[j][0][0], codes[j][0][1], codes[j][1][0], codes[j][1][1]};
+                    }
+                }
+            }
+        };
+
+        auto use = [&](int32_t tile) __attribute__((always_inline)) {
+            const int lane = opaque(threadIdx.x & 63), r = lane & 31, g = lane >> 5;
+            const Tile<DP> &t = tiles[(tile - lo) & 1];
+            const Scales &sc = scales[(tile - lo) & 1];
+            const bool masked = (tile + 1) * (int64_t)kTile > open || !sc.all_there;
+            // 32 kAtOnce keys at a time; key 32 h + 8 e + 4 g + i is value 4 e + i of block h
+#pragma unroll
+            for (int h0 = 0; h0 < 2; h0 += kAtOnce) {
+                v16f dots[kAtOnce] = {};
+#pragma unroll
+                for (int h = 0; h < kAtOnce; ++h)
+#pragma unroll
+                    for (int c = 0; c < DP / 16; ++c) {
+                        const h8 codes = *reinterpret_cast<const h8 *>(t.k + (32 * (h0 + h) + r) * DP * 2 + 16 * ((2 * c + g) ^ (r & 7)));
+#pragma unroll
+                        for (int p = 0; p < kQuery; ++p) dots[h] = __builtin_amdgcn_mfma_f32_32x32x16_f16(codes, query[p][c], dots[h], 0, 0, 0);
+                        if (c % 4 == 3) __builtin_amdgcn_sched_barrier(0);  // (operands that far ahead, and no further: registers)
+                    }
+#pragma unroll
+                for (int h = 0; h < kAtOnce; ++h)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const v4f k = *reinterpret_cast<const v4f *>(&sc.k[32 * (h0 + h) + 8 * e + 4 * g]);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) dots[h][4 * e + i] *= mult * k[i];
+                        if (e == 3) __builtin_amdgcn_sched_barrier(0);
+                    }
+                if constexpr (kMore) {
+                    if (a.cap > 0.0f) {
+#pragma unroll
+                        for (int h = 0; h < kAtOnce; ++h)
+#pragma unroll
+                            for (int x = 0; x < 16; ++x) dots[h][x] = a.cap * tanh_of(dots[h][x] * inverse_cap);
+                    }
+#pragma unroll
+                    for (int h = 0; h < kAtOnce; ++h)
+#pragma unroll
+                        for (int x = 0; x < 16; ++x) dots[h][x] = dots[h][x] * kLog2e;
+                    if (a.slopes) {
+#pragma unroll
+                        for (int h = 0; h < kAtOnce; ++h)
+#pragma unroll
+                            for (int x = 0; x < 16; ++x)
+                                dots[h][x] -= sight.slope * (float)(sight.place - sc.place[32 * (h0 + h) + 8 * (x / 4) + 4 * g + x % 4]);
+                    }
+                }
+                auto mask = [&](auto tree) __attribute__((always_inline)) {
+#pragma unroll
+                    for (int h = 0; h < kAtOnce; ++h)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const int from = 32 * (h0 + h) + 8 * e + 4 * g;
+                            const v4f bias = *reinterpret_cast<const v4f *>(&sc.bias[from]);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const bool sees = sight.sees<decltype(tree)::value>(s, tile * kTile + from + i) & (bias[i] == 0.0f);
+                                dots[h][4 * e + i] = sees ? dots[h][4 * e + i] : -INFINITY;
+                            }
+                        }
+                };
+                if (masked) {
+                    if (a.tree)
+                        mask(std::true_type{});
+                    else
+                        mask(std::false_type{});
+                }
+                // weights from R on, their sum without the values' scales, and the largest
+                h8 weights[kWeight][2 * kAtOnce];
+                float sum, largest;
+                auto weigh = [&]() __attribute__((always_inline)) {
+                    const float from = level == -INFINITY ? 0.0f : level;
+                    sum = 0.0f, largest = 0.0f;
+#pragma unroll
+                    for (int h = 0; h < kAtOnce; ++h) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const v4f v = *reinterpret_cast<const v4f *>(&sc.v[32 * (h0 + h) + 8 * e + 4 * g]);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const float x = dots[h][4 * e + i], p = __builtin_amdgcn_exp2f(x - from);
+                                float w = p * v[i];
+                                if (masked) w = x == -INFINITY ? 0.0f : w;  // (a scale that is NaN is only for those who see it)
+                                sum += p, largest = fmaxf(largest, fabsf(w));
+                                _Float16 y[kWeight];
+                                attention::split(w, y);
+#pragma unroll
+                                for (int q = 0; q < kWeight; ++q) weights[q][2 * h + (e >> 1)][4 * (e & 1) + i] = y[q];
+                            }
+                        }
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                };
+                weigh();
+                if (__any(level == -INFINITY || largest > 32768.0f)) {
+                    float most = -INFINITY;
+#pragma unroll
+                    for (int h = 0; h < kAtOnce; ++h)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const v4f v = *reinterpret_cast<const v4f *>(&sc.log_v[32 * (h0 + h) + 8 * e + 4 * g]);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) most = fmaxf(most, dots[h][4 * e + i] + v[i]);
+                        }
+                    most = fmaxf(most, __shfl_xor(most, 32)), largest = fmaxf(largest, __shfl_xor(largest, 32));
+                    // (whether a query's R moves depends on that query alone)
+                    const bool moves = (level == -INFINITY || largest > 32768.0f) && most > level;
+                    const float now = moves ? most - 8.0f : level, factor = level == now ? 1.0f : __builtin_amdgcn_exp2f(level - now);
+                    level = now;
+                    total *= factor;
+#pragma unroll
+                    for (int d = 0; d < DP / 32; ++d) out[d] *= factor;
+                    weigh();
+                }
+                total += sum;
+#pragma unroll
+                for (int c = 0; c < 2 * kAtOnce; ++c)
+#pragma unroll
+                    for (int d = 0; d < DP / 32; ++d) {
+                        const h8 codes = *reinterpret_cast<const h8 *>(t.v + (32 * d + r) * kTile * 2 + 16 * ((2 * (2 * h0 + c) + g) ^ (r & 7)));
+#pragma unroll
+                        for (int q = 0; q < kWeight; ++q) out[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(codes, weights[q][c], out[d], 0, 0, 0);
+                        if (d % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+                    }
+            }
+        };
+
+        __syncthreads();  // (the rows before are done with LDS)
+        if (lo < hi) {
+            Ahead even, odd;  // scales of tiles lo, lo + 2, .. and lo + 1, lo + 3, ..
+            uint32_t at = paged::kNoRow;
+            if (tid < kTile) {
+                ask(lo, find(lo), even);
+                ask(lo + 1, find(lo + 1), odd);
+                note(lo, even);
+                at = find(lo + 2);
+            }
+            __syncthreads();
+            fetch(lo);
+            put(lo);
+            fetch(lo + 1);
+            __syncthreads();
+            if (tid < kTile) {
+                ask(lo + 2, at, even);
+                at = find(lo + 3);
+            }
+            __syncthreads();
+            // at the top: tile t in LDS, the codes of t + 1 and scales of t + 1, t + 2 under way
+            auto turn = [&](int32_t t, Ahead &next) __attribute__((always_inline)) {
+                if (t + 1 < hi) put(t + 1);
+                if (t + 2 < hi) fetch(t + 2);
+                if (tid < kTile) {
+                    if (t + 1 < hi) note(t + 1, next);
+                    ask(t + 3, at, next);
+                    at = find(t + 4);
+                }
+                if (busy) use(t);
+                __syncthreads();
+            };
+            for (int32_t t = lo; t < hi; ++t) {
+                turn(t, odd);
+                const Ahead swap = odd;
+                odd = even, even = swap;
+            }
+        }
+
+        if (busy) {
+            const int g = opaque(threadIdx.x & 63) >> 5;
+            total += __shfl_xor(total, 32);
+            const bool mine = first + 32u * wave + r <= last;
+            const float inverse = total == 0.0f ? 0.0f : 1.0f / total;
+            const int64_t to = ((int64_t)split * a.tokens + row.token) * a.heads_q + row.head;
+            if (mine && a.splits > 1 && g == 0) a.state[to] = make_float2(level, total);
+            // four values 4 x + 0 .. 3 are at rows x, x + DP / 4, ..; of them this lane has x = 8 e + 4 g + 0 .. 3
+#pragma unroll
+            for (int e = 0; e < DP / 32; ++e)
+#pragma unroll
+                for (int i = 0; i < 4; i += 2) {
+                    float y[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const int at_row = (j & 3) * (DP / 4) + 8 * e;
+                        y[j] = out[at_row / 32][at_row % 32 / 8 * 4 + i + (j >> 2)];
+                    }
+                    const int d = 4 * (8 * e + 4 * g + i);
+                    if (mine && d < a.D) {
+                        if (a.splits == 1) {
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) y[j] = total == 0.0f ? 0.0f : y[j] * inverse;
+                            store_eight<T>(a.out, row.token * a.ld_out + row.head * a.step_out + d, y);
+                        } else if (!(total == 0.0f)) {
+                            __builtin_memcpy(a.part + to * a.D + d, y, sizeof y);
+                        }
+                    }
+                }
+        }
+    }
+}
+
+template <typename T, int DP, int kWaves>
+int launch(const Args &a, dim3 grid, hipStream_t s) {
+    if (a.cap > 0.0f || a.slopes) return QNN_LAUNCH("cache_attention", (many_rows_kernel<T, DP, kWaves, true>), grid, dim3(64 * kWaves), 0, s, a);
+    return QNN_LAUNCH("cache_attention", (many_rows_kernel<T, DP, kWaves, false>), grid, dim3(64 * kWaves), 0, s, a);
+}
+
+}  // namespace
+
+int launch_many(const Args &a, int type, dim3 grid, hipStream_t s) {
+    return rows::with_type(type, [&](auto tag) {
+        typedef decltype(tag) T;
+        if (a.D <= 64) return launch<T, 64, 8>(a, grid, s);
+        if (a.D <= 128) return launch<T, 128, 8>(a, grid, s);
+        if constexpr (!std::is_same<T, float>::value) return launch<T, 256, 4>(a, grid, s);
+        return fail(QNN_ERR_UNSUPPORTED, "cache_attention: no kernel");  // (as takes_many says)
+    });
+}
+
+}  // namespace attention
+}  // namespace qnn
