@@ -101,10 +101,9 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NB, Parts<T>::kQuery)) vo
             const Row row = row_at(a, s, min(first + 16u * n + r, last), head);
             query[n].load(a, row);
             sight[n].load(a, s, row);
-            if constexpr (!kMore) query[n].mult *= kLog2e;
+            query[n].mult *= kMore && a.cap > 0.0f ? 1.0f / a.cap : kLog2e;
         }
         v4f out[DP / 16][NB] = {};
-        const float inverse_cap = kMore && a.cap > 0.0f ? 1.0f / a.cap : 0.0f;
         float level[NB], total[NB];  // R; the sum of 2^(t - R) over this lane's keys
 #pragma unroll
         for (int n = 0; n < NB; ++n) level[n] = -INFINITY, total[n] = 0.0f;
@@ -204,9 +203,8 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NB, Parts<T>::kQuery)) vo
                         // (the scales first: a key that is not there has 0, and no product with it may overflow)
                         float x = dots[h][n][e] * (query[n].mult * k_scale[h][e]);
                         if constexpr (kMore) {
-                            if (a.cap > 0.0f) x = a.cap * tanh_of(x * inverse_cap);
-                            x *= kLog2e;
-                            if (a.slopes) x -= sight[n].slope * (float)(sight[n].place - k.place[16 * h + 4 * g + e]);
+                            if (a.cap > 0.0f) x = a.cap * kLog2e * tanh_of(x);
+                            if (a.slopes) x = __fmaf_rn(sight[n].slope, (float)(k.place[16 * h + 4 * g + e] - sight[n].place), x);
                         }
                         t[h][e] = x + bias[h][e];
                     }

@@ -19,9 +19,9 @@ struct Tile {
     uint8_t k[kTile * DP * 2];
     uint8_t v[kTile * DP * 2];
 };
-struct Scales {
+struct __attribute__((aligned(16))) Scales {
     float k[kTile], v[kTile], log_v[kTile], bias[kTile];  // log_v: log2 of v, rounded up; bias: 0, or -infinity for a key that is not there
-    int32_t place[kTile];
+    float place[kTile];  // from the tile's first key's on
     int32_t all_there;
 };
 
@@ -29,7 +29,6 @@ template <typename T, int DP, int kWaves, bool kMore>
 __global__ __launch_bounds__(64 * kWaves, kWaves / 4) void many_rows_kernel(const Args a) {
     constexpr int kThreads = 64 * kWaves, kRows = 32 * kWaves, kQuery = Parts<T>::kQuery, kWeight = Parts<T>::kWeight;
     constexpr int kUnitsK = kTile * DP / 16, kUnitsV = kTile / 4 * (DP / 4), kLoadsK = (kUnitsK + kThreads - 1) / kThreads, kLoadsV = (kUnitsV + kThreads - 1) / kThreads;
-    constexpr int kAtOnce = DP > 128 || kQuery == 2 || kMore ? 1 : 2;  // (registers)
     __shared__ __attribute__((aligned(16))) Tile<DP> tiles[2];
     __shared__ __attribute__((aligned(16))) Scales scales[2];
     __shared__ uint32_t rows_of[2][kTile];
@@ -75,8 +74,7 @@ __global__ __launch_bounds__(64 * kWaves, kWaves / 4) void many_rows_kernel(cons
             }
             top = max(top, (uint32_t)__shfl_xor((int)top, 32));
             const Scaling scaling(top);
-            mult = scaling.mult(a.scale);
-            if constexpr (!kMore) mult *= kLog2e;
+            mult = scaling.mult(a.scale) * (kMore && a.cap > 0.0f ? 1.0f / a.cap : kLog2e);
 #pragma unroll
             for (int c = 0; c < DP / 16; ++c)
 #pragma unroll
@@ -90,7 +88,6 @@ __global__ __launch_bounds__(64 * kWaves, kWaves / 4) void many_rows_kernel(cons
         }
         v16f out[DP / 32] = {};
         float level = -INFINITY, total = 0.0f;
-        const float inverse_cap = kMore && a.cap > 0.0f ? 1.0f / a.cap : 0.0f;
 
         // ---- codes: page numbers four tiles ahead, rows and scales three, codes two, float16 one
         auto find = [&](int32_t tile) __attribute__((always_inline)) -> uint32_t {  // (threads below kTile)
@@ -116,7 +113,7 @@ __global__ __launch_bounds__(64 * kWaves, kWaves / 4) void many_rows_kernel(cons
             const bool there = x.row != paged::kNoRow;
             to.k[tid] = x.k, to.v[tid] = x.v, to.bias[tid] = there ? 0.0f : -INFINITY;
             to.log_v[tid] = log_scale(x.v);
-            if constexpr (kMore) to.place[tid] = x.place;
+            if constexpr (kMore) to.place[tid] = (float)(x.place - tile * kTile);
             const bool all = __all(there);
             if (tid == 0) to.all_there = all;
         };
@@ -180,104 +177,128 @@ __global__ __launch_bounds__(64 * kWaves, kWaves / 4) void many_rows_kernel(cons
             const Tile<DP> &t = tiles[(tile - lo) & 1];
             const Scales &sc = scales[(tile - lo) & 1];
             const bool masked = (tile + 1) * (int64_t)kTile > open || !sc.all_there;
-            // 32 kAtOnce keys at a time; key 32 h + 8 e + 4 g + i is value 4 e + i of block h
+            // Operands are read from LDS eight at a time and well ahead: K's of the first 32 keys at once, of the others before the products with V, V's before the
+            // weights.  (The scheduler by itself reads one ahead, and every product waits for LDS: 489 us where this takes 300, 2048 of 8192 tokens, 32 heads of 128.)
+            constexpr int kOperands = DP / 16, kAhead = kQuery == 2 || DP > 128 ? 4 : 8;  // of K, of V, for 32 keys; (registers)
+            h8 of_k[kAhead], of_v[kAhead];
+            auto read_k = [&](int h, int c0) __attribute__((always_inline)) {
 #pragma unroll
-            for (int h0 = 0; h0 < 2; h0 += kAtOnce) {
-                v16f dots[kAtOnce] = {};
+                for (int c = c0; c < c0 + kAhead && c < kOperands; ++c)
+                    of_k[c - c0] = *reinterpret_cast<const h8 *>(t.k + (32 * h + r) * DP * 2 + 16 * ((2 * c + g) ^ (r & 7)));
+                __builtin_amdgcn_sched_barrier(0);
+            };
+            auto read_v = [&](int h, int x0) __attribute__((always_inline)) {  // operand x: step x / (DP / 32) of 16 keys, rows 32 (x mod DP / 32) on
 #pragma unroll
-                for (int h = 0; h < kAtOnce; ++h)
+                for (int x = x0; x < x0 + kAhead && x < kOperands; ++x) {
+                    const int c = x / (DP / 32), d = x % (DP / 32);
+                    of_v[x - x0] = *reinterpret_cast<const h8 *>(t.v + (32 * d + r) * kTile * 2 + 16 * ((2 * (2 * h + c) + g) ^ (r & 7)));
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            };
+            read_k(0, 0);
 #pragma unroll
-                    for (int c = 0; c < DP / 16; ++c) {
-                        const h8 codes = *reinterpret_cast<const h8 *>(t.k + (32 * (h0 + h) + r) * DP * 2 + 16 * ((2 * c + g) ^ (r & 7)));
+            for (int h = 0; h < 2; ++h) {
+                // 32 keys: key 32 h + 8 e + 4 g + i is value 4 e + i
+                v16f dots = {};
 #pragma unroll
-                        for (int p = 0; p < kQuery; ++p) dots[h] = __builtin_amdgcn_mfma_f32_32x32x16_f16(codes, query[p][c], dots[h], 0, 0, 0);
-                        if (c % 4 == 3) __builtin_amdgcn_sched_barrier(0);  // (operands that far ahead, and no further: registers)
-                    }
+                for (int c0 = 0; c0 < kOperands; c0 += kAhead) {
+                    if (c0 > 0) read_k(h, c0);
 #pragma unroll
-                for (int h = 0; h < kAtOnce; ++h)
+                    for (int c = c0; c < c0 + kAhead && c < kOperands; ++c)
+#pragma unroll
+                        for (int p = 0; p < kQuery; ++p) dots = __builtin_amdgcn_mfma_f32_32x32x16_f16(of_k[c - c0], query[p][c], dots, 0, 0, 0);
+                }
+                read_v(h, 0);
+                auto four = [&](const float *from, int e) __attribute__((always_inline)) { return *reinterpret_cast<const v4f *>(from + 32 * h + 8 * e + 4 * g); };
+                auto scale = [&]() __attribute__((always_inline)) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const v4f k = *reinterpret_cast<const v4f *>(&sc.k[32 * (h0 + h) + 8 * e + 4 * g]);
+                        const v4f k = four(sc.k, e);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) dots[h][4 * e + i] *= mult * k[i];
-                        if (e == 3) __builtin_amdgcn_sched_barrier(0);
+                        for (int i = 0; i < 4; ++i) dots[4 * e + i] *= mult * k[i];
                     }
+                };
                 if constexpr (kMore) {
+                    scale();
                     if (a.cap > 0.0f) {
+                        asm volatile("" ::: "memory");  // (keeps the branch a branch, here and below)
 #pragma unroll
-                        for (int h = 0; h < kAtOnce; ++h)
-#pragma unroll
-                            for (int x = 0; x < 16; ++x) dots[h][x] = a.cap * tanh_of(dots[h][x] * inverse_cap);
+                        for (int x = 0; x < 16; ++x) dots[x] = a.cap * kLog2e * tanh_of(dots[x]);
                     }
-#pragma unroll
-                    for (int h = 0; h < kAtOnce; ++h)
-#pragma unroll
-                        for (int x = 0; x < 16; ++x) dots[h][x] = dots[h][x] * kLog2e;
                     if (a.slopes) {
-#pragma unroll
-                        for (int h = 0; h < kAtOnce; ++h)
-#pragma unroll
-                            for (int x = 0; x < 16; ++x)
-                                dots[h][x] -= sight.slope * (float)(sight.place - sc.place[32 * (h0 + h) + 8 * (x / 4) + 4 * g + x % 4]);
-                    }
-                }
-                auto mask = [&](auto tree) __attribute__((always_inline)) {
-#pragma unroll
-                    for (int h = 0; h < kAtOnce; ++h)
+                        const float place = (float)(sight.place - tile * kTile);  // (from the tile's beginning: whole numbers, exact)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            const int from = 32 * (h0 + h) + 8 * e + 4 * g;
-                            const v4f bias = *reinterpret_cast<const v4f *>(&sc.bias[from]);
+                            const v4f of = four(sc.place, e);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) dots[4 * e + i] = __fmaf_rn(sight.slope, of[i] - place, dots[4 * e + i]);
+                        }
+                    }
+                }
+                if (masked) {
+                    asm volatile("" ::: "memory");
+                    if constexpr (!kMore) scale();
+                    auto mask = [&](auto tree) __attribute__((always_inline)) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const v4f bias = four(sc.bias, e);
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
-                                const bool sees = sight.sees<decltype(tree)::value>(s, tile * kTile + from + i) & (bias[i] == 0.0f);
-                                dots[h][4 * e + i] = sees ? dots[h][4 * e + i] : -INFINITY;
+                                const bool sees = sight.template sees<decltype(tree)::value>(s, tile * kTile + 32 * h + 8 * e + 4 * g + i) & (bias[i] == 0.0f);
+                                dots[4 * e + i] = sees ? dots[4 * e + i] : -INFINITY;
                             }
                         }
-                };
-                if (masked) {
-                    if (a.tree)
+                    };
+                    if (a.tree) {
+                        asm volatile("" ::: "memory");
                         mask(std::true_type{});
-                    else
+                    } else {
+                        asm volatile("" ::: "memory");
                         mask(std::false_type{});
+                    }
                 }
-                // weights from R on, their sum without the values' scales, and the largest
-                h8 weights[kWeight][2 * kAtOnce];
+                // weights from R on, their sum without the values' scales, and the largest.  kRaw: of products that have no scale yet.  kMasked: where a score may
+                // be -infinity (a scale that is NaN is only for those who see it)
+                h8 weights[kWeight][2];
                 float sum, largest;
-                auto weigh = [&]() __attribute__((always_inline)) {
+                auto weigh = [&](auto raw, auto some) __attribute__((always_inline)) {
+                    constexpr bool kRaw = decltype(raw)::value, kMasked = decltype(some)::value;
                     const float from = level == -INFINITY ? 0.0f : level;
                     sum = 0.0f, largest = 0.0f;
 #pragma unroll
-                    for (int h = 0; h < kAtOnce; ++h) {
+                    for (int e = 0; e < 4; ++e) {
+                        const v4f v = four(sc.v, e);
+                        v4f k;
+                        if constexpr (kRaw) k = four(sc.k, e);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const v4f v = *reinterpret_cast<const v4f *>(&sc.v[32 * (h0 + h) + 8 * e + 4 * g]);
+                        for (int i = 0; i < 4; ++i) {
+                            const float x = dots[4 * e + i], p = __builtin_amdgcn_exp2f(kRaw ? __fmaf_rn(x, mult * k[i], -from) : x - from);
+                            float w = p * v[i];
+                            if constexpr (kMasked) w = x == -INFINITY ? 0.0f : w;
+                            sum += p, largest = fmaxf(largest, fabsf(w));
+                            _Float16 y[kWeight];
+                            attention::split(w, y);
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const float x = dots[h][4 * e + i], p = __builtin_amdgcn_exp2f(x - from);
-                                float w = p * v[i];
-                                if (masked) w = x == -INFINITY ? 0.0f : w;  // (a scale that is NaN is only for those who see it)
-                                sum += p, largest = fmaxf(largest, fabsf(w));
-                                _Float16 y[kWeight];
-                                attention::split(w, y);
-#pragma unroll
-                                for (int q = 0; q < kWeight; ++q) weights[q][2 * h + (e >> 1)][4 * (e & 1) + i] = y[q];
-                            }
+                            for (int q = 0; q < kWeight; ++q) weights[q][e >> 1][4 * (e & 1) + i] = y[q];
                         }
-                        __builtin_amdgcn_sched_barrier(0);
                     }
                 };
-                weigh();
+                if (masked) {
+                    asm volatile("" ::: "memory");
+                    weigh(std::false_type{}, std::true_type{});
+                } else {
+                    weigh(std::integral_constant<bool, !kMore>{}, std::false_type{});
+                }
                 if (__any(level == -INFINITY || largest > 32768.0f)) {
+                    asm volatile("" ::: "memory");
+                    if (!kMore && !masked) scale();
                     float most = -INFINITY;
 #pragma unroll
-                    for (int h = 0; h < kAtOnce; ++h)
+                    for (int e = 0; e < 4; ++e) {
+                        const v4f v = four(sc.log_v, e);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const v4f v = *reinterpret_cast<const v4f *>(&sc.log_v[32 * (h0 + h) + 8 * e + 4 * g]);
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) most = fmaxf(most, dots[h][4 * e + i] + v[i]);
-                        }
+                        for (int i = 0; i < 4; ++i) most = fmaxf(most, dots[4 * e + i] + v[i]);
+                    }
                     most = fmaxf(most, __shfl_xor(most, 32)), largest = fmaxf(largest, __shfl_xor(largest, 32));
                     // (whether a query's R moves depends on that query alone)
                     const bool moves = (level == -INFINITY || largest > 32768.0f) && most > level;
@@ -286,18 +307,19 @@ __global__ __launch_bounds__(64 * kWaves, kWaves / 4) void many_rows_kernel(cons
                     total *= factor;
 #pragma unroll
                     for (int d = 0; d < DP / 32; ++d) out[d] *= factor;
-                    weigh();
+                    weigh(std::false_type{}, std::true_type{});
                 }
                 total += sum;
+                if (h == 0) read_k(1, 0);
 #pragma unroll
-                for (int c = 0; c < 2 * kAtOnce; ++c)
+                for (int x0 = 0; x0 < kOperands; x0 += kAhead) {
+                    if (x0 > 0) read_v(h, x0);
 #pragma unroll
-                    for (int d = 0; d < DP / 32; ++d) {
-                        const h8 codes = *reinterpret_cast<const h8 *>(t.v + (32 * d + r) * kTile * 2 + 16 * ((2 * (2 * h0 + c) + g) ^ (r & 7)));
+                    for (int x = x0; x < x0 + kAhead && x < kOperands; ++x)
 #pragma unroll
-                        for (int q = 0; q < kWeight; ++q) out[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(codes, weights[q][c], out[d], 0, 0, 0);
-                        if (d % 4 == 3) __builtin_amdgcn_sched_barrier(0);
-                    }
+                        for (int q = 0; q < kWeight; ++q)
+                            out[x % (DP / 32)] = __builtin_amdgcn_mfma_f32_32x32x16_f16(of_v[x - x0], weights[q][x / (DP / 32)], out[x % (DP / 32)], 0, 0, 0);
+                }
             }
         };
 
