@@ -125,6 +125,8 @@ struct Scaling {
 };
 template <int kParts>
 __device__ __forceinline__ void split(float y, _Float16 (&part)[kParts]) {
+    // (from the value in fp32: a product that the compiler rounds to fp16 in one instruction may differ from the one that it takes off for the second part)
+    if constexpr (kParts == 2) asm("" : "+v"(y));
     part[0] = (_Float16)y;
     if constexpr (kParts == 2) part[1] = (_Float16)(y - (float)part[0]);
 }

@@ -115,12 +115,12 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NB, Parts<T>::kQuery)) vo
             float k_scale, v_scale;
             int32_t place;
         };
-        auto find = [&](int32_t step) __attribute__((always_inline)) -> uint32_t {
+        auto find = [&](int32_t step) __attribute__((always_inline)) -> paged::Place {
             const int32_t key = step * kStep + at;
-            const uint32_t row = step < hi && key < end ? paged::row_of(a.pages, b, (uint32_t)key) : paged::kNoRow;
-            return row == paged::kNoRow ? row : row + head * a.pages.page;
+            return step < hi && key < end ? paged::place_of(a.pages, b, (uint32_t)key) : paged::Place{paged::kNoRow, 0u};
         };
-        auto scales = [&](int32_t step, uint32_t row, Ahead &x) __attribute__((always_inline)) {
+        auto scales = [&](int32_t step, const paged::Place &place, Ahead &x) __attribute__((always_inline)) {
+            const uint32_t row = paged::row_of(a.pages, place, head);
             x.row = row;
             x.k_scale = row != paged::kNoRow ? a.k_scale[row] : 0.0f, x.v_scale = row != paged::kNoRow ? a.v_scale[row] : 0.0f;
             x.place = step * kStep + at;
@@ -289,7 +289,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NB, Parts<T>::kQuery)) vo
         {
             Ahead ahead;
             const int32_t step0 = lo + wave;
-            uint32_t row = find(step0);
+            paged::Place row = find(step0);
             scales(step0, row, ahead);
             row = find(step0 + kWaves);
             if (step0 < hi) {

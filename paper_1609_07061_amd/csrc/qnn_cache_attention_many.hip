@@ -25,13 +25,15 @@ struct __attribute__((aligned(16))) Scales {
     int32_t all_there;
 };
 
-template <typename T, int DP, int kWaves, bool kMore>
+// kKind: 0 plain scores, 1 a bias by distance, 2 capped, with a bias or not
+template <typename T, int DP, int kWaves, int kKind>
 __global__ __launch_bounds__(64 * kWaves, kWaves / 4) void many_rows_kernel(const Args a) {
     constexpr int kThreads = 64 * kWaves, kRows = 32 * kWaves, kQuery = Parts<T>::kQuery, kWeight = Parts<T>::kWeight;
     constexpr int kUnitsK = kTile * DP / 16, kUnitsV = kTile / 4 * (DP / 4), kLoadsK = (kUnitsK + kThreads - 1) / kThreads, kLoadsV = (kUnitsV + kThreads - 1) / kThreads;
     __shared__ __attribute__((aligned(16))) Tile<DP> tiles[2];
     __shared__ __attribute__((aligned(16))) Scales scales[2];
     __shared__ uint32_t rows_of[2][kTile];
+    __shared__ __attribute__((aligned(16))) float ones[kTile];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, r = lane & 31, g = lane >> 5;
     uint32_t head, split, block, b;
     {
@@ -41,6 +43,7 @@ __global__ __launch_bounds__(64 * kWaves, kWaves / 4) void many_rows_kernel(cons
         b = quotient(rest, (uint32_t)a.blocks, a.blocks_inverse, block);
     }
     if ((int64_t)b >= a.sequences) return;  // (of the launch's last line)
+    if (tid < kTile) ones[tid] = 1.0f;
     const Sequence s = sequence_at(a, b);
     const uint32_t n_rows = (uint32_t)s.fresh * (uint32_t)a.group;
     for (uint32_t first = block * kRows; first < n_rows; first += (uint32_t)a.blocks * kRows) {
@@ -74,7 +77,7 @@ __global__ __launch_bounds__(64 * kWaves, kWaves / 4) void many_rows_kernel(cons
             }
             top = max(top, (uint32_t)__shfl_xor((int)top, 32));
             const Scaling scaling(top);
-            mult = scaling.mult(a.scale) * (kMore && a.cap > 0.0f ? 1.0f / a.cap : kLog2e);
+            mult = scaling.mult(a.scale) * (kKind == 2 ? 1.0f / a.cap : kLog2e);
 #pragma unroll
             for (int c = 0; c < DP / 16; ++c)
 #pragma unroll
@@ -89,39 +92,44 @@ __global__ __launch_bounds__(64 * kWaves, kWaves / 4) void many_rows_kernel(cons
         v16f out[DP / 32] = {};
         float level = -INFINITY, total = 0.0f;
 
-        // ---- codes: page numbers four tiles ahead, rows and scales three, codes two, float16 one
-        auto find = [&](int32_t tile) __attribute__((always_inline)) -> uint32_t {  // (threads below kTile)
-            const int32_t key = tile * kTile + tid;
-            const uint32_t at = tile < hi && key < end ? paged::row_of(a.pages, b, (uint32_t)key) : paged::kNoRow;
-            return at == paged::kNoRow ? at : at + head * a.pages.page;
+        // ---- codes: page numbers four tiles ahead, rows and scales three, codes two, float16 one.  Tiles are taken from the last on (tile_at): the keys next to a
+        // query weigh most, all the more with a bias by distance, and R, which follows the largest, moves once.  (From the first on: 607 us where this takes 416, 2048
+        // of 8192 tokens, 32 heads of 128, half of whose slopes are above 2^-4.)
+        auto tile_at = [&](int32_t t) __attribute__((always_inline)) { return lo + hi - 1 - t; };
+        auto find = [&](int32_t t) __attribute__((always_inline)) -> paged::Place {  // (threads below kTile)
+            const int32_t key = tile_at(t) * kTile + tid;
+            return t < hi && key < end ? paged::place_of(a.pages, b, (uint32_t)key) : paged::Place{paged::kNoRow, 0u};
         };
         struct Ahead {
             uint32_t row;
             float k, v;
             int32_t place;
         };
-        auto ask = [&](int32_t tile, uint32_t at, Ahead &x) __attribute__((always_inline)) {
-            rows_of[(tile - lo) & 1][tid] = at == paged::kNoRow ? 0u : at;
+        auto ask = [&](int32_t t, const paged::Place &place, Ahead &x) __attribute__((always_inline)) {
+            const uint32_t at = paged::row_of(a.pages, place, head);
+            rows_of[(t - lo) & 1][tid] = at == paged::kNoRow ? 0u : at;
             x.row = at;
             x.k = at != paged::kNoRow ? a.k_scale[at] : 0.0f, x.v = at != paged::kNoRow ? a.v_scale[at] : 0.0f;
-            x.place = tile * kTile + tid;
-            if (kMore && a.tree && x.place >= s.base && at != paged::kNoRow && x.place - s.base < s.fresh)
+            x.place = tile_at(t) * kTile + tid;
+            if (kKind > 0 && a.tree && x.place >= s.base && at != paged::kNoRow && x.place - s.base < s.fresh)
                 x.place = s.base - 1 + __popcll(a.tree[s.first + (x.place - s.base)]);
         };
-        auto note = [&](int32_t tile, const Ahead &x) __attribute__((always_inline)) {
-            Scales &to = scales[(tile - lo) & 1];
+        auto note = [&](int32_t t, const Ahead &x) __attribute__((always_inline)) {
+            Scales &to = scales[(t - lo) & 1];
             const bool there = x.row != paged::kNoRow;
-            to.k[tid] = x.k, to.v[tid] = x.v, to.bias[tid] = there ? 0.0f : -INFINITY;
+            // (a scale of values that is not finite becomes a score that is NaN, for those who see it)
+            const bool fine = rows::magnitude(x.v) < 0x7F800000u;
+            to.k[tid] = fine ? x.k : __uint_as_float(0x7FC00000u), to.v[tid] = fine ? x.v : 0.0f, to.bias[tid] = there ? 0.0f : -INFINITY;
             to.log_v[tid] = log_scale(x.v);
-            if constexpr (kMore) to.place[tid] = (float)(x.place - tile * kTile);
+            if constexpr (kKind > 0) to.place[tid] = (float)(x.place - tile_at(t) * kTile);
             const bool all = __all(there);
             if (tid == 0) to.all_there = all;
         };
         v4u raw_k[kLoadsK];
         uint32_t raw_v[kLoadsV][4];
-        auto fetch = [&](int32_t tile) __attribute__((always_inline)) {
+        auto fetch = [&](int32_t t) __attribute__((always_inline)) {
             const int tid = opaque(threadIdx.x);
-            const uint32_t *const at = rows_of[(tile - lo) & 1];
+            const uint32_t *const at = rows_of[(t - lo) & 1];
 #pragma unroll
             for (int i = 0; i < kLoadsK; ++i) {
                 const int u = tid + kThreads * i, key = u / (DP / 16), d = u % (DP / 16) * 16;
@@ -136,9 +144,9 @@ __global__ __launch_bounds__(64 * kWaves, kWaves / 4) void many_rows_kernel(cons
                 }
             }
         };
-        auto put = [&](int32_t tile) __attribute__((always_inline)) {
+        auto put = [&](int32_t t) __attribute__((always_inline)) {
             const int tid = opaque(threadIdx.x);
-            Tile<DP> &to = tiles[(tile - lo) & 1];
+            Tile<DP> &to = tiles[(t - lo) & 1];
 #pragma unroll
             for (int i = 0; i < kLoadsK; ++i) {
                 const int u = tid + kThreads * i, key = u / (DP / 16), piece = u % (DP / 16) * 2;
@@ -172,20 +180,25 @@ __global__ __launch_bounds__(64 * kWaves, kWaves / 4) void many_rows_kernel(cons
             }
         };
 
-        auto use = [&](int32_t tile) __attribute__((always_inline)) {
+        // ---- a tile's products.  Operands are read from LDS a group ahead; of a tile's two halves (32 keys each) the second's product with K runs beside the first's
+        // weights, the first's product with V beside the second's: a wave's matrix instructions and its vector ones take turns, since the two waves of a SIMD, which
+        // meet at a barrier every tile, would do the same at the same time.
+        constexpr int kOperands = DP / 16, kAhead = kQuery == 2 || DP > 128 ? 2 : 4;  // of K, of V, for 32 keys; as many ahead as registers allow
+        auto use = [&](int32_t number) __attribute__((always_inline)) {
+            const int32_t tile = tile_at(number);
             const int lane = opaque(threadIdx.x & 63), r = lane & 31, g = lane >> 5;
-            const Tile<DP> &t = tiles[(tile - lo) & 1];
-            const Scales &sc = scales[(tile - lo) & 1];
-            const bool masked = (tile + 1) * (int64_t)kTile > open || !sc.all_there;
-            // Operands are read from LDS eight at a time and well ahead: K's of the first 32 keys at once, of the others before the products with V, V's before the
-            // weights.  (The scheduler by itself reads one ahead, and every product waits for LDS: 489 us where this takes 300, 2048 of 8192 tokens, 32 heads of 128.)
-            constexpr int kOperands = DP / 16, kAhead = kQuery == 2 || DP > 128 ? 4 : 8;  // of K, of V, for 32 keys; (registers)
+            const Tile<DP> &t = tiles[(number - lo) & 1];
+            const Scales &sc = scales[(number - lo) & 1];
+            const bool masked = (tile + 1) * (int64_t)kTile > open || !sc.all_there;  // some rows do not see some keys
+            // products are scaled on the way to the exponent, unless they had to be before
+            const bool scaled = kKind > 0 || masked;
+            const float *const rest_k = scaled ? ones : sc.k;
+            const float rest = scaled ? 1.0f : mult;
             h8 of_k[kAhead], of_v[kAhead];
             auto read_k = [&](int h, int c0) __attribute__((always_inline)) {
 #pragma unroll
                 for (int c = c0; c < c0 + kAhead && c < kOperands; ++c)
                     of_k[c - c0] = *reinterpret_cast<const h8 *>(t.k + (32 * h + r) * DP * 2 + 16 * ((2 * c + g) ^ (r & 7)));
-                __builtin_amdgcn_sched_barrier(0);
             };
             auto read_v = [&](int h, int x0) __attribute__((always_inline)) {  // operand x: step x / (DP / 32) of 16 keys, rows 32 (x mod DP / 32) on
 #pragma unroll
@@ -193,59 +206,68 @@ __global__ __launch_bounds__(64 * kWaves, kWaves / 4) void many_rows_kernel(cons
                     const int c = x / (DP / 32), d = x % (DP / 32);
                     of_v[x - x0] = *reinterpret_cast<const h8 *>(t.v + (32 * d + r) * kTile * 2 + 16 * ((2 * (2 * h + c) + g) ^ (r & 7)));
                 }
-                __builtin_amdgcn_sched_barrier(0);
             };
-            read_k(0, 0);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                // 32 keys: key 32 h + 8 e + 4 g + i is value 4 e + i
-                v16f dots = {};
+            v16f dots[2];  // key 32 h + 8 e + 4 g + i is value 4 e + i of half h
+            h8 weights[2][kWeight][2];
+            float sum, largest;
+            auto four = [&](const float *from, int h, int e) __attribute__((always_inline)) { return *reinterpret_cast<const v4f *>(from + 32 * h + 8 * e + 4 * g); };
+            auto with_k = [&](int h) __attribute__((always_inline)) {
+                dots[h] = v16f{};
 #pragma unroll
                 for (int c0 = 0; c0 < kOperands; c0 += kAhead) {
                     if (c0 > 0) read_k(h, c0);
 #pragma unroll
                     for (int c = c0; c < c0 + kAhead && c < kOperands; ++c)
 #pragma unroll
-                        for (int p = 0; p < kQuery; ++p) dots = __builtin_amdgcn_mfma_f32_32x32x16_f16(of_k[c - c0], query[p][c], dots, 0, 0, 0);
+                        for (int p = 0; p < kQuery; ++p) dots[h] = __builtin_amdgcn_mfma_f32_32x32x16_f16(of_k[c - c0], query[p][c], dots[h], 0, 0, 0);
                 }
-                read_v(h, 0);
-                auto four = [&](const float *from, int e) __attribute__((always_inline)) { return *reinterpret_cast<const v4f *>(from + 32 * h + 8 * e + 4 * g); };
-                auto scale = [&]() __attribute__((always_inline)) {
+            };
+            auto with_v = [&](int h) __attribute__((always_inline)) {
+#pragma unroll
+                for (int x0 = 0; x0 < kOperands; x0 += kAhead) {
+                    if (x0 > 0) read_v(h, x0);
+#pragma unroll
+                    for (int x = x0; x < x0 + kAhead && x < kOperands; ++x)
+#pragma unroll
+                        for (int q = 0; q < kWeight; ++q)
+                            out[x % (DP / 32)] = __builtin_amdgcn_mfma_f32_32x32x16_f16(of_v[x - x0], weights[h][q][x / (DP / 32)], out[x % (DP / 32)], 0, 0, 0);
+                }
+            };
+            auto scale = [&](int h) __attribute__((always_inline)) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const v4f k = four(sc.k, h, e);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) dots[h][4 * e + i] *= mult * k[i];
+                }
+            };
+            // scores times log2(e), -infinity where a row does not see a key
+            auto score = [&](int h) __attribute__((always_inline)) {
+                if constexpr (kKind > 0) scale(h);
+                if constexpr (kKind == 2) {
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) dots[h][x] = a.cap * kLog2e * tanh_of(dots[h][x]);
+                }
+                if (kKind == 1 || (kKind == 2 && a.slopes)) {
+                    const float place = (float)(sight.place - tile * kTile);  // (from the tile's beginning: whole numbers, exact)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const v4f k = four(sc.k, e);
+                        const v4f of = four(sc.place, h, e);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) dots[4 * e + i] *= mult * k[i];
-                    }
-                };
-                if constexpr (kMore) {
-                    scale();
-                    if (a.cap > 0.0f) {
-                        asm volatile("" ::: "memory");  // (keeps the branch a branch, here and below)
-#pragma unroll
-                        for (int x = 0; x < 16; ++x) dots[x] = a.cap * kLog2e * tanh_of(dots[x]);
-                    }
-                    if (a.slopes) {
-                        const float place = (float)(sight.place - tile * kTile);  // (from the tile's beginning: whole numbers, exact)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const v4f of = four(sc.place, e);
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) dots[4 * e + i] = __fmaf_rn(sight.slope, of[i] - place, dots[4 * e + i]);
-                        }
+                        for (int i = 0; i < 4; ++i) dots[h][4 * e + i] = __fmaf_rn(sight.slope, of[i] - place, dots[h][4 * e + i]);
                     }
                 }
                 if (masked) {
-                    asm volatile("" ::: "memory");
-                    if constexpr (!kMore) scale();
+                    asm volatile("" ::: "memory");  // (keeps the branch a branch, here and below)
+                    if constexpr (kKind == 0) scale(h);
                     auto mask = [&](auto tree) __attribute__((always_inline)) {
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            const v4f bias = four(sc.bias, e);
+                            const v4f bias = four(sc.bias, h, e);
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
                                 const bool sees = sight.template sees<decltype(tree)::value>(s, tile * kTile + 32 * h + 8 * e + 4 * g + i) & (bias[i] == 0.0f);
-                                dots[4 * e + i] = sees ? dots[4 * e + i] : -INFINITY;
+                                dots[h][4 * e + i] = sees ? dots[h][4 * e + i] : -INFINITY;
                             }
                         }
                     };
@@ -257,76 +279,86 @@ __global__ __launch_bounds__(64 * kWaves, kWaves / 4) void many_rows_kernel(cons
                         mask(std::false_type{});
                     }
                 }
-                // weights from R on, their sum without the values' scales, and the largest.  kRaw: of products that have no scale yet.  kMasked: where a score may
-                // be -infinity (a scale that is NaN is only for those who see it)
-                h8 weights[kWeight][2];
-                float sum, largest;
-                auto weigh = [&](auto raw, auto some) __attribute__((always_inline)) {
-                    constexpr bool kRaw = decltype(raw)::value, kMasked = decltype(some)::value;
-                    const float from = level == -INFINITY ? 0.0f : level;
-                    sum = 0.0f, largest = 0.0f;
+            };
+            // weights from R on, their sum without the values' scales, and the largest
+            auto weigh = [&](int h) __attribute__((always_inline)) {
+                const float from = level == -INFINITY ? 0.0f : level;
+                sum = 0.0f, largest = 0.0f;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const v4f v = four(sc.v, e);
-                        v4f k;
-                        if constexpr (kRaw) k = four(sc.k, e);
+                for (int e = 0; e < 4; ++e) {
+                    const v4f v = four(sc.v, h, e);
+                    v4f k;
+                    if constexpr (kKind == 0) k = four(rest_k, h, e);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const float x = dots[4 * e + i], p = __builtin_amdgcn_exp2f(kRaw ? __fmaf_rn(x, mult * k[i], -from) : x - from);
-                            float w = p * v[i];
-                            if constexpr (kMasked) w = x == -INFINITY ? 0.0f : w;
-                            sum += p, largest = fmaxf(largest, fabsf(w));
-                            _Float16 y[kWeight];
-                            attention::split(w, y);
+                    for (int i = 0; i < 4; ++i) {
+                        const float x = dots[h][4 * e + i], p = __builtin_amdgcn_exp2f(kKind == 0 ? __fmaf_rn(x, rest * k[i], -from) : x - from);
+                        const float w = p * v[i];
+                        sum += p, largest = fmaxf(largest, fabsf(w));
+                        _Float16 y[kWeight];
+                        attention::split(w, y);
 #pragma unroll
-                            for (int q = 0; q < kWeight; ++q) weights[q][e >> 1][4 * (e & 1) + i] = y[q];
-                        }
+                        for (int q = 0; q < kWeight; ++q) weights[h][q][e >> 1][4 * (e & 1) + i] = y[q];
                     }
-                };
-                if (masked) {
-                    asm volatile("" ::: "memory");
-                    weigh(std::false_type{}, std::true_type{});
-                } else {
-                    weigh(std::integral_constant<bool, !kMore>{}, std::false_type{});
                 }
+            };
+            // moves R where a weight would be too large, which is seldom, and takes the half's sum in
+            auto settle = [&](int h) __attribute__((always_inline)) {
                 if (__any(level == -INFINITY || largest > 32768.0f)) {
                     asm volatile("" ::: "memory");
-                    if (!kMore && !masked) scale();
                     float most = -INFINITY;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const v4f v = four(sc.log_v, e);
+                        const v4f v = four(sc.log_v, h, e), k = four(rest_k, h, e);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) most = fmaxf(most, dots[4 * e + i] + v[i]);
+                        for (int i = 0; i < 4; ++i) most = fmaxf(most, dots[h][4 * e + i] * (rest * k[i]) + v[i]);
                     }
                     most = fmaxf(most, __shfl_xor(most, 32)), largest = fmaxf(largest, __shfl_xor(largest, 32));
-                    // (whether a query's R moves depends on that query alone)
+                    // (whether a query's R moves, and what it gets, depends on that query alone)
                     const bool moves = (level == -INFINITY || largest > 32768.0f) && most > level;
                     const float now = moves ? most - 8.0f : level, factor = level == now ? 1.0f : __builtin_amdgcn_exp2f(level - now);
                     level = now;
                     total *= factor;
 #pragma unroll
                     for (int d = 0; d < DP / 32; ++d) out[d] *= factor;
-                    weigh(std::false_type{}, std::true_type{});
+                    weigh(h);
                 }
                 total += sum;
-                if (h == 0) read_k(1, 0);
+            };
+            // kVector vector instructions after each matrix one
+            auto in_turn = [](auto matrix, auto vector) __attribute__((always_inline)) {
 #pragma unroll
-                for (int x0 = 0; x0 < kOperands; x0 += kAhead) {
-                    if (x0 > 0) read_v(h, x0);
-#pragma unroll
-                    for (int x = x0; x < x0 + kAhead && x < kOperands; ++x)
-#pragma unroll
-                        for (int q = 0; q < kWeight; ++q)
-                            out[x % (DP / 32)] = __builtin_amdgcn_mfma_f32_32x32x16_f16(of_v[x - x0], weights[q][x / (DP / 32)], out[x % (DP / 32)], 0, 0, 0);
+                for (int i = 0; i < decltype(matrix)::value; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x002, decltype(vector)::value, 0);
                 }
-            }
+                __builtin_amdgcn_sched_barrier(0);
+            };
+            typedef std::integral_constant<int, kOperands * kQuery> OfK;
+            typedef std::integral_constant<int, kOperands * kWeight> OfV;
+            read_k(0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            with_k(0);
+            read_k(1, 0);
+            read_v(0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            score(0);
+            with_k(1);
+            weigh(0);
+            in_turn(OfK{}, std::integral_constant<int, 112 / (kOperands * kQuery)>{});
+            settle(0);
+            score(1);
+            with_v(0);
+            weigh(1);
+            in_turn(OfV{}, std::integral_constant<int, 112 / (kOperands * kWeight)>{});
+            read_v(1, 0);
+            settle(1);
+            with_v(1);
         };
 
         __syncthreads();  // (the rows before are done with LDS)
         if (lo < hi) {
             Ahead even, odd;  // scales of tiles lo, lo + 2, .. and lo + 1, lo + 3, ..
-            uint32_t at = paged::kNoRow;
+            paged::Place at = {paged::kNoRow, 0u};
             if (tid < kTile) {
                 ask(lo, find(lo), even);
                 ask(lo + 1, find(lo + 1), odd);
@@ -343,22 +375,19 @@ __global__ __launch_bounds__(64 * kWaves, kWaves / 4) void many_rows_kernel(cons
                 at = find(lo + 3);
             }
             __syncthreads();
-            // at the top: tile t in LDS, the codes of t + 1 and scales of t + 1, t + 2 under way
-            auto turn = [&](int32_t t, Ahead &next) __attribute__((always_inline)) {
-                if (t + 1 < hi) put(t + 1);
-                if (t + 2 < hi) fetch(t + 2);
+            // at the top: tile t in LDS, the codes of t + 1 and scales of t + 1, t + 2 under way.  (Behind the last tile rows are 0: loads that nobody uses.)
+            for (int32_t t = lo; t < hi; ++t) {
+                put(t + 1);
+                fetch(t + 2);
                 if (tid < kTile) {
-                    if (t + 1 < hi) note(t + 1, next);
-                    ask(t + 3, at, next);
+                    note(t + 1, odd);
+                    ask(t + 3, at, odd);
                     at = find(t + 4);
+                    const Ahead swap = odd;
+                    odd = even, even = swap;
                 }
                 if (busy) use(t);
                 __syncthreads();
-            };
-            for (int32_t t = lo; t < hi; ++t) {
-                turn(t, odd);
-                const Ahead swap = odd;
-                odd = even, even = swap;
             }
         }
 
@@ -397,8 +426,8 @@ __global__ __launch_bounds__(64 * kWaves, kWaves / 4) void many_rows_kernel(cons
 
 template <typename T, int DP, int kWaves>
 int launch(const Args &a, dim3 grid, hipStream_t s) {
-    if (a.cap > 0.0f || a.slopes) return QNN_LAUNCH("cache_attention", (many_rows_kernel<T, DP, kWaves, true>), grid, dim3(64 * kWaves), 0, s, a);
-    return QNN_LAUNCH("cache_attention", (many_rows_kernel<T, DP, kWaves, false>), grid, dim3(64 * kWaves), 0, s, a);
+    auto kernel = a.cap > 0.0f ? many_rows_kernel<T, DP, kWaves, 2> : (a.slopes ? many_rows_kernel<T, DP, kWaves, 1> : many_rows_kernel<T, DP, kWaves, 0>);
+    return QNN_LAUNCH("cache_attention", kernel, grid, dim3(64 * kWaves), 0, s, a);
 }
 
 }  // namespace

@@ -187,7 +187,7 @@ __global__ __launch_bounds__(kThreads) void heads_kernel(const HeadsArgs a) {
             uint32_t row = kNoRow;
             if (b >= 0) {
                 const int64_t at = (int64_t)a.lengths[b] - (a.starts[b + 1] - t);
-                if (at >= 0) row = paged::row_of(a.pages, b, (uint32_t)at);
+                if (at >= 0) row = paged::row_of(a.pages, paged::place_of(a.pages, b, (uint32_t)at), 0u);
             }
             if ((threadIdx.x & 63) == 0) places[token] = row, known[token] = b >= 0;
         }

@@ -13,13 +13,19 @@ struct Pages {
     int64_t ld, width;
     uint32_t pages, heads, page, page_inverse;  // page_inverse: inverse_of(page)
 };
-// Row of the cache (head 0 of it: add page * head for others) that holds token `at` of a sequence, kNoRow without one.  at >= 0
-__device__ __forceinline__ uint32_t row_of(const Pages &p, int64_t sequence, uint32_t at) {
-    uint32_t in_page;
-    const uint32_t number = quotient(at, p.page, p.page_inverse, in_page);
-    if ((int64_t)number >= p.width) return kNoRow;
-    const uint32_t id = (uint32_t)p.table[sequence * p.ld + number];
-    return id < p.pages ? id * p.heads * p.page + in_page : kNoRow;
+// Where token `at` of a sequence is: the page's number, as the table has it (kNoRow beyond the table), and the place in it.  at >= 0
+struct Place {
+    uint32_t id, in_page;
+};
+__device__ __forceinline__ Place place_of(const Pages &p, int64_t sequence, uint32_t at) {
+    Place x;
+    const uint32_t number = quotient(at, p.page, p.page_inverse, x.in_page);
+    x.id = (int64_t)number < p.width ? (uint32_t)p.table[sequence * p.ld + number] : kNoRow;
+    return x;
+}
+// The row of the cache for a head, kNoRow without one.  (A step of its own: what asks for the number need not wait for it.)
+__device__ __forceinline__ uint32_t row_of(const Pages &p, const Place &x, uint32_t head) {
+    return x.id < p.pages ? (x.id * p.heads + head) * p.page + x.in_page : kNoRow;
 }
 inline Pages pages_of(const qnn_paged_cache &c) {
     return {c.table, c.ld_table, c.width, (uint32_t)c.pages, (uint32_t)c.heads, (uint32_t)c.page, inverse_of(c.page)};
