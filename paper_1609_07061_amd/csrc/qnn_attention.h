@@ -50,7 +50,7 @@ struct Args {
     float scale, cap;
     int64_t tokens, sequences;
     int32_t D, heads_q, group, splits, blocks;  // blocks: of rows, for each sequence and head of the cache
-    uint32_t group_inverse, heads_inverse, splits_inverse, blocks_inverse;
+    uint32_t group_inverse, heads_inverse, heads_q_inverse, splits_inverse, blocks_inverse;
     float *part;   // [splits][tokens][heads_q][D]: sums, where splits > 1
     float2 *state;  // [splits][tokens][heads_q]: R, sum of 2^(t - R)
 };
@@ -74,14 +74,20 @@ __device__ __forceinline__ h8 eight_codes(uint32_t x, uint32_t y) {
     return h8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
 }
 
-// tanh within some 5 units in the last place: 1 - 2 / (e^2x + 1), and the beginning of its series where that would lose digits
-__device__ __forceinline__ float tanh_of(float x) {
-    const float size = __uint_as_float(rows::magnitude(x)), a = size > 20.0f ? 20.0f : size, s = a * a;
-    const float far = 1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(a * (2.0f * kLog2e)));
+// Capped scores times log2(e): cap log2(e) tanh(x), from y = 2 log2(e) x.  1 - 2 / (e^2x + 1), off by 2^-23 of the cap; kClose (fp32 results): where |x| < 0.35 the
+// beginning of tanh's series instead, which keeps the digits of small scores.
+struct Cap {
+    float size, inverse;  // cap log2(e), 2 log2(e) / cap
+};
+__device__ __forceinline__ Cap cap_of(const Args &a) { return {a.cap * kLog2e, 2.0f * kLog2e / a.cap}; }
+template <bool kClose>
+__device__ __forceinline__ float capped(const Cap &c, float y) {
+    const float far = __fmaf_rn(-2.0f * c.size, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(y)), c.size);
+    if constexpr (!kClose) return far;
+    const float x = y * 0.34657359f, s = x * x;
     float near = __fmaf_rn(s, -8.86323553e-3f, 2.18694885e-2f);  // -1382 / 155925, 62 / 2835
     near = __fmaf_rn(s, near, -5.39682540e-2f), near = __fmaf_rn(s, near, 0.133333333f), near = __fmaf_rn(s, near, -0.333333333f);
-    near = __fmaf_rn(a * s, near, a);
-    return copysignf(a < 0.35f ? near : far, x);
+    return fabsf(x) < 0.35f ? c.size * __fmaf_rn(x * s, near, x) : far;
 }
 
 // A sequence as the kernels need it

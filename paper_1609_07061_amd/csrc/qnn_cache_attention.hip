@@ -11,6 +11,9 @@ namespace {
 
 constexpr int kStep = 32, kWaves = 4;
 
+// What sums that belong to one R are multiplied by for another one
+__device__ __forceinline__ float factor_of(float level, float top) { return level == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(level - top); }
+
 // Keys of a step, as a wave needs them: by the lane in memory order, in LDS
 struct __attribute__((aligned(16))) Keys {
     uint32_t row[kStep];
@@ -33,17 +36,22 @@ struct Query {
     static constexpr int kParts = Parts<T>::kQuery;
     h8 part[kParts][DP / 64][2];
     float mult;
-    __device__ __forceinline__ void load(const Args &a, const Row &row) {
+    T x[DP / 64][16];
+    __device__ __forceinline__ void ask(const Args &a, const Row &row) {
         const int g = (threadIdx.x & 63) >> 4;
-        T x[DP / 64][16];
-        uint32_t top = 0u;
 #pragma unroll
         for (int c = 0; c < DP / 64; ++c) {
             const int d = 64 * c + 16 * g;
             __builtin_memcpy(x[c], static_cast<const T *>(a.q) + row.token * a.ld_q + row.head * a.step_q + (d < a.D ? d : 0), sizeof x[c]);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) x[c][i] = d < a.D ? x[c][i] : (T)0.0f;
         }
+    }
+    __device__ __forceinline__ void make(const Args &a) {
+        const int g = (threadIdx.x & 63) >> 4;
+        uint32_t top = 0u;
+#pragma unroll
+        for (int c = 0; c < DP / 64; ++c)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[c][i] = 64 * c + 16 * g < a.D ? x[c][i] : (T)0.0f;
 #pragma unroll
         for (int c = 0; c < DP / 64; ++c) {
 #pragma unroll
@@ -94,15 +102,9 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NB, Parts<T>::kQuery)) vo
         const int64_t steps = (end + (int64_t)kStep - 1) / kStep;
         const int32_t lo = (int32_t)(steps * split / a.splits), hi = (int32_t)(steps * (split + 1) / a.splits);
 
+        const Cap cap = kMore && a.cap > 0.0f ? cap_of(a) : Cap{};
         Query<T, DP> query[NB];
         Sight sight[NB];
-#pragma unroll
-        for (int n = 0; n < NB; ++n) {
-            const Row row = row_at(a, s, min(first + 16u * n + r, last), head);
-            query[n].load(a, row);
-            sight[n].load(a, s, row);
-            query[n].mult *= kMore && a.cap > 0.0f ? 1.0f / a.cap : kLog2e;
-        }
         v4f out[DP / 16][NB] = {};
         float level[NB], total[NB];  // R; the sum of 2^(t - R) over this lane's keys
 #pragma unroll
@@ -203,7 +205,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NB, Parts<T>::kQuery)) vo
                         // (the scales first: a key that is not there has 0, and no product with it may overflow)
                         float x = dots[h][n][e] * (query[n].mult * k_scale[h][e]);
                         if constexpr (kMore) {
-                            if (a.cap > 0.0f) x = a.cap * kLog2e * tanh_of(x);
+                            if (a.cap > 0.0f) x = capped<kQuery == 2>(cap, x);
                             if (a.slopes) x = __fmaf_rn(sight[n].slope, (float)(k.place[16 * h + 4 * g + e] - sight[n].place), x);
                         }
                         t[h][e] = x + bias[h][e];
@@ -290,6 +292,12 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NB, Parts<T>::kQuery)) vo
             Ahead ahead;
             const int32_t step0 = lo + wave;
             paged::Place row = find(step0);
+#pragma unroll
+            for (int n = 0; n < NB; ++n) {
+                const Row of = row_at(a, s, min(first + 16u * n + r, last), head);
+                query[n].ask(a, of);
+                sight[n].load(a, s, of);
+            }
             scales(step0, row, ahead);
             row = find(step0 + kWaves);
             if (step0 < hi) {
@@ -299,6 +307,11 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NB, Parts<T>::kQuery)) vo
             }
             scales(step0 + kWaves, row, ahead);
             row = find(step0 + 2 * kWaves);
+#pragma unroll
+            for (int n = 0; n < NB; ++n) {
+                query[n].make(a);
+                query[n].mult *= kMore && a.cap > 0.0f ? cap.inverse : kLog2e;
+            }
             int turn = 0;
             for (int32_t step = step0; step < hi; step += kWaves) {
                 use_k();
@@ -326,7 +339,6 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NB, Parts<T>::kQuery)) vo
             for (int w = 1; w < kWaves; ++w) most = fmaxf(most, states[w][row].x);
             return most;
         };
-        auto factor_of = [](float level, float most) __attribute__((always_inline)) { return level == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(level - most); };
         auto put = [&](bool add) __attribute__((always_inline)) {
 #pragma unroll
             for (int n = 0; n < NB; ++n) {
@@ -373,58 +385,113 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NB, Parts<T>::kQuery)) vo
     }
 }
 
-// Parts of the keys joined: a workgroup for each query and head.  32 lanes (64 where a head is longer than 128) have a part's sums, 4 values a lane.
+// Parts of the keys joined.  32 lanes (64 where a head is longer than 128) take a query and head, 4 values a lane: up to 8 parts, all asked for at once.  Where there
+// are more, 256 / kLanes groups of lanes share them, 16 parts each at most.  (2 parts of 32768 rows of 128: 10.7 us, and 49.7 with a workgroup for each row.)
 template <typename T>
-__global__ __launch_bounds__(256) void join_kernel(const Args a) {
-    __shared__ float factors[kMostSplits], totals[4], tops[4];
-    __shared__ v4f sums[8][64];
-    const int tid = threadIdx.x;
-    const int64_t id = rows::block_number(), rows_all = a.tokens * a.heads_q;
-    if (id >= rows_all) return;
-    const int64_t token = id / a.heads_q, head = id % a.heads_q;
-    if (token < a.starts[0] || token >= a.starts[a.sequences]) return;
-    float level = -INFINITY, total = 0.0f;
-    if (tid < a.splits) {
-        const float2 x = a.state[tid * rows_all + id];
-        level = x.x, total = x.y;
+__device__ __forceinline__ void store_joined(const Args &a, int64_t token, int64_t head, int at, const v4f &y, float total) {
+    if (4 * at >= a.D) return;
+    struct Four {
+        T e[4];
+    } four;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        float x = total == 0.0f ? 0.0f : y[e] / total;
+        if constexpr (std::is_same<T, rows::f16>::value) asm("" : "+v"(x));  // (rounded from the value in fp32)
+        four.e[e] = (T)x;
     }
-    float top = level;
+    __builtin_memcpy(static_cast<T *>(a.out) + token * a.ld_out + head * a.step_out + 4 * at, &four, sizeof four);
+}
+template <typename T, int kLanes, int kParts>
+__global__ __launch_bounds__(256) void join_few_kernel(const Args a) {
+    const int at = threadIdx.x % kLanes;
+    const int64_t all = a.tokens * a.heads_q, id = (int64_t)rows::block_number() * (256 / kLanes) + threadIdx.x / kLanes;
+    if (id >= all) return;
+    uint32_t head;
+    const int64_t token = quotient((uint32_t)id, (uint32_t)a.heads_q, a.heads_q_inverse, head);
+    const float *const from = a.part + id * a.D + (4 * at < a.D ? 4 * at : 0);
+    float2 state[kParts];
+    v4f part[kParts];
+    // (parts beyond the last are the last again, and take no part; what was not written, because nothing was seen, neither)
+#pragma unroll
+    for (int s = 0; s < kParts; ++s) {
+        const int64_t from_part = min(s, a.splits - 1) * all;
+        state[s] = a.state[from_part + id], part[s] = *reinterpret_cast<const v4f *>(from + from_part * a.D);
+    }
+    if (token < a.starts[0] || token >= a.starts[a.sequences]) return;
+    float top = -INFINITY, total = 0.0f;
+    v4f y = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int s = 0; s < kParts; ++s) top = fmaxf(top, state[s].x);
+#pragma unroll
+    for (int s = 0; s < kParts; ++s) {
+        const float factor = s < a.splits ? factor_of(state[s].x, top) : 0.0f;
+        const bool none = s >= a.splits || state[s].y == 0.0f;
+        total = none ? total : __fmaf_rn(state[s].y, factor, total);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = none ? y[e] : __fmaf_rn(factor, part[s][e], y[e]);
+    }
+    store_joined<T>(a, token, head, at, y, total);
+}
+
+template <typename T, int kLanes>
+__global__ __launch_bounds__(256) void join_many_kernel(const Args a) {
+    constexpr int kTeams = 256 / kLanes, kPer = kMostSplits / kTeams;
+    __shared__ v4f sums[kTeams][kLanes];
+    const int lane = threadIdx.x & 63, at = threadIdx.x % kLanes, team = threadIdx.x / kLanes;
+    const int64_t all = a.tokens * a.heads_q, id = rows::block_number();
+    if (id >= all) return;
+    uint32_t head;
+    const int64_t token = quotient((uint32_t)id, (uint32_t)a.heads_q, a.heads_q_inverse, head);
+    // every wave reads all states, two a lane
+    float2 state[2];
+    v4f part[kPer];
+    const float *const from = a.part + id * a.D + (4 * at < a.D ? 4 * at : 0);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) state[i] = lane + 64 * i < a.splits ? a.state[(lane + 64 * i) * all + id] : make_float2(-INFINITY, 0.0f);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+        if (team + kTeams * i < a.splits) part[i] = *reinterpret_cast<const v4f *>(from + (team + kTeams * i) * all * a.D);
+    if (token < a.starts[0] || token >= a.starts[a.sequences]) return;
+    float top = fmaxf(state[0].x, state[1].x);
 #pragma unroll
     for (int d = 32; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-    if ((tid & 63) == 0) tops[tid >> 6] = top;
-    __syncthreads();
-    top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-    const float factor = level == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(level - top);
-    if (tid < a.splits) factors[tid] = total == 0.0f ? -1.0f : factor;  // (nothing there, and no sums written)
-    float sum = total * factor;
+    float factor[2], total = 0.0f;
 #pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) sum += __shfl_xor(sum, d);
-    if ((tid & 63) == 0) totals[tid >> 6] = sum;
-    __syncthreads();
-    sum = (totals[0] + totals[1]) + (totals[2] + totals[3]);
-    const int lanes = a.D > 128 ? 64 : 32, parts = 256 / lanes, part = tid / lanes, at = tid % lanes;
-    v4f y = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (4 * at < a.D)
-        for (int s = part; s < a.splits; s += parts)
-            if (!(factors[s] < 0.0f)) y += factors[s] * *reinterpret_cast<const v4f *>(a.part + (s * rows_all + id) * a.D + 4 * at);
-    sums[part][at] = y;
-    __syncthreads();
-    if (8 * tid < a.D) {
-        float z[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            float x = 0.0f;
-            for (int p = 0; p < parts; ++p) x += sums[p][2 * tid + e / 4][e % 4];
-            z[e] = sum == 0.0f ? 0.0f : x / sum;
-        }
-        store_eight<T>(a.out, token * a.ld_out + head * a.step_out + 8 * tid, z);
+    for (int i = 0; i < 2; ++i) {
+        factor[i] = factor_of(state[i].x, top);
+        total = __fmaf_rn(state[i].y, factor[i], total);
+        if (state[i].y == 0.0f) factor[i] = -1.0f;  // (nothing there)
     }
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) total += __shfl_xor(total, d);
+    v4f y = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int s = team + kTeams * i;
+        const float f = s < 64 ? __shfl(factor[0], s & 63) : __shfl(factor[1], s & 63);
+        if (s < a.splits && !(f < 0.0f)) y += f * part[i];
+    }
+    sums[team][at] = y;
+    __syncthreads();
+    if (team != 0) return;
+#pragma unroll
+    for (int t = 1; t < kTeams; ++t) y += sums[t][at];
+    store_joined<T>(a, token, head, at, y, total);
+}
+
+template <typename T>
+int launch_join(const Args &a, hipStream_t s) {
+    auto launch = [&](auto kernel, int rows) { return QNN_LAUNCH("cache_attention", kernel, rows::grid_of(ceil_div(a.tokens * a.heads_q, rows)), dim3(256), 0, s, a); };
+    auto few = [&](auto two, auto four, auto eight, int rows) { return launch(a.splits <= 2 ? two : (a.splits <= 4 ? four : eight), rows); };
+    if (a.splits > 8) return a.D <= 128 ? launch(join_many_kernel<T, 32>, 1) : launch(join_many_kernel<T, 64>, 1);
+    if (a.D <= 128) return few(join_few_kernel<T, 32, 2>, join_few_kernel<T, 32, 4>, join_few_kernel<T, 32, 8>, 8);
+    return few(join_few_kernel<T, 64, 2>, join_few_kernel<T, 64, 4>, join_few_kernel<T, 64, 8>, 4);
 }
 
 Plan plan_of(int64_t sequences, int64_t heads_q, int64_t heads, int64_t D, int type, int64_t most_new, int64_t longest) {
     Plan p;
     const int64_t rows = most_new * (heads_q / heads);
-    p.rows = rows <= 64 || !takes_many(D, type) ? (rows <= 16 || D > 128 ? 16 : 32) : many_rows(D);
+    p.rows = rows <= 256 || !takes_many(D, type) ? (rows <= 16 || D > 128 ? 16 : 32) : many_rows(D);
     p.blocks = ceil_div(rows, p.rows);
     // two workgroups a compute unit (one of the large ones), as long as a part has a step for every wave
     const int64_t have = sequences * heads * p.blocks, want = ceil_div((p.rows > 32 ? 1 : 2) * (int64_t)compute_units(), have);
@@ -506,7 +573,7 @@ extern "C" int qnn_cache_attention(const qnn_paged_cache *cache, const void *q, 
     a.pages = paged::pages_of(*cache), a.starts = cache->starts, a.lengths = cache->lengths, a.slopes = slopes, a.tree = tree, a.scale = scale, a.cap = cap;
     a.tokens = tokens, a.sequences = cache->sequences, a.D = (int32_t)D, a.heads_q = (int32_t)heads_q;
     a.group = (int32_t)(heads_q / cache->heads), a.splits = (int32_t)p.splits, a.blocks = (int32_t)p.blocks;
-    a.group_inverse = inverse_of(a.group), a.heads_inverse = inverse_of(cache->heads), a.splits_inverse = inverse_of(p.splits), a.blocks_inverse = inverse_of(p.blocks);
+    a.group_inverse = inverse_of(a.group), a.heads_inverse = inverse_of(cache->heads), a.heads_q_inverse = inverse_of(heads_q), a.splits_inverse = inverse_of(p.splits), a.blocks_inverse = inverse_of(p.blocks);
     a.part = part, a.state = reinterpret_cast<float2 *>(part + p.splits * queries * D);
     hipStream_t s = static_cast<hipStream_t>(stream);
     const dim3 grid = rows::grid_of((int64_t)blocks);
@@ -514,5 +581,5 @@ extern "C" int qnn_cache_attention(const qnn_paged_cache *cache, const void *q, 
                        ? attention::launch_many(a, type, grid, s)
                        : rows::with_type(type, [&](auto tag) { return attention::launch_few<decltype(tag)>(a, p.rows, grid, s); });
     if (rc || p.splits == 1) return rc;
-    return rows::with_type(type, [&](auto tag) { return QNN_LAUNCH(what, attention::join_kernel<decltype(tag)>, rows::grid_of(queries), dim3(256), 0, s, a); });
+    return rows::with_type(type, [&](auto tag) { return attention::launch_join<decltype(tag)>(a, s); });
 }

@@ -60,6 +60,7 @@ __global__ __launch_bounds__(64 * kWaves, kWaves / 4) void many_rows_kernel(cons
         // ---- the query: DP / 16 steps of 16 values, 8 g + 0 .. 7 of each in this lane
         h8 query[kQuery][DP / 16];
         float mult;
+        const Cap cap = kKind == 2 ? cap_of(a) : Cap{};
         Sight sight;
         {
             T x[DP / 16][8];
@@ -77,7 +78,7 @@ __global__ __launch_bounds__(64 * kWaves, kWaves / 4) void many_rows_kernel(cons
             }
             top = max(top, (uint32_t)__shfl_xor((int)top, 32));
             const Scaling scaling(top);
-            mult = scaling.mult(a.scale) * (kKind == 2 ? 1.0f / a.cap : kLog2e);
+            mult = scaling.mult(a.scale) * (kKind == 2 ? cap.inverse : kLog2e);
 #pragma unroll
             for (int c = 0; c < DP / 16; ++c)
 #pragma unroll
@@ -246,7 +247,7 @@ __global__ __launch_bounds__(64 * kWaves, kWaves / 4) void many_rows_kernel(cons
                 if constexpr (kKind > 0) scale(h);
                 if constexpr (kKind == 2) {
 #pragma unroll
-                    for (int x = 0; x < 16; ++x) dots[h][x] = a.cap * kLog2e * tanh_of(dots[h][x]);
+                    for (int x = 0; x < 16; ++x) dots[h][x] = capped<kQuery == 2>(cap, dots[h][x]);
                 }
                 if (kKind == 1 || (kKind == 2 && a.slopes)) {
                     const float place = (float)(sight.place - tile * kTile);  // (from the tile's beginning: whole numbers, exact)
