@@ -488,16 +488,19 @@ int launch_join(const Args &a, hipStream_t s) {
     return few(join_few_kernel<T, 64, 2>, join_few_kernel<T, 64, 4>, join_few_kernel<T, 64, 8>, 4);
 }
 
+// Few rows (up to 256 of a sequence and head of the cache): 16 or 32 a workgroup, and as many parts of the keys as fill the card, each the same number of steps for every
+// wave.  (us, bf16, 32 heads on 8 of 128: 64 sequences of up to 8192 tokens in one part each 163, in two 146, in three 148; one sequence of 10000 in 79 parts 17.)
+// Many rows: 128 or 256 a workgroup, one on a compute unit.  (16 sequences with 64 drafted tokens each, 256 rows: 79 on the kernel for few, 83 on the one for many;
+// 3 sequences with 700, 3500 rows of 80: 144 and 86.)
 Plan plan_of(int64_t sequences, int64_t heads_q, int64_t heads, int64_t D, int type, int64_t most_new, int64_t longest) {
     Plan p;
     const int64_t rows = most_new * (heads_q / heads);
-    p.rows = rows <= 256 || !takes_many(D, type) ? (rows <= 16 || D > 128 ? 16 : 32) : many_rows(D);
+    const bool few = rows <= 256 || !takes_many(D, type);
+    p.rows = few ? (rows <= 16 || D > 128 ? 16 : 32) : many_rows(D);
     p.blocks = ceil_div(rows, p.rows);
-    // two workgroups a compute unit (one of the large ones), as long as a part has a step for every wave
-    const int64_t have = sequences * heads * p.blocks, want = ceil_div((p.rows > 32 ? 1 : 2) * (int64_t)compute_units(), have);
-    const int64_t most = ceil_div(longest, p.rows > 32 ? 256 : kStep * kWaves);
-    p.splits = want < 1 ? 1 : (want < most ? want : most);
-    if (p.splits > kMostSplits) p.splits = kMostSplits;
+    const int64_t on_unit = few ? waves_of(D <= 64 ? 64 : (D <= 128 ? 128 : 256), p.rows / 16, 1) : 1;
+    const int64_t want = ceil_div(on_unit * compute_units(), sequences * heads * p.blocks), per_turn = few ? kStep * kWaves : 256, turns = ceil_div(longest, per_turn);
+    p.splits = ceil_div(turns, ceil_div(turns, want < kMostSplits ? want : kMostSplits));
     return p;
 }
 bool plannable(int64_t tokens, int64_t sequences, int64_t heads_q, int64_t heads, int64_t D, int64_t most_new, int64_t longest) {

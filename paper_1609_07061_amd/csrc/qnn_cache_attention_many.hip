@@ -184,7 +184,8 @@ __global__ __launch_bounds__(64 * kWaves, kWaves / 4) void many_rows_kernel(cons
         // ---- a tile's products.  Operands are read from LDS a group ahead; of a tile's two halves (32 keys each) the second's product with K runs beside the first's
         // weights, the first's product with V beside the second's: a wave's matrix instructions and its vector ones take turns, since the two waves of a SIMD, which
         // meet at a barrier every tile, would do the same at the same time.
-        constexpr int kOperands = DP / 16, kAhead = kQuery == 2 || DP > 128 ? 2 : 4;  // of K, of V, for 32 keys; as many ahead as registers allow
+        constexpr int kOperands = DP / 16, kOfK = kOperands * kQuery, kOfV = kOperands * kWeight;  // of K, of V, for 32 keys; products
+        constexpr int kAhead = kQuery == 2 || DP > 128 ? 2 : 4;                                    // as many as registers allow
         auto use = [&](int32_t number) __attribute__((always_inline)) {
             const int32_t tile = tile_at(number);
             const int lane = opaque(threadIdx.x & 63), r = lane & 31, g = lane >> 5;
@@ -195,43 +196,36 @@ __global__ __launch_bounds__(64 * kWaves, kWaves / 4) void many_rows_kernel(cons
             const bool scaled = kKind > 0 || masked;
             const float *const rest_k = scaled ? ones : sc.k;
             const float rest = scaled ? 1.0f : mult;
+            // operands: K's number c of half h at place (h kOperands + c) mod kAhead, V's likewise
             h8 of_k[kAhead], of_v[kAhead];
-            auto read_k = [&](int h, int c0) __attribute__((always_inline)) {
-#pragma unroll
-                for (int c = c0; c < c0 + kAhead && c < kOperands; ++c)
-                    of_k[c - c0] = *reinterpret_cast<const h8 *>(t.k + (32 * h + r) * DP * 2 + 16 * ((2 * c + g) ^ (r & 7)));
+            auto read_k = [&](int n) __attribute__((always_inline)) {
+                const int h = n / kOperands, c = n % kOperands;
+                if (n < 2 * kOperands) of_k[n % kAhead] = *reinterpret_cast<const h8 *>(t.k + (32 * h + r) * DP * 2 + 16 * ((2 * c + g) ^ (r & 7)));
             };
-            auto read_v = [&](int h, int x0) __attribute__((always_inline)) {  // operand x: step x / (DP / 32) of 16 keys, rows 32 (x mod DP / 32) on
-#pragma unroll
-                for (int x = x0; x < x0 + kAhead && x < kOperands; ++x) {
-                    const int c = x / (DP / 32), d = x % (DP / 32);
-                    of_v[x - x0] = *reinterpret_cast<const h8 *>(t.v + (32 * d + r) * kTile * 2 + 16 * ((2 * (2 * h + c) + g) ^ (r & 7)));
-                }
+            auto read_v = [&](int n) __attribute__((always_inline)) {  // step c of 16 keys, rows 32 d on
+                const int h = n / kOperands, c = n % kOperands / (DP / 32), d = n % (DP / 32);
+                if (n < 2 * kOperands) of_v[n % kAhead] = *reinterpret_cast<const h8 *>(t.v + (32 * d + r) * kTile * 2 + 16 * ((2 * (2 * h + c) + g) ^ (r & 7)));
             };
             v16f dots[2];  // key 32 h + 8 e + 4 g + i is value 4 e + i of half h
             h8 weights[2][kWeight][2];
             float sum, largest;
             auto four = [&](const float *from, int h, int e) __attribute__((always_inline)) { return *reinterpret_cast<const v4f *>(from + 32 * h + 8 * e + 4 * g); };
-            auto with_k = [&](int h) __attribute__((always_inline)) {
-                dots[h] = v16f{};
+            // the j-th eighth of the products of half h
+            auto with_k = [&](int h, int j) __attribute__((always_inline)) {
 #pragma unroll
-                for (int c0 = 0; c0 < kOperands; c0 += kAhead) {
-                    if (c0 > 0) read_k(h, c0);
-#pragma unroll
-                    for (int c = c0; c < c0 + kAhead && c < kOperands; ++c)
-#pragma unroll
-                        for (int p = 0; p < kQuery; ++p) dots[h] = __builtin_amdgcn_mfma_f32_32x32x16_f16(of_k[c - c0], query[p][c], dots[h], 0, 0, 0);
+                for (int m = kOfK * j / 8; m < kOfK * (j + 1) / 8; ++m) {
+                    const int n = h * kOperands + m / kQuery, p = m % kQuery;
+                    if (m == 0) dots[h] = v16f{};
+                    dots[h] = __builtin_amdgcn_mfma_f32_32x32x16_f16(of_k[n % kAhead], query[p][n % kOperands], dots[h], 0, 0, 0);
+                    if (p == kQuery - 1) read_k(n + kAhead);
                 }
             };
-            auto with_v = [&](int h) __attribute__((always_inline)) {
+            auto with_v = [&](int h, int j) __attribute__((always_inline)) {
 #pragma unroll
-                for (int x0 = 0; x0 < kOperands; x0 += kAhead) {
-                    if (x0 > 0) read_v(h, x0);
-#pragma unroll
-                    for (int x = x0; x < x0 + kAhead && x < kOperands; ++x)
-#pragma unroll
-                        for (int q = 0; q < kWeight; ++q)
-                            out[x % (DP / 32)] = __builtin_amdgcn_mfma_f32_32x32x16_f16(of_v[x - x0], weights[h][q][x / (DP / 32)], out[x % (DP / 32)], 0, 0, 0);
+                for (int m = kOfV * j / 8; m < kOfV * (j + 1) / 8; ++m) {
+                    const int n = h * kOperands + m / kWeight, q = m % kWeight, d = n % (DP / 32);
+                    out[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(of_v[n % kAhead], weights[h][q][n % kOperands / (DP / 32)], out[d], 0, 0, 0);
+                    if (q == kWeight - 1) read_v(n + kAhead);
                 }
             };
             auto scale = [&](int h) __attribute__((always_inline)) {
@@ -281,25 +275,23 @@ __global__ __launch_bounds__(64 * kWaves, kWaves / 4) void many_rows_kernel(cons
                     }
                 }
             };
-            // weights from R on, their sum without the values' scales, and the largest
-            auto weigh = [&](int h) __attribute__((always_inline)) {
-                const float from = level == -INFINITY ? 0.0f : level;
-                sum = 0.0f, largest = 0.0f;
+            // weights from R on, their sum without the values' scales, and the largest: the j-th eighth, two of a lane
+            float from;
+            auto begin = [&]() __attribute__((always_inline)) { from = level == -INFINITY ? 0.0f : level, sum = 0.0f, largest = 0.0f; };
+            auto weigh = [&](int h, int j) __attribute__((always_inline)) {
+                const int e = j / 2;
+                const v4f v = four(sc.v, h, e);
+                v4f k;
+                if constexpr (kKind == 0) k = four(rest_k, h, e);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const v4f v = four(sc.v, h, e);
-                    v4f k;
-                    if constexpr (kKind == 0) k = four(rest_k, h, e);
+                for (int i = 2 * (j & 1); i < 2 * (j & 1) + 2; ++i) {
+                    const float x = dots[h][4 * e + i], p = __builtin_amdgcn_exp2f(kKind == 0 ? __fmaf_rn(x, rest * k[i], -from) : x - from);
+                    const float w = p * v[i];
+                    sum += p, largest = fmaxf(largest, fabsf(w));
+                    _Float16 y[kWeight];
+                    attention::split(w, y);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float x = dots[h][4 * e + i], p = __builtin_amdgcn_exp2f(kKind == 0 ? __fmaf_rn(x, rest * k[i], -from) : x - from);
-                        const float w = p * v[i];
-                        sum += p, largest = fmaxf(largest, fabsf(w));
-                        _Float16 y[kWeight];
-                        attention::split(w, y);
-#pragma unroll
-                        for (int q = 0; q < kWeight; ++q) weights[h][q][e >> 1][4 * (e & 1) + i] = y[q];
-                    }
+                    for (int q = 0; q < kWeight; ++q) weights[h][q][e >> 1][4 * (e & 1) + i] = y[q];
                 }
             };
             // moves R where a weight would be too large, which is seldom, and takes the half's sum in
@@ -321,39 +313,38 @@ __global__ __launch_bounds__(64 * kWaves, kWaves / 4) void many_rows_kernel(cons
                     total *= factor;
 #pragma unroll
                     for (int d = 0; d < DP / 32; ++d) out[d] *= factor;
-                    weigh(h);
+                    begin();
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) weigh(h, j);
                 }
                 total += sum;
             };
-            // kVector vector instructions after each matrix one
-            auto in_turn = [](auto matrix, auto vector) __attribute__((always_inline)) {
 #pragma unroll
-                for (int i = 0; i < decltype(matrix)::value; ++i) {
-                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                    __builtin_amdgcn_sched_group_barrier(0x002, decltype(vector)::value, 0);
-                }
-                __builtin_amdgcn_sched_barrier(0);
-            };
-            typedef std::integral_constant<int, kOperands * kQuery> OfK;
-            typedef std::integral_constant<int, kOperands * kWeight> OfV;
-            read_k(0, 0);
-            __builtin_amdgcn_sched_barrier(0);
-            with_k(0);
-            read_k(1, 0);
-            read_v(0, 0);
-            __builtin_amdgcn_sched_barrier(0);
+            for (int n = 0; n < kAhead; ++n) read_k(n);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) with_k(0, j);
+#pragma unroll
+            for (int n = 0; n < kAhead; ++n) read_v(n);
             score(0);
-            with_k(1);
-            weigh(0);
-            in_turn(OfK{}, std::integral_constant<int, 112 / (kOperands * kQuery)>{});
+            __builtin_amdgcn_sched_barrier(0);
+            begin();
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                with_k(1, j);
+                weigh(0, j);
+            }
             settle(0);
             score(1);
-            with_v(0);
-            weigh(1);
-            in_turn(OfV{}, std::integral_constant<int, 112 / (kOperands * kWeight)>{});
-            read_v(1, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            begin();
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                with_v(0, j);
+                weigh(1, j);
+            }
             settle(1);
-            with_v(1);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) with_v(1, j);
         };
 
         __syncthreads();  // (the rows before are done with LDS)
