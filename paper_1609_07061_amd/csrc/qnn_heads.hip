@@ -223,7 +223,7 @@ __global__ __launch_bounds__(kThreads) void heads_kernel(const HeadsArgs a) {
             uint32_t top = 0u;
 #pragma unroll
             for (int i = 0; i < kVec; ++i) top = max(top, lane.on ? max(magnitude(x[i]), magnitude(y[i])) : 0u);
-            const Quantizer quantizer(most_of_head<G>(top), 1.0f);
+            const ExactQuantizer quantizer(most_of_head<G>(top), 1.0f);
             const uint32_t place = places[now.token], head = now.head - (uint32_t)(a.heads_q + (k ? 0 : a.heads_k));
             if (place != kNoRow && lane.on) {
                 const uint32_t row = place + head * a.pages.page;

@@ -115,8 +115,28 @@ struct Quantizer {
         return zero ? 0u : code(a) | code(b) << 8 | code(c) << 16 | code(d) << 24;
     }
 };
-template <bool kShort>
-__device__ __forceinline__ void store_codes(int8_t *row, const Window &at, int64_t K, const Quantizer &q, const float (&v)[kVec]) {
+// The same for values that are the caller's own, not this library's arithmetic, and often have few digits: v 127 / a lies on the middle between two codes now and then,
+// where (v pre) mul, which is off by up to 2^-15.4, says little.  There 254 |v| is compared with (2 f + 1) a, both exact in 64 bits.
+struct ExactQuantizer : Quantizer {
+    float top;
+    __device__ __forceinline__ ExactQuantizer(uint32_t top_bits, float factor) : Quantizer(top_bits, factor), top(__uint_as_float(top_bits)) {}
+    __device__ __forceinline__ uint32_t code(float v) const {
+        const float u = v * pre * mul, n = rintf(u);
+        int c = (int)n;
+        if (fabsf(fabsf(u - n) - 0.5f) < 0x1p-14f) {
+            const int f = (int)fabsf(u);
+            const double a = 254.0 * fabs((double)v), b = (2.0 * f + 1.0) * (double)top;
+            const int size = a > b || (a == b && (f & 1)) ? f + 1 : f;
+            c = v < 0.0f ? -size : size;
+        }
+        return (uint32_t)c & 0xFFu;
+    }
+    __device__ __forceinline__ uint32_t four(float a, float b, float c, float d) const {
+        return zero ? 0u : code(a) | code(b) << 8 | code(c) << 16 | code(d) << 24;
+    }
+};
+template <bool kShort, typename Q>
+__device__ __forceinline__ void store_codes(int8_t *row, const Window &at, int64_t K, const Q &q, const float (&v)[kVec]) {
     const uint32_t w[2] = {q.four(v[0], v[1], v[2], v[3]), q.four(v[4], v[5], v[6], v[7])};
     if (!kShort && at.skip == 0) {
         __builtin_memcpy(row + at.from, w, sizeof w);
@@ -214,6 +234,16 @@ static __global__ __launch_bounds__(1024) void add_parts_kernel(const AddParts o
 
 constexpr int rows_per_block(int threads) { return threads >= 256 ? 1 : 256 / threads; }
 
+// The quantizer of a source's rows: exact where it says so
+template <typename Source, typename = void>
+struct QuantizerOf {
+    typedef Quantizer type;
+};
+template <typename Source>
+struct QuantizerOf<Source, std::enable_if_t<Source::kExact>> {
+    typedef ExactQuantizer type;
+};
+
 // One row per kThreads lanes.  Source: `load<kShort>(row, window, K, values, kept)` the values to be quantized, up to the factor `factor(sum)`;
 // `add(kept, i, sum)` the sum with value i's part; `keep<kShort>(row, window, K, kept)` writes what else it does.
 // kPer: windows that a lane keeps in registers; 0: as many as there are, loaded a second time for the codes.
@@ -236,7 +266,8 @@ __global__ __launch_bounds__(kThreads >= 256 ? kThreads : 256) void quant_rows_k
             s.top = max(s.top, mine ? magnitude(v[i][e]) : 0u);
         }
     };
-    auto give = [&](const Quantizer &q, int i, const Window &w) __attribute__((always_inline)) {
+    typedef typename QuantizerOf<Source>::type Q;
+    auto give = [&](const Q &q, int i, const Window &w) __attribute__((always_inline)) {
         src.template keep<kShort>(row, w, K, kept[i]);
         store_codes<kShort>(codes + row * ld_codes, w, K, q, v[i]);
     };
@@ -252,7 +283,7 @@ __global__ __launch_bounds__(kThreads >= 256 ? kThreads : 256) void quant_rows_k
         }
     }
     s = across<kThreads>(s, SumTop::join, shared, 0);
-    const Quantizer q(s.top, src.factor(s.sum, K));
+    const Q q(s.top, src.factor(s.sum, K));
     if (lane == 0) scale[row] = q.scale;
     if constexpr (kPer > 0) {
 #pragma unroll

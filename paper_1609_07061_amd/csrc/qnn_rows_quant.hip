@@ -12,6 +12,7 @@ using namespace rows;
 template <typename T, bool kOnce>
 struct PlainSource {
     struct Kept {};
+    static constexpr bool kExact = true;
     const T *x;
     int64_t ldx;
     template <bool kShort>

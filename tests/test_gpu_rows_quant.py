@@ -46,3 +46,23 @@ def test_beyond_the_caches(seed):
     for part in (slice(0, 100), slice(19900, 20000)):
         again = q.qnn_rows_quant(x[part])
         assert torch.equal(again[0], codes[part]) and torch.equal(again[1], scale[part])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_codes_are_the_definition(seed, dtype):
+    """Values of few digits, of which v 127 / max is often the middle between two codes: every code is rint(v 127 / max) in exact arithmetic, ties to even."""
+    import paper_1609_07061_amd as q
+
+    g = generator(seed, 11)
+    m = torch.randint(-128, 129, (64, 2048), generator=g, device="cuda").double()
+    x = (m * 2.0 ** torch.randint(-9, 4, (64, 1), generator=g, device="cuda").double()).to(dtype)
+    x[:, 0] = x[:, 0].abs().clamp(min=1)
+    y = x.double()
+    # in whole numbers: 254 |v| against (2 f + 1) max, in units of the row's power of two
+    top = y.abs().amax(dim=1, keepdim=True)
+    f = torch.floor(y.abs() * 127 / top)
+    f = torch.where((f + 1) * top <= 127 * y.abs(), f + 1, torch.where(f * top > 127 * y.abs(), f - 1, f))
+    a, b = 254 * y.abs(), (2 * f + 1) * top
+    size = torch.where((a > b) | ((a == b) & (f % 2 == 1)), f + 1, f)
+    assert int((a == b).sum()) > 100
+    assert torch.equal(q.qnn_rows_quant(x)[0].double(), torch.sign(y) * size)
