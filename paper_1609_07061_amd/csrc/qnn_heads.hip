@@ -118,6 +118,13 @@ __device__ __forceinline__ void load_gamma(const void *gamma, bool is_f32, const
     load_either<false, T>(gamma, is_f32, Window(l.second, D), D, y);
 }
 
+// norm_factor of a head, from the sum of its squares: the root's reciprocal within a unit in the last place, without a root and a quotient
+__device__ __forceinline__ float head_factor(float total, float inverse_D, float eps) {
+    const float mean = __fmaf_rn(total, inverse_D, eps);
+    if (mean < 0x1p-126f) return __uint_as_float(0x7F800000u);
+    return magnitude(mean) < 0x7F800000u ? __builtin_amdgcn_rsqf(mean) : __uint_as_float(0x7FC00000u);
+}
+
 // Sequence of a token: the last that begins at or before it, found by a whole wave, 64 beginnings at a time.  -1: none
 __device__ __forceinline__ int64_t sequence_of(const int32_t *starts, int64_t sequences, int64_t token) {
     int64_t lo = 0, n = sequences;
@@ -137,7 +144,7 @@ struct HeadsArgs {
     Matrix q, k, v, q_out, k_out;
     const void *gamma_q, *gamma_k;
     bool gamma_f32;
-    float eps;
+    float eps, inverse_D;
     Angles angles;
     int64_t tokens;
     int32_t D, heads_q, heads_k, per_block;  // per_block: tokens of a workgroup
@@ -152,88 +159,99 @@ struct HeadsArgs {
 
 constexpr int kMostTokens = 4;
 
-template <typename T, int G, bool kAppend>
+// kOnce: past the caches (beyond_caches)
+template <typename T, int G, bool kAppend, bool kOnce>
 __global__ __launch_bounds__(kThreads) void heads_kernel(const HeadsArgs a) {
     __shared__ float2 turns[kMostTokens][kMostPairs];
     __shared__ uint32_t places[kMostTokens];
     __shared__ bool known[kMostTokens];  // to a sequence
-    const int64_t t0 = (int64_t)block_number() * a.per_block;
-    const int n_tokens = (int)(a.tokens - t0 < a.per_block ? a.tokens - t0 : a.per_block);
-    if (n_tokens <= 0) return;  // (of the launch's last line)
     const int unit = threadIdx.x % G;
     const Lane lane(unit, a.D, a.angles);
     const Window first(lane.first, a.D), second(lane.second, a.D);
-    const uint32_t heads = (uint32_t)(a.heads_q + (kAppend ? 2 : 1) * a.heads_k), items = (uint32_t)n_tokens * heads;
-    struct Item {
-        uint32_t token, head;
-        Raw<T> x, y;
-    };
-    auto load = [&](uint32_t n, Item &i) __attribute__((always_inline)) {
-        if (n >= items) return;
-        i.token = quotient(n, heads, a.heads_inverse, i.head);
-        const bool q = i.head < (uint32_t)a.heads_q, k = i.head < (uint32_t)(a.heads_q + a.heads_k);
-        const Matrix &m = q ? a.q : (k ? a.k : a.v);
-        const T *const from = m.at<const T>(t0 + i.token, i.head - (q ? 0u : (k ? (uint32_t)a.heads_q : (uint32_t)(a.heads_q + a.heads_k))));
-        i.x = load_raw<false, false>(from, first, a.D);
-        i.y = load_raw<false, false>(from, second, a.D);
-    };
-    Item now, next;
-    uint32_t n = threadIdx.x / G;
-    load(n, now);
-    if constexpr (kAppend) {
-        const int token = threadIdx.x >> 6;
-        if (token < n_tokens) {
-            const int64_t t = t0 + token, b = sequence_of(a.starts, a.sequences, t);
-            uint32_t row = kNoRow;
-            if (b >= 0) {
-                const int64_t at = (int64_t)a.lengths[b] - (a.starts[b + 1] - t);
-                if (at >= 0) row = paged::row_of(a.pages, paged::place_of(a.pages, b, (uint32_t)at), 0u);
-            }
-            if ((threadIdx.x & 63) == 0) places[token] = row, known[token] = b >= 0;
-        }
+    const uint32_t heads = (uint32_t)(a.heads_q + (kAppend ? 2 : 1) * a.heads_k);
+    // (the weights stay in registers: asked for with an item, they would come behind the next one's values, which would be waited for)
+    float gamma[2][2][kVec];
+    if (a.gamma_q) {
+        load_gamma<T>(a.gamma_q, a.gamma_f32, lane, a.D, gamma[0][0], gamma[0][1]);
+        load_gamma<T>(a.heads_k > 0 ? a.gamma_k : a.gamma_q, a.gamma_f32, lane, a.D, gamma[1][0], gamma[1][1]);
     }
-    turns_of(a.angles, t0, n_tokens, turns);
-    __syncthreads();
-    for (; n < items; n += kThreads / G) {
-        load(n + kThreads / G, next);
-        const bool q = now.head < (uint32_t)a.heads_q, k = now.head < (uint32_t)(a.heads_q + a.heads_k);
-        float x[kVec], y[kVec];
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) x[i] = lane.on ? (float)now.x.e[i] : 0.0f, y[i] = lane.on ? (float)now.y.e[i] : 0.0f;
-        if (!kAppend || q || k) {
-            if (a.gamma_q) {
-                float sum = 0.0f, gx[kVec], gy[kVec];
-                load_gamma<T>(q ? a.gamma_q : a.gamma_k, a.gamma_f32, lane, a.D, gx, gy);
-#pragma unroll
-                for (int i = 0; i < kVec; ++i) sum = __fmaf_rn(x[i], x[i], sum), sum = __fmaf_rn(y[i], y[i], sum);
-                const float r = norm_factor(sum_of_head<G>(sum), a.D, a.eps);
-#pragma unroll
-                for (int i = 0; i < kVec; ++i) x[i] = x[i] * r * gx[i], y[i] = y[i] * r * gy[i];
-            }
-            turn<1>(lane, turns[now.token], x, y);
-        }
-        if (!kAppend || q) {
-            const Matrix &m = q ? a.q_out : a.k_out;
-            T *const to = m.at<T>(t0 + now.token, now.head - (q ? 0u : (uint32_t)a.heads_q));
-            if (lane.on && (!kAppend || known[now.token])) {
-                store_values<false, false>(to, first, a.D, x);
-                store_values<false, false>(to, second, a.D, y);
-            }
-        } else {
-            uint32_t top = 0u;
-#pragma unroll
-            for (int i = 0; i < kVec; ++i) top = max(top, lane.on ? max(magnitude(x[i]), magnitude(y[i])) : 0u);
-            const ExactQuantizer quantizer(most_of_head<G>(top), 1.0f);
-            const uint32_t place = places[now.token], head = now.head - (uint32_t)(a.heads_q + (k ? 0 : a.heads_k));
-            if (place != kNoRow && lane.on) {
-                const uint32_t row = place + head * a.pages.page;
-                int8_t *const to = (k ? a.codes_k : a.codes_v) + (int64_t)row * a.D;
-                store_codes<false>(to, first, a.D, quantizer, x);
-                store_codes<false>(to, second, a.D, quantizer, y);
-                if (unit == 0) (k ? a.scale_k : a.scale_v)[row] = quantizer.scale;
+    for (int64_t t0 = (int64_t)blockIdx.x * a.per_block; t0 < a.tokens; t0 += (int64_t)gridDim.x * a.per_block) {
+        const int n_tokens = (int)(a.tokens - t0 < a.per_block ? a.tokens - t0 : a.per_block);
+        const uint32_t items = (uint32_t)n_tokens * heads;
+        struct Item {
+            uint32_t token, head;
+            Raw<T> x, y;
+        };
+        auto load = [&](uint32_t n, Item &i) __attribute__((always_inline)) {
+            if (n >= items) return;
+            i.token = quotient(n, heads, a.heads_inverse, i.head);
+            const bool q = i.head < (uint32_t)a.heads_q, k = i.head < (uint32_t)(a.heads_q + a.heads_k);
+            const Matrix &m = q ? a.q : (k ? a.k : a.v);
+            const T *const from = m.at<const T>(t0 + i.token, i.head - (q ? 0u : (k ? (uint32_t)a.heads_q : (uint32_t)(a.heads_q + a.heads_k))));
+            i.x = load_raw<kOnce, false>(from, first, a.D);
+            i.y = load_raw<kOnce, false>(from, second, a.D);
+        };
+        Item now, next;
+        uint32_t n = threadIdx.x / G;
+        load(n, now);
+        __syncthreads();  // (the turns and places of the group before are read)
+        if constexpr (kAppend) {
+            const int token = threadIdx.x >> 6;
+            if (token < n_tokens) {
+                const int64_t t = t0 + token, b = sequence_of(a.starts, a.sequences, t);
+                uint32_t row = kNoRow;
+                if (b >= 0) {
+                    const int64_t at = (int64_t)a.lengths[b] - (a.starts[b + 1] - t);
+                    if (at >= 0) row = paged::row_of(a.pages, paged::place_of(a.pages, b, (uint32_t)at), 0u);
+                }
+                if ((threadIdx.x & 63) == 0) places[token] = row, known[token] = b >= 0;
             }
         }
-        now = next;
+        turns_of(a.angles, t0, n_tokens, turns);
+        __syncthreads();
+        for (; n < items; n += kThreads / G) {
+            load(n + kThreads / G, next);
+            const bool q = now.head < (uint32_t)a.heads_q, k = now.head < (uint32_t)(a.heads_q + a.heads_k);
+            float x[kVec], y[kVec];
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) x[i] = lane.on ? (float)now.x.e[i] : 0.0f, y[i] = lane.on ? (float)now.y.e[i] : 0.0f;
+            if (!kAppend || q || k) {
+                if (a.gamma_q) {
+                    float sum = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < kVec; ++i) sum = __fmaf_rn(x[i], x[i], sum), sum = __fmaf_rn(y[i], y[i], sum);
+                    const float r = head_factor(sum_of_head<G>(sum), a.inverse_D, a.eps);
+#pragma unroll
+                    for (int i = 0; i < kVec; ++i) {
+                        x[i] = x[i] * r * (q ? gamma[0][0][i] : gamma[1][0][i]);
+                        y[i] = y[i] * r * (q ? gamma[0][1][i] : gamma[1][1][i]);
+                    }
+                }
+                turn<1>(lane, turns[now.token], x, y);
+            }
+            if (!kAppend || q) {
+                const Matrix &m = q ? a.q_out : a.k_out;
+                T *const to = m.at<T>(t0 + now.token, now.head - (q ? 0u : (uint32_t)a.heads_q));
+                if (lane.on && (!kAppend || known[now.token])) {
+                    store_values<kOnce, false>(to, first, a.D, x);
+                    store_values<kOnce, false>(to, second, a.D, y);
+                }
+            } else {
+                uint32_t top = 0u;
+#pragma unroll
+                for (int i = 0; i < kVec; ++i) top = max(top, lane.on ? max(magnitude(x[i]), magnitude(y[i])) : 0u);
+                const ExactQuantizer quantizer(most_of_head<G>(top), 1.0f);
+                const uint32_t place = places[now.token], head = now.head - (uint32_t)(a.heads_q + (k ? 0 : a.heads_k));
+                if (place != kNoRow && lane.on) {
+                    const uint32_t row = place + head * a.pages.page;
+                    int8_t *const to = (k ? a.codes_k : a.codes_v) + (int64_t)row * a.D;
+                    store_codes<false>(to, first, a.D, quantizer, x);
+                    store_codes<false>(to, second, a.D, quantizer, y);
+                    if (unit == 0) (k ? a.scale_k : a.scale_v)[row] = quantizer.scale;
+                }
+            }
+            now = next;
+        }
     }
 }
 
@@ -243,7 +261,7 @@ struct HeadsGradArgs {
     Matrix grad[2], h[2], out[2];
     const void *gamma[2];
     bool gamma_f32;
-    float eps;
+    float eps, inverse_D;
     Angles angles;
     int64_t tokens;
     int32_t D, per_block, heads[2], blocks[2];
@@ -251,7 +269,7 @@ struct HeadsGradArgs {
     float *parts;
 };
 
-template <typename T, int G>
+template <typename T, int G, bool kOnce>
 __global__ __launch_bounds__(kThreads) void heads_backward_kernel(const HeadsGradArgs a) {
     __shared__ float2 turns[kMostTokens][kMostPairs];
     __shared__ float joined[kThreads][17];
@@ -276,11 +294,11 @@ __global__ __launch_bounds__(kThreads) void heads_backward_kernel(const HeadsGra
             uint32_t head;
             const uint32_t token = quotient(n, heads, heads_inverse, head);
             const T *const from = grad.at<const T>(t0 + token, head);
-            const Raw<T> g0 = load_raw<false, false>(from, first, a.D), g1 = load_raw<false, false>(from, second, a.D);
+            const Raw<T> g0 = load_raw<kOnce, false>(from, first, a.D), g1 = load_raw<kOnce, false>(from, second, a.D);
             Raw<T> h0, h1;
             if (gamma) {
                 const T *const values = h.at<const T>(t0 + token, head);
-                h0 = load_raw<false, false>(values, first, a.D), h1 = load_raw<false, false>(values, second, a.D);
+                h0 = load_raw<kOnce, false>(values, first, a.D), h1 = load_raw<kOnce, false>(values, second, a.D);
             }
             float x[kVec], y[kVec];
 #pragma unroll
@@ -294,7 +312,7 @@ __global__ __launch_bounds__(kThreads) void heads_backward_kernel(const HeadsGra
                     sum = __fmaf_rn(u[i], u[i], sum), sum = __fmaf_rn(v[i], v[i], sum);
                     dot = __fmaf_rn(gx[i] * x[i], u[i], dot), dot = __fmaf_rn(gy[i] * y[i], v[i], dot);
                 }
-                const float r = norm_factor(sum_of_head<G>(sum), a.D, a.eps), c = r * r * (sum_of_head<G>(dot) / (float)a.D);
+                const float r = head_factor(sum_of_head<G>(sum), a.inverse_D, a.eps), c = r * r * (sum_of_head<G>(dot) * a.inverse_D);
 #pragma unroll
                 for (int i = 0; i < kVec; ++i) {
                     sx[i] = __fmaf_rn(x[i], u[i] * r, sx[i]), sy[i] = __fmaf_rn(y[i], v[i] * r, sy[i]);
@@ -303,8 +321,8 @@ __global__ __launch_bounds__(kThreads) void heads_backward_kernel(const HeadsGra
             }
             if (lane.on) {
                 T *const to = out.at<T>(t0 + token, head);
-                store_values<false, false>(to, first, a.D, x);
-                store_values<false, false>(to, second, a.D, y);
+                store_values<kOnce, false>(to, first, a.D, x);
+                store_values<kOnce, false>(to, second, a.D, y);
             }
         }
     }
@@ -322,7 +340,7 @@ __global__ __launch_bounds__(kThreads) void heads_backward_kernel(const HeadsGra
     }
 }
 
-constexpr int64_t kMostBlocks = 1024;
+constexpr int64_t kResident = 4, kMostBlocks = 1024;  // workgroups of heads_kernel on a compute unit; of the gradient, at most
 
 // Workgroups of the two sides: in proportion to their heads, and so that all have the same number of groups or one less
 struct Split {
@@ -337,8 +355,9 @@ Split split_of(int64_t tokens, int64_t heads_q, int64_t heads_k, int64_t per_blo
     };
     return {of(heads_q), of(heads_k)};
 }
-// Tokens of a workgroup: one while there are few, so that they spread over the card
+// Tokens that a workgroup takes at a time: one while there are few, so that they spread over the card
 int tokens_per_block(int64_t tokens) { return tokens < 4 * 1024 ? 1 : kMostTokens; }
+int tokens_per_group(int64_t tokens) { return tokens < 512 ? 1 : kMostTokens; }  // of the gradient
 
 int check_heads(const char *what, const Matrix &m, int64_t heads, int64_t D, int64_t tokens, int type) {
     if (heads == 0) return QNN_OK;
@@ -387,10 +406,17 @@ template <bool kAppend>
 int launch_heads(const char *what, int type, HeadsArgs a, hipStream_t s) {
     a.per_block = tokens_per_block(a.tokens);
     a.heads_inverse = inverse_of(a.heads_q + (kAppend ? 2 : 1) * a.heads_k);
-    const dim3 grid = grid_of(ceil_div(a.tokens, a.per_block));
+    // as many workgroups as are resident, each with the same number of groups of tokens or one less
+    const int64_t groups = ceil_div(a.tokens, a.per_block);
+    const dim3 grid((unsigned)ceil_div(groups, ceil_div(groups, kResident * (int64_t)compute_units())));
     return with_type(type, [&](auto tag) {
         typedef decltype(tag) T;
-        return with_lanes(a.D, [&](auto lanes) { return QNN_LAUNCH(what, (heads_kernel<T, decltype(lanes)::value, kAppend>), grid, dim3(kThreads), 0, s, a); });
+        return with_lanes(a.D, [&](auto lanes) {
+            constexpr int G = decltype(lanes)::value;
+            const double values = 2.0 * (double)a.tokens * a.D * (a.heads_q + a.heads_k);
+            auto kernel = beyond_caches(sizeof(T) * values) ? heads_kernel<T, G, kAppend, true> : heads_kernel<T, G, kAppend, false>;
+            return QNN_LAUNCH(what, kernel, grid, dim3(kThreads), 0, s, a);
+        });
     });
 }
 
@@ -413,13 +439,13 @@ extern "C" int qnn_qk_norm_rotate(const void *q, int64_t ld_q, int64_t step_q, i
         if (int rc = check_heads(what, *m, heads_k, D, tokens, type)) return rc;
     if (int rc = check_rotation_pointers(what, *rotation)) return rc;
     a.gamma_q = gamma_q ? gamma_q : gamma_k, a.gamma_k = gamma_k, a.gamma_f32 = gamma_type == QNN_F32, a.eps = eps;
-    a.angles = angles_of(*rotation), a.tokens = tokens, a.D = (int32_t)D, a.heads_q = (int32_t)heads_q, a.heads_k = (int32_t)heads_k;
+    a.angles = angles_of(*rotation), a.tokens = tokens, a.D = (int32_t)D, a.inverse_D = 1.0f / (float)D, a.heads_q = (int32_t)heads_q, a.heads_k = (int32_t)heads_k;
     return launch_heads<false>(what, type, a, static_cast<hipStream_t>(stream));
 }
 
 extern "C" size_t qnn_qk_norm_rotate_backward_workspace_bytes(int64_t tokens, int64_t heads_q, int64_t heads_k, int64_t D) {
     if (tokens < 1 || heads_q < 0 || heads_k < 0 || heads_q + heads_k < 1 || D < 16 || D > paged::kMostD) return 0;
-    const Split s = split_of(tokens, heads_q, heads_k, tokens_per_block(tokens));
+    const Split s = split_of(tokens, heads_q, heads_k, tokens_per_group(tokens));
     return (size_t)(s.q + s.k) * (size_t)D * 4;
 }
 
@@ -452,8 +478,8 @@ extern "C" int qnn_qk_norm_rotate_backward(const void *grad_q, int64_t ld_grad_q
     const size_t need = norm ? qnn_qk_norm_rotate_backward_workspace_bytes(tokens, heads_q, heads_k, D) : 0;
     if (need > 0 && (!workspace || !aligned_to(workspace, 256) || workspace_bytes < need))
         return fail(QNN_ERR_WORKSPACE, "%s: workspace NULL, misaligned or smaller than %zu bytes", what, need);
-    a.gamma_f32 = gamma_type == QNN_F32, a.eps = eps, a.angles = angles_of(*rotation), a.tokens = tokens, a.D = (int32_t)D;
-    a.per_block = tokens_per_block(tokens), a.parts = static_cast<float *>(workspace);
+    a.gamma_f32 = gamma_type == QNN_F32, a.eps = eps, a.angles = angles_of(*rotation), a.tokens = tokens, a.D = (int32_t)D, a.inverse_D = 1.0f / (float)D;
+    a.per_block = tokens_per_group(tokens), a.parts = static_cast<float *>(workspace);
     const Split split = split_of(tokens, heads_q, heads_k, a.per_block);
     a.blocks[0] = (int32_t)split.q, a.blocks[1] = (int32_t)split.k;
     for (int i = 0; i < 2; ++i) a.heads[i] = (int32_t)heads[i], a.heads_inverse[i] = inverse_of(heads[i] > 0 ? heads[i] : 1);
@@ -461,7 +487,10 @@ extern "C" int qnn_qk_norm_rotate_backward(const void *grad_q, int64_t ld_grad_q
     const int rc = with_type(type, [&](auto tag) {
         typedef decltype(tag) T;
         return with_lanes(D, [&](auto lanes) {
-            return QNN_LAUNCH(what, (heads_backward_kernel<T, decltype(lanes)::value>), dim3((unsigned)(split.q + split.k)), dim3(kThreads), 0, s, a);
+            constexpr int G = decltype(lanes)::value;
+            auto kernel = beyond_caches(sizeof(T) * (norm ? 3.0 : 2.0) * (double)tokens * (double)(heads_q + heads_k) * (double)D) ? heads_backward_kernel<T, G, true>
+                                                                                                                                     : heads_backward_kernel<T, G, false>;
+            return QNN_LAUNCH(what, kernel, dim3((unsigned)(split.q + split.k)), dim3(kThreads), 0, s, a);
         });
     });
     if (rc || !norm) return rc;
@@ -487,7 +516,7 @@ extern "C" int qnn_cache_append(const qnn_paged_cache *cache, const void *q, int
     if (int rc = check_rotation_pointers(what, *rotation)) return rc;
     if (int rc = paged::check_cache_pointers(what, cache)) return rc;
     a.gamma_q = gamma_q ? gamma_q : gamma_k, a.gamma_k = gamma_k, a.gamma_f32 = gamma_type == QNN_F32, a.eps = eps;
-    a.angles = angles_of(*rotation), a.tokens = tokens, a.D = (int32_t)D, a.heads_q = (int32_t)heads_q, a.heads_k = (int32_t)cache->heads;
+    a.angles = angles_of(*rotation), a.tokens = tokens, a.D = (int32_t)D, a.inverse_D = 1.0f / (float)D, a.heads_q = (int32_t)heads_q, a.heads_k = (int32_t)cache->heads;
     a.pages = paged::pages_of(*cache), a.starts = cache->starts, a.lengths = cache->lengths, a.sequences = cache->sequences;
     a.codes_k = cache->k, a.codes_v = cache->v, a.scale_k = cache->k_scale, a.scale_v = cache->v_scale;
     return launch_heads<true>(what, type, a, static_cast<hipStream_t>(stream));
