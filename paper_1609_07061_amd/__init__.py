@@ -110,7 +110,9 @@ _lib.qnn_version.restype = C.c_char_p
 _MARSHALLED = {"pack_sign": "qnn_pack_sign", "linear_quant_planes": "qnn_linear_quant_planes", "binary_gemm": "qnn_binary_gemm",
                "binary_gemm_sign": "qnn_binary_gemm_sign", "bitplane_gemm": "qnn_bitplane_gemm", "bitplane_conv2d": "qnn_bitplane_conv2d",
                "rms_norm_quant": "qnn_rms_norm_quant", "rms_norm_backward": "qnn_rms_norm_backward", "silu_gate_quant": "qnn_silu_gate_quant",
-               "silu_gate_backward": "qnn_silu_gate_backward", "int8_gemm": "qnn_int8_gemm", "int8_moe": "qnn_int8_moe"}
+               "silu_gate_backward": "qnn_silu_gate_backward", "int8_gemm": "qnn_int8_gemm", "int8_moe": "qnn_int8_moe",
+               "qk_norm_rotate": "qnn_qk_norm_rotate", "qk_norm_rotate_backward": "qnn_qk_norm_rotate_backward", "cache_append": "qnn_cache_append",
+               "cache_attention": "qnn_cache_attention", "rows_quant": "qnn_rows_quant"}
 
 
 def _load_native():
@@ -875,6 +877,10 @@ def qnn_qk_norm_rotate(q: torch.Tensor, k: torch.Tensor, gamma_q: Optional[torch
     """Norm of every head of queries and keys (none where the gammas are None) and the rotation by the tokens' positions (none where freq is None).
     q, k: [tokens][heads][D], also parts of one product's rows; positions: int32 [axes][tokens] (or [tokens]); freq: float64 [pairs], radians a position; axis: int32
     [pairs], which row of positions a pair takes; neighbours: pairs are values 2 i, 2 i + 1 instead of i, i + pairs -> (q_out, k_out), which may be q, k."""
+    if q_out is not None and k_out is not None and (
+            status := _native.qk_norm_rotate(q, k, gamma_q, gamma_k, eps, positions, freq, axis, neighbours, q_out, k_out, _current_device, _stream)) >= 0:
+        _check(status)
+        return q_out, k_out
     T, Hq, D = _heads_shape(q, "q")
     Hk = _heads_shape(k, "k")[1]
     kind = _float_type(q, "q")
@@ -900,6 +906,11 @@ def qnn_qk_norm_rotate_backward(grad_q: torch.Tensor, grad_k: torch.Tensor, q: t
                                 grad_gamma_k: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
     """Gradient of qnn_qk_norm_rotate.  q, k: what the forward call read (so not outputs in their place) -> (out_q, out_k of the type of q, which may be grad_q,
     grad_k, grad_gamma_q, grad_gamma_k float32 [D], None without gammas)."""
+    if out_q is not None and workspace is not None and (
+            status := _native.qk_norm_rotate_backward(grad_q, grad_k, q, k, gamma_q, gamma_k, eps, positions, freq, axis, neighbours, out_q, out_k, grad_gamma_q,
+                                                      grad_gamma_k, workspace, _current_device, _stream)) >= 0:
+        _check(status)
+        return out_q, out_k, None if gamma_q is None else grad_gamma_q, None if gamma_k is None else grad_gamma_k
     T, Hq, D = _heads_shape(q, "q")
     Hk = _heads_shape(k, "k")[1]
     kind = _float_type(q, "q")
@@ -924,7 +935,7 @@ def qnn_qk_norm_rotate_backward(grad_q: torch.Tensor, grad_k: torch.Tensor, q: t
         *_heads(k, T, Hk, D, q.dtype, "k"), Hk, kind, gq, gk, gamma_kind, eps, C.byref(_rotation(positions, freq, axis, neighbours, T)), T, D,
         *_heads(out_q, T, Hq, D, q.dtype, "out_q"), *_heads(out_k, T, Hk, D, q.dtype, "out_k"), *sums,
         None if workspace is None else _here(workspace, torch.uint8, "workspace"), 0 if workspace is None else workspace.numel(), _stream()))
-    return (out_q, out_k, grad_gamma_q, grad_gamma_k) if norm else (out_q, out_k, None, None)
+    return out_q, out_k, None if gamma_q is None else grad_gamma_q, None if gamma_k is None else grad_gamma_k
 
 
 def qnn_new_cache(pages: int, heads: int, page: int, D: int, device="cuda"):
@@ -952,6 +963,10 @@ def qnn_cache_append(cache, table: torch.Tensor, starts: torch.Tensor, lengths: 
     """Keys and values of new tokens into a paged cache (qnn_new_cache), keys normed and rotated as in qnn_qk_norm_rotate; with q its heads likewise, to q_out (which
     may be q) -> q_out.  table: int32 [sequences][pages of a sequence]; starts: int32 [sequences + 1], where each sequence's new tokens begin among the call's;
     lengths: int32 [sequences], all tokens of a sequence, the new ones among them."""
+    if (q is None or q_out is not None) and (status := _native.cache_append(cache, table, starts, lengths, k, v, gamma_k, eps, positions, freq, axis, neighbours, q,
+                                                                            gamma_q, q_out, _current_device, _stream)) >= 0:
+        _check(status)
+        return None if q is None else q_out
     c = _paged(cache, table, starts, lengths)
     T, Hk, D = _heads_shape(k, "k")
     if (Hk, D) != (c.heads, c.D):
@@ -980,6 +995,10 @@ def qnn_cache_attention(q: torch.Tensor, cache, table: torch.Tensor, starts: tor
     qnn_cache_append).  scale: 1 / sqrt(D) if None; cap > 0: scores become cap * tanh(score / cap); slopes: float32 [heads], times the distance taken off a score;
     tree: int64 [tokens], bit t of a token's mask: it sees new token t of its sequence (without one it sees all tokens up to itself).  most_new, longest: the most
     new tokens of a sequence and the longest sequence, as far as the host knows; they set how the work is split, and any numbers are right."""
+    if out is not None and workspace is not None and scale is not None and (
+            status := _native.cache_attention(q, cache, table, starts, lengths, scale, cap, slopes, tree, most_new, longest, out, workspace, _current_device, _stream)) >= 0:
+        _check(status)
+        return out
     c = _paged(cache, table, starts, lengths)
     T, Hq, D = _heads_shape(q, "q")
     if D != c.D:
@@ -1002,6 +1021,9 @@ def qnn_cache_attention(q: torch.Tensor, cache, table: torch.Tensor, starts: tor
 
 def qnn_rows_quant(x: torch.Tensor, codes: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None):
     """Codes int8 [rows][K] and scale float32 [rows] of the rows of x -> (codes, scale)."""
+    if codes is not None and scale is not None and (status := _native.rows_quant(x, codes, scale, _current_device, _stream)) >= 0:
+        _check(status)
+        return codes, scale
     rows, K, ldx = _rows_ld(x, "x")
     kind = _float_type(x, "x")
     if codes is None:

@@ -94,7 +94,7 @@ def _built_for() -> str:
 
 
 def _binding_stale() -> bool:
-    if _stale(NATIVE, [os.path.join(CSRC, "qnn_binding.cpp")]) or not os.path.exists(NATIVE_STAMP):
+    if _stale(NATIVE, _deps(os.path.join(CSRC, "qnn_binding.cpp"))) or not os.path.exists(NATIVE_STAMP):
         return True
     with open(NATIVE_STAMP) as f:
         return f.read() != _built_for()
@@ -114,7 +114,7 @@ def _build_binding(run) -> None:
             os.remove(old)
     try:
         run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
-             f'-DQNN_BUILT_FOR="{_built_for()}"', *[f"-I{d}" for d in (*include_paths(), sysconfig.get_paths()["include"])], src, "-o", NATIVE,
+             f'-DQNN_BUILT_FOR="{_built_for()}"', *[f"-I{d}" for d in (os.path.join(ROOT, "include"), *include_paths(), sysconfig.get_paths()["include"])], src, "-o", NATIVE,
              *[f"-L{d}" for d in library_paths()], "-ltorch_python", "-ltorch_cpu", "-lc10"])
     except (OSError, RuntimeError) as e:
         print(f"the binding's native part was not built: {e}", file=sys.stderr)

@@ -9,6 +9,8 @@
 
 #include <torch/csrc/autograd/python_variable.h>
 
+#include "qnn.h"
+
 namespace {
 
 typedef int (*PackSign)(const float *, int64_t, int64_t, int64_t, uint32_t *, int64_t, void *);
@@ -28,7 +30,13 @@ typedef int (*SiluGateBackward)(const void *, int64_t, const void *, int64_t, co
 typedef int (*Int8Gemm)(const int8_t *, int64_t, const float *, const int8_t *, int64_t, const float *, const float *, void *, int64_t, int, int64_t, int64_t, int64_t, void *);
 typedef int (*Int8Moe)(const int8_t *, int64_t, const float *, const float *, int64_t, int64_t, int, int, int64_t, int64_t, const int8_t *, int64_t, const float *,
                        const int8_t *, int64_t, const float *, void *, int64_t, int, void *, size_t, void *);
-enum { kPackSign, kLinearQuant, kBinaryGemm, kBinaryGemmSign, kBitplaneGemm, kConv2d, kRmsNormQuant, kRmsNormBackward, kSiluGateQuant, kSiluGateBackward, kInt8Gemm, kInt8Moe, kEntries };
+typedef decltype(&qnn_qk_norm_rotate) QkNormRotate;
+typedef decltype(&qnn_qk_norm_rotate_backward) QkNormRotateBackward;
+typedef decltype(&qnn_cache_append) CacheAppend;
+typedef decltype(&qnn_cache_attention) CacheAttention;
+typedef decltype(&qnn_rows_quant) RowsQuant;
+enum { kPackSign, kLinearQuant, kBinaryGemm, kBinaryGemmSign, kBitplaneGemm, kConv2d, kRmsNormQuant, kRmsNormBackward, kSiluGateQuant, kSiluGateBackward, kInt8Gemm, kInt8Moe, kQkNormRotate, kQkNormRotateBackward,
+       kCacheAppend, kCacheAttention, kRowsQuant, kEntries };
 void *g_entry[kEntries];
 
 constexpr int kMaxPlanes = 8;  // QNN_MAX_PLANES
@@ -305,6 +313,192 @@ PyObject *int8_moe(PyObject *const *a) {
     });
 }
 
+// A plain tensor on the device that the call is going to run on
+struct Here {
+    int64_t device = -1;
+    bool set(PyObject *function) { return stream(function, device); }  // (any function without arguments that gives a whole number)
+    const at::Tensor *operator()(PyObject *o, at::ScalarType type, int64_t dims) const {
+        const at::Tensor *const t = tensor(o, type, dims);
+        return t && t->get_device() == device ? t : nullptr;
+    }
+    bool vector(PyObject *o, at::ScalarType type, int64_t n, void *&p) const {
+        const at::Tensor *const t = (*this)(o, type, 1);
+        if (!t || t->size(0) != n || (n > 1 && t->stride(0) != 1)) return false;
+        p = t->data_ptr();
+        return true;
+    }
+};
+// [tokens][heads][D] with contiguous heads
+struct Heads {
+    void *p = nullptr;
+    int64_t tokens = 0, heads = 0, D = 0, ld = 0, step = 0;
+};
+bool heads_of(const Here &here, PyObject *o, at::ScalarType type, Heads &h) {
+    const at::Tensor *const t = here(o, type, 3);
+    if (!t) return false;
+    const auto size = t->sizes(), step = t->strides();
+    h.tokens = size[0], h.heads = size[1], h.D = size[2];
+    if (h.D > 1 && step[2] != 1) return false;
+    h.step = h.heads > 1 ? step[1] : h.D;
+    h.ld = h.tokens > 1 ? step[0] : h.heads * h.step;
+    h.p = t->data_ptr();
+    return true;
+}
+bool heads_like(const Here &here, PyObject *o, at::ScalarType type, const Heads &like, Heads &h) {
+    return heads_of(here, o, type, h) && h.tokens == like.tokens && h.heads == like.heads && h.D == like.D;
+}
+bool scalar_type(PyObject *o, at::ScalarType &t) {
+    if (!THPVariable_CheckExact(o)) return false;
+    t = THPVariable_Unpack(o).scalar_type();
+    return float_type(t) >= 0;
+}
+// gamma_q, gamma_k: none, or of one type
+bool gammas_of(const Here &here, PyObject *q, PyObject *k, int64_t D, void *&pq, void *&pk, int &kind) {
+    at::ScalarType tq = at::kFloat, tk = at::kFloat;
+    pq = pk = nullptr;
+    if (q != Py_None && (!scalar_type(q, tq) || !here.vector(q, tq, D, pq))) return false;
+    if (k != Py_None && (!scalar_type(k, tk) || !here.vector(k, tk, D, pk))) return false;
+    if (q != Py_None && k != Py_None && tq != tk) return false;
+    kind = float_type(q != Py_None ? tq : tk);
+    return true;
+}
+// positions, freq, axis, neighbours
+bool rotation_of(const Here &here, PyObject *const *a, int64_t tokens, qnn_rotation &r) {
+    r = {};
+    if (a[1] == Py_None) return true;
+    const at::Tensor *p = here(a[0], at::kInt, 2);
+    const at::Tensor *const f = here(a[1], at::kDouble, 1);
+    if (!p || !f || p->size(1) != tokens || (tokens > 1 && p->stride(1) != 1) || p->size(0) > INT32_MAX || f->size(0) > INT32_MAX ||
+        (f->size(0) > 1 && f->stride(0) != 1) || !PyBool_Check(a[3]))
+        return false;
+    r.positions = static_cast<const int32_t *>(p->data_ptr()), r.freq = static_cast<const double *>(f->data_ptr());
+    r.axes = (int32_t)p->size(0), r.pairs = (int32_t)f->size(0), r.neighbours = a[3] == Py_True;
+    r.ld_positions = r.axes > 1 ? p->stride(0) : (tokens > 1 ? tokens : 1);
+    if (a[2] != Py_None) {
+        void *axis;
+        if (!here.vector(a[2], at::kInt, f->size(0), axis)) return false;
+        r.axis = static_cast<const int32_t *>(axis);
+    }
+    return true;
+}
+// cache, table, starts, lengths
+bool cache_of(const Here &here, PyObject *const *a, qnn_paged_cache &c) {
+    if (!PyTuple_CheckExact(a[0]) || PyTuple_GET_SIZE(a[0]) != 4) return false;
+    const at::Tensor *const k = here(PyTuple_GET_ITEM(a[0], 0), at::kChar, 4), *const ks = here(PyTuple_GET_ITEM(a[0], 1), at::kFloat, 3),
+                            *const v = here(PyTuple_GET_ITEM(a[0], 2), at::kChar, 4), *const vs = here(PyTuple_GET_ITEM(a[0], 3), at::kFloat, 3),
+                            *const t = here(a[1], at::kInt, 2);
+    if (!k || !ks || !v || !vs || !t || !k->is_contiguous() || !v->is_contiguous() || !ks->is_contiguous() || !vs->is_contiguous() || v->sizes() != k->sizes() ||
+        ks->sizes() != k->sizes().slice(0, 3) || vs->sizes() != ks->sizes() || (t->size(1) > 1 && t->stride(1) != 1))
+        return false;
+    void *starts, *lengths;
+    c.sequences = t->size(0), c.width = t->size(1);
+    if (!here.vector(a[2], at::kInt, c.sequences + 1, starts) || !here.vector(a[3], at::kInt, c.sequences, lengths)) return false;
+    c.ld_table = c.sequences > 1 ? t->stride(0) : (c.width > 1 ? c.width : 1);
+    c.k = static_cast<int8_t *>(k->data_ptr()), c.v = static_cast<int8_t *>(v->data_ptr());
+    c.k_scale = static_cast<float *>(ks->data_ptr()), c.v_scale = static_cast<float *>(vs->data_ptr());
+    c.pages = k->size(0), c.heads = k->size(1), c.page = k->size(2), c.D = k->size(3);
+    c.table = static_cast<const int32_t *>(t->data_ptr()), c.starts = static_cast<const int32_t *>(starts), c.lengths = static_cast<const int32_t *>(lengths);
+    return true;
+}
+
+// q, k, gamma_q, gamma_k, eps, positions, freq, axis, neighbours, q_out, k_out, device, stream
+PyObject *qk_norm_rotate(PyObject *const *a) {
+    Here here;
+    Heads q, k, qo, ko;
+    at::ScalarType t;
+    void *gq, *gk;
+    int gamma_kind;
+    qnn_rotation r;
+    int64_t s;
+    if (!here.set(a[11]) || !PyFloat_CheckExact(a[4]) || !scalar_type(a[0], t) || !heads_of(here, a[0], t, q) || !heads_of(here, a[1], t, k) || k.tokens != q.tokens ||
+        k.D != q.D || !gammas_of(here, a[2], a[3], q.D, gq, gk, gamma_kind) || !rotation_of(here, a + 5, q.tokens, r) || !heads_like(here, a[9], t, q, qo) ||
+        !heads_like(here, a[10], t, k, ko) || !stream(a[12], s))
+        return not_here();
+    const float eps = (float)PyFloat_AS_DOUBLE(a[4]);
+    return call([&] {
+        return reinterpret_cast<QkNormRotate>(g_entry[kQkNormRotate])(q.p, q.ld, q.step, q.heads, k.p, k.ld, k.step, k.heads, float_type(t), gq, gk, gamma_kind, eps, &r,
+                                                                      q.tokens, q.D, qo.p, qo.ld, qo.step, ko.p, ko.ld, ko.step, stream_of(s));
+    });
+}
+// grad_q, grad_k, q, k, gamma_q, gamma_k, eps, positions, freq, axis, neighbours, out_q, out_k, grad_gamma_q, grad_gamma_k, workspace, device, stream
+PyObject *qk_norm_rotate_backward(PyObject *const *a) {
+    Here here;
+    Heads dq, dk, q, k, qo, ko;
+    at::ScalarType t;
+    void *gq, *gk, *sq = nullptr, *sk = nullptr;
+    int gamma_kind;
+    qnn_rotation r;
+    int64_t s;
+    if (!here.set(a[16]) || !PyFloat_CheckExact(a[6]) || !scalar_type(a[2], t) || !heads_of(here, a[2], t, q) || !heads_of(here, a[3], t, k) || k.tokens != q.tokens ||
+        k.D != q.D || !heads_like(here, a[0], t, q, dq) || !heads_like(here, a[1], t, k, dk) || !gammas_of(here, a[4], a[5], q.D, gq, gk, gamma_kind) ||
+        !rotation_of(here, a + 7, q.tokens, r) || !heads_like(here, a[11], t, q, qo) || !heads_like(here, a[12], t, k, ko))
+        return not_here();
+    const at::Tensor *const ws = here(a[15], at::kByte, 1);
+    if (!ws || !ws->is_contiguous() || (gq && !here.vector(a[13], at::kFloat, q.D, sq)) || (gk && !here.vector(a[14], at::kFloat, q.D, sk)) || !stream(a[17], s)) return not_here();
+    const float eps = (float)PyFloat_AS_DOUBLE(a[6]);
+    void *const w = ws->data_ptr();
+    const size_t bytes = (size_t)ws->numel();
+    return call([&] {
+        return reinterpret_cast<QkNormRotateBackward>(g_entry[kQkNormRotateBackward])(dq.p, dq.ld, dq.step, dk.p, dk.ld, dk.step, q.p, q.ld, q.step, q.heads, k.p, k.ld, k.step, k.heads,
+                                                                                      float_type(t), gq, gk, gamma_kind, eps, &r, q.tokens, q.D, qo.p, qo.ld, qo.step, ko.p, ko.ld,
+                                                                                      ko.step, static_cast<float *>(sq), static_cast<float *>(sk), w, bytes, stream_of(s));
+    });
+}
+// cache, table, starts, lengths, k, v, gamma_k, eps, positions, freq, axis, neighbours, q, gamma_q, q_out, device, stream
+PyObject *cache_append(PyObject *const *a) {
+    Here here;
+    qnn_paged_cache c;
+    Heads q, k, v, qo;
+    at::ScalarType t;
+    void *gq, *gk;
+    int gamma_kind;
+    qnn_rotation r;
+    int64_t s;
+    if (!here.set(a[15]) || !PyFloat_CheckExact(a[7]) || !cache_of(here, a, c) || !scalar_type(a[4], t) || !heads_of(here, a[4], t, k) || k.heads != c.heads || k.D != c.D ||
+        !heads_like(here, a[5], t, k, v) || !gammas_of(here, a[13], a[6], k.D, gq, gk, gamma_kind) || !rotation_of(here, a + 8, k.tokens, r) ||
+        (a[12] != Py_None && (!heads_of(here, a[12], t, q) || q.tokens != k.tokens || q.D != k.D || !heads_like(here, a[14], t, q, qo))) || !stream(a[16], s))
+        return not_here();
+    const float eps = (float)PyFloat_AS_DOUBLE(a[7]);
+    return call([&] {
+        return reinterpret_cast<CacheAppend>(g_entry[kCacheAppend])(&c, q.p, q.ld, q.step, q.heads, k.p, k.ld, k.step, v.p, v.ld, v.step, float_type(t), gq, gk, gamma_kind, eps, &r,
+                                                                    k.tokens, qo.p, qo.ld, qo.step, stream_of(s));
+    });
+}
+// q, cache, table, starts, lengths, scale, cap, slopes, tree, most_new, longest, out, workspace, device, stream
+PyObject *cache_attention(PyObject *const *a) {
+    Here here;
+    qnn_paged_cache c;
+    Heads q, o;
+    at::ScalarType t;
+    void *slopes = nullptr, *tree = nullptr;
+    int64_t most_new, longest, s;
+    if (!here.set(a[13]) || !PyFloat_CheckExact(a[5]) || !PyFloat_CheckExact(a[6]) || !cache_of(here, a + 1, c) || !scalar_type(a[0], t) || !heads_of(here, a[0], t, q) || q.D != c.D ||
+        (a[7] != Py_None && !here.vector(a[7], at::kFloat, q.heads, slopes)) || (a[8] != Py_None && !here.vector(a[8], at::kLong, q.tokens, tree)) || !integer(a[9], most_new) ||
+        !integer(a[10], longest) || !heads_like(here, a[11], t, q, o))
+        return not_here();
+    const at::Tensor *const ws = here(a[12], at::kByte, 1);
+    if (!ws || !ws->is_contiguous() || !stream(a[14], s)) return not_here();
+    const float scale = (float)PyFloat_AS_DOUBLE(a[5]), cap = (float)PyFloat_AS_DOUBLE(a[6]);
+    void *const w = ws->data_ptr();
+    const size_t bytes = (size_t)ws->numel();
+    return call([&] {
+        return reinterpret_cast<CacheAttention>(g_entry[kCacheAttention])(&c, q.p, q.ld, q.step, q.heads, float_type(t), scale, cap, static_cast<const float *>(slopes),
+                                                                          static_cast<const uint64_t *>(tree), q.tokens, most_new, longest, o.p, o.ld, o.step, w, bytes, stream_of(s));
+    });
+}
+// x, codes, scale, device, stream
+PyObject *rows_quant(PyObject *const *a) {
+    Here here;
+    Rows x, c;
+    void *scale;
+    int type;
+    int64_t s;
+    if (!here.set(a[3]) || !floats_of(a[0], x, type) || THPVariable_Unpack(a[0]).get_device() != here.device || !here(a[1], at::kChar, 2) || !codes_like(a[1], x.rows, x.cols, c) ||
+        !here.vector(a[2], at::kFloat, x.rows, scale) || !stream(a[4], s))
+        return not_here();
+    return call([&] { return reinterpret_cast<RowsQuant>(g_entry[kRowsQuant])(x.p, x.ld, type, x.rows, x.cols, as<int8_t>(c), c.ld, static_cast<float *>(scale), stream_of(s)); });
+}
+
 // (C++ errors, of a tensor that has no memory for instance, are the general path's)
 template <PyObject *(*kCall)(PyObject *const *), Py_ssize_t kArgs, int kEntry>
 PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n) {
@@ -342,6 +536,11 @@ PyMethodDef kMethods[] = {
     {"silu_gate_backward", function(entry<silu_gate_backward, 6, kSiluGateBackward>), METH_FASTCALL, nullptr},
     {"int8_gemm", function(entry<int8_gemm, 7, kInt8Gemm>), METH_FASTCALL, nullptr},
     {"int8_moe", function(entry<int8_moe, 11, kInt8Moe>), METH_FASTCALL, nullptr},
+    {"qk_norm_rotate", function(entry<qk_norm_rotate, 13, kQkNormRotate>), METH_FASTCALL, nullptr},
+    {"qk_norm_rotate_backward", function(entry<qk_norm_rotate_backward, 18, kQkNormRotateBackward>), METH_FASTCALL, nullptr},
+    {"cache_append", function(entry<cache_append, 17, kCacheAppend>), METH_FASTCALL, nullptr},
+    {"cache_attention", function(entry<cache_attention, 15, kCacheAttention>), METH_FASTCALL, nullptr},
+    {"rows_quant", function(entry<rows_quant, 5, kRowsQuant>), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
