@@ -421,7 +421,7 @@ int qnn_cache_append(const qnn_paged_cache *cache, const void *q, int64_t ld_q, 
 
 /* Attention of the new tokens' queries over the cache, after their own keys and values are in it.  heads_q is a multiple of cache->heads; query head h reads
  * head h / (heads_q / cache->heads).  Of query i and key j of a sequence of n tokens, m of them new:
- *   s = scale * q_i . k_j;  with cap > 0: s = cap * tanh(s / cap);  with slopes: s -= slopes[h] * (place(i) - place(j));   out_i = sum_j softmax_j(s) v_j.
+ *   s = scale * q_i . k_j;  with cap > 0 (1e-30 at least): s = cap * tanh(s / cap);  with slopes: s -= slopes[h] * (place(i) - place(j));   out_i = sum_j softmax_j(s) v_j.
  * A query sees the tokens up to itself.  With a tree it sees the first n - m tokens and, of the new ones, those whose bit is set in its mask tree[i] (bit t: new
  * token t of the sequence; new tokens from the 65th on are seen by none).  A query that sees nothing gets zeros.
  * place is the index in the sequence; with a tree that of a new token is n - m - 1 + (bits set in its mask).

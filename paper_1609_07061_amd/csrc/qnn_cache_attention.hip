@@ -488,14 +488,15 @@ int launch_join(const Args &a, hipStream_t s) {
     return few(join_few_kernel<T, 64, 2>, join_few_kernel<T, 64, 4>, join_few_kernel<T, 64, 8>, 4);
 }
 
-// Few rows (up to 256 of a sequence and head of the cache): 16 or 32 a workgroup, and as many parts of the keys as fill the card, each the same number of steps for every
-// wave.  (us, bf16, 32 heads on 8 of 128: 64 sequences of up to 8192 tokens in one part each 163, in two 146, in three 148; one sequence of 10000 in 79 parts 17.)
-// Many rows: 128 or 256 a workgroup, one on a compute unit.  (16 sequences with 64 drafted tokens each, 256 rows: 79 on the kernel for few, 83 on the one for many;
-// 3 sequences with 700, 3500 rows of 80: 144 and 86.)
+// Few rows (up to 768 of a sequence and head of the cache): 16 or 32 a workgroup, and as many parts of the keys as fill the card, each the same number of steps for
+// every wave.  (us, bf16, 32 heads on 8 of 128: 64 sequences of up to 8192 tokens in one part each 163, in two 146, in three 148; one sequence of 10000 in 79 parts 17.)
+// Many rows: 128 or 256 a workgroup, one on a compute unit.  (us on the kernel for few and on the one for many, sequences of up to: 16 of 2000 with 256 rows each 67 and
+// 74, 512 rows 109 and 106; 2 of 5000 with 640 rows 65 and 70, 800 rows 77 and 80; one of 8192 with 512 rows 59 and 65, 1024 rows 99 and 79; heads of 256: 4 of 4000
+// with 400 rows 108 and 166, one of 4096 with 1024 rows 111 and 110, 2048 rows 191 and 178.)
 Plan plan_of(int64_t sequences, int64_t heads_q, int64_t heads, int64_t D, int type, int64_t most_new, int64_t longest) {
     Plan p;
     const int64_t rows = most_new * (heads_q / heads);
-    const bool few = rows <= 256 || !takes_many(D, type);
+    const bool few = rows <= 768 || !takes_many(D, type);
     p.rows = few ? (rows <= 16 || D > 128 ? 16 : 32) : many_rows(D);
     p.blocks = ceil_div(rows, p.rows);
     const int64_t on_unit = few ? waves_of(D <= 64 ? 64 : (D <= 128 ? 128 : 256), p.rows / 16, 1) : 1;
@@ -550,7 +551,7 @@ extern "C" int qnn_cache_attention(const qnn_paged_cache *cache, const void *q, 
         return fail(QNN_ERR_SHAPE, "%s: %lld tokens, %lld heads on %lld of the cache, most_new = %lld, longest = %lld", what, (long long)tokens, (long long)heads_q,
                     (long long)cache->heads, (long long)most_new, (long long)longest);
     if (!rows::known_type(type)) return fail(QNN_ERR_SHAPE, "%s: type %d", what, type);
-    if (!(cap >= 0.0f) || cap > 3.0e38f || !(scale >= -3.0e38f && scale <= 3.0e38f)) return fail(QNN_ERR_SHAPE, "%s: scale = %g, cap = %g", what, (double)scale, (double)cap);
+    if (!(cap == 0.0f || (cap >= 1e-30f && cap <= 3.0e38f)) || !(scale >= -3.0e38f && scale <= 3.0e38f)) return fail(QNN_ERR_SHAPE, "%s: scale = %g, cap = %g", what, (double)scale, (double)cap);
     if (tokens == 0 || cache->sequences == 0) return QNN_OK;
     if ((double)tokens * (double)(heads_q / cache->heads) > 2147483647.0) return fail(QNN_ERR_UNSUPPORTED, "%s: %lld tokens", what, (long long)tokens);
     if (!paged::heads_fit(ld_q, step_q, heads_q, D, tokens) || !paged::heads_fit(ld_out, step_out, heads_q, D, tokens))

@@ -108,7 +108,7 @@ def test_cache_attention(q):
         assert call(cache=_cache(q, **change)) == status, change
     inf, nan = float("inf"), float("nan")
     for change, status in [(dict(cache=None), NULL), (dict(tokens=-1), SHAPE), (dict(heads_q=0), SHAPE), (dict(heads_q=9), SHAPE), (dict(heads_q=70000), SHAPE), (dict(most_new=0), SHAPE),
-                           (dict(longest=0), SHAPE), (dict(type=4), SHAPE), (dict(cap=-1.0), SHAPE), (dict(cap=nan), SHAPE), (dict(cap=inf), SHAPE), (dict(scale=nan), SHAPE),
+                           (dict(longest=0), SHAPE), (dict(type=4), SHAPE), (dict(cap=-1.0), SHAPE), (dict(cap=9e-31), SHAPE), (dict(cap=nan), SHAPE), (dict(cap=inf), SHAPE), (dict(scale=nan), SHAPE),
                            (dict(scale=inf), SHAPE), (dict(ldq=511), SHAPE), (dict(ldo=511), SHAPE), (dict(sq=63), SHAPE), (dict(so=-64), SHAPE), (dict(q=None), NULL), (dict(out=None), NULL),
                            (dict(q=FAKE + 1), ALIGN), (dict(out=FAKE + 1), ALIGN), (dict(slopes=FAKE + 2), ALIGN), (dict(tree=FAKE + 4), ALIGN), (dict(ws=None), WORKSPACE),
                            (dict(ws=BIG + 64), WORKSPACE), (dict(bytes=need - 1), WORKSPACE)]:

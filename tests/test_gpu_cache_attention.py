@@ -67,6 +67,20 @@ def test_attention(seed, case, type, kind, with_tree):
         assert torch.equal(again[written], q.qnn_cache_attention(x, *p.args, None, **options, most_new=most_new, longest=longest)[written])
 
 
+# the same on more than 768 rows of a head of the cache
+MANY = [([31, 32, 64, 65], [31, 32, 1, 65], 18, 3, 64, 7), ([1000], [100], 16, 2, 128, 32), ([130, 9], [17, 9], 32, 1, 112, 16), ([70], [70], 12, 1, 240, 128),
+        ([300, 900], [250, 150], 4, 2, 16, 5), ([420, 0, 1], [400, 0, 1], 5, 1, 80, 20), ([900], [256], 8, 2, 256, 64)]
+
+
+@pytest.mark.parametrize("case", MANY)
+@pytest.mark.parametrize("type,kind", EACH)
+@pytest.mark.parametrize("with_tree", [False, True])
+def test_many_rows(seed, case, type, kind, with_tree):
+    lengths, fresh, H, heads, D, page = case
+    assert (sum(fresh) + 3) * H // heads > 768
+    test_attention(seed, case, type, kind, with_tree)
+
+
 @pytest.mark.parametrize("type", ["f32", "bf16"])
 @pytest.mark.parametrize("lengths,fresh,H,heads,D,page", [([20000], [1], 8, 2, 128, 16), ([9000, 3, 4000], [1, 1, 1], 2, 1, 256, 64), ([3000, 2500], [64, 40], 8, 2, 64, 16),
                                                           ([5000], [700], 8, 2, 128, 64)])
@@ -80,7 +94,7 @@ def test_long(seed, lengths, fresh, H, heads, D, page, type):
 
 
 @pytest.mark.parametrize("type", ["f32", "f16", "bf16"])
-@pytest.mark.parametrize("fresh", [1, 40, 200])
+@pytest.mark.parametrize("fresh", [1, 40, 200, 450])
 def test_what_is_not_seen_does_not_matter(seed, fresh, type):
     """Scales that are NaN or infinite at later tokens, behind the sequence's end, on other pages and in pages that are none; and what a query that sees one gets."""
     import paper_1609_07061_amd as q
@@ -114,7 +128,7 @@ def test_what_is_not_seen_does_not_matter(seed, fresh, type):
     assert torch.equal(got, want)
 
 
-@pytest.mark.parametrize("fresh", [1, 30, 300])
+@pytest.mark.parametrize("fresh", [1, 30, 300, 390])
 def test_pages_that_are_none(seed, fresh):
     """Tokens whose page is outside the cache or beyond the table are not seen; a query left with nothing gets zeros."""
     import paper_1609_07061_amd as q
