@@ -489,7 +489,10 @@ int launch_join(const Args &a, hipStream_t s) {
 }
 
 // Few rows (up to 768 of a sequence and head of the cache): 16 or 32 a workgroup, and as many parts of the keys as fill the card, each the same number of steps for
-// every wave.  (us, bf16, 32 heads on 8 of 128: 64 sequences of up to 8192 tokens in one part each 163, in two 146, in three 148; one sequence of 10000 in 79 parts 17.)
+// every wave.  (us, bf16, 32 heads on 8 of 128: 16 sequences of up to 4000 tokens in 6 parts each 27, in one 69; one sequence of 10000 in 79 parts 17.)  Where there is
+// work for every unit without: parts of 8 turns of the waves at least, for their joining takes 5 us (64 sequences of up to 500 tokens in one part each 17, in two 22),
+// and where a sequence has one workgroup's rows, 2.5 times what the card holds, so that long sequences and short ones come out even (64 of up to 8192 in one part 163, in
+// two 146, in four 138; 128 of up to 4096 in one 156, in two 145).
 // Many rows: 128 or 256 a workgroup, one on a compute unit.  (us on the kernel for few and on the one for many, sequences of up to: 16 of 2000 with 256 rows each 67 and
 // 74, 512 rows 109 and 106; 2 of 5000 with 640 rows 65 and 70, 800 rows 77 and 80; one of 8192 with 512 rows 59 and 65, 1024 rows 99 and 79; heads of 256: 4 of 4000
 // with 400 rows 108 and 166, one of 4096 with 1024 rows 111 and 110, 2048 rows 191 and 178.)
@@ -500,13 +503,19 @@ Plan plan_of(int64_t sequences, int64_t heads_q, int64_t heads, int64_t D, int t
     p.rows = few ? (rows <= 16 || D > 128 ? 16 : 32) : many_rows(D);
     p.blocks = ceil_div(rows, p.rows);
     const int64_t on_unit = few ? waves_of(D <= 64 ? 64 : (D <= 128 ? 128 : 256), p.rows / 16, 1) : 1;
-    const int64_t want = ceil_div(on_unit * compute_units(), sequences * heads * p.blocks), per_turn = few ? kStep * kWaves : 256, turns = ceil_div(longest, per_turn);
+    const double blocks = (double)sequences * (double)heads * (double)p.blocks;
+    const int64_t units = compute_units(), wanted = blocks < 1e12 ? (int64_t)blocks : (int64_t)1e12, per_turn = few ? kStep * kWaves : 256, turns = ceil_div(longest, per_turn);
+    int64_t want = ceil_div(on_unit * units, wanted);
+    if (few && wanted >= units) {
+        if (p.blocks == 1) want = ceil_div(on_unit * units * 5 / 2, wanted);
+        want = want < turns / 8 ? want : (turns >= 8 ? turns / 8 : 1);
+    }
     p.splits = ceil_div(turns, ceil_div(turns, want < kMostSplits ? want : kMostSplits));
     return p;
 }
 bool plannable(int64_t tokens, int64_t sequences, int64_t heads_q, int64_t heads, int64_t D, int64_t most_new, int64_t longest) {
-    return tokens >= 1 && sequences >= 1 && heads >= 1 && heads_q >= 1 && heads_q % heads == 0 && heads_q <= 65535 && D >= 16 && D <= paged::kMostD && most_new >= 1 &&
-           longest >= 1;
+    return tokens >= 1 && tokens <= 0x7FFFFFFF && sequences >= 1 && sequences <= 0x3FFFFFFF && heads >= 1 && heads_q >= 1 && heads_q % heads == 0 &&
+           heads_q <= 65535 && D >= 16 && D <= paged::kMostD && most_new >= 1 && longest >= 1;
 }
 // (numbers above what there can be do no more than these)
 int64_t at_most(int64_t x, int64_t limit) { return x < limit ? x : limit; }

@@ -444,7 +444,7 @@ extern "C" int qnn_qk_norm_rotate(const void *q, int64_t ld_q, int64_t step_q, i
 }
 
 extern "C" size_t qnn_qk_norm_rotate_backward_workspace_bytes(int64_t tokens, int64_t heads_q, int64_t heads_k, int64_t D) {
-    if (tokens < 1 || heads_q < 0 || heads_k < 0 || heads_q + heads_k < 1 || D < 16 || D > paged::kMostD) return 0;
+    if (tokens < 1 || tokens > 0x7FFFFFFF || heads_q < 0 || heads_k < 0 || heads_q > 65535 || heads_k > 65535 || heads_q + heads_k < 1 || D < 16 || D > paged::kMostD) return 0;
     const Split s = split_of(tokens, heads_q, heads_k, tokens_per_group(tokens));
     return (size_t)(s.q + s.k) * (size_t)D * 4;
 }

@@ -175,3 +175,16 @@ def test_binding_refuses_on_the_gpu(q):
         z = lambda *n, dtype=torch.int32: torch.zeros(*n, dtype=dtype, device="cuda")
         q.qnn_cache_attention(z(1, 3, 64, dtype=torch.float32), q.qnn_new_cache(1, 2, 16, 64), z(1, 1), z(2), z(1))
     assert e.value.status == SHAPE
+
+
+def test_workspaces_of_absurd_sizes():
+    """Numbers whose products pass 64 bits: an answer, and no fault."""
+    import paper_1609_07061_amd as q
+
+    big = (1 << 63) - 1
+    for tokens in (1, 1 << 31, 1 << 40, big):
+        for other in (1, 1 << 30, 1 << 32, 1 << 48, big):
+            for heads in (1, 65535):
+                assert q.qnn_cache_attention_workspace_bytes(tokens, other, 65535, heads, 256, big, big) >= 0
+                assert q.qnn_cache_attention_workspace_bytes(other, tokens, 65535, heads, 16, other, tokens) >= 0
+                assert q.qnn_qk_norm_rotate_backward_workspace_bytes(tokens, other, heads, 256) >= 0
