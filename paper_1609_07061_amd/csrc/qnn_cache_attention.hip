@@ -493,8 +493,9 @@ int launch_join(const Args &a, hipStream_t s) {
 // work for every unit without: parts of 8 turns of the waves at least, for their joining takes 5 us (64 sequences of up to 500 tokens in one part each 17, in two 22),
 // and where a sequence has one workgroup's rows, 2.5 times what the card holds, so that long sequences and short ones come out even (64 of up to 8192 in one part 163, in
 // two 146, in four 138; 128 of up to 4096 in one 156, in two 145).
-// Many rows: 128 or 256 a workgroup, one on a compute unit.  (us on the kernel for few and on the one for many, sequences of up to: 16 of 2000 with 256 rows each 67 and
-// 74, 512 rows 109 and 106; 2 of 5000 with 640 rows 65 and 70, 800 rows 77 and 80; one of 8192 with 512 rows 59 and 65, 1024 rows 99 and 79; heads of 256: 4 of 4000
+// Many rows: 128 or 256 a workgroup, one on a compute unit, and parts only as far as all are resident (1500 of up to 6000 tokens, 16 heads on 4 of 64: 96 workgroups in
+// 2 parts 140, in 3 171), but 2 where they are more than half as many, for sequences of different lengths (3 of up to 2500 with 700 new ones: 84, in one part 121).
+// (us on the kernel for few and on the one for many, sequences of up to: 16 of 2000 with 256 rows each 67 and 74, 512 rows 109 and 106; 2 of 5000 with 640 rows 65 and 70, 800 rows 77 and 80; one of 8192 with 512 rows 59 and 65, 1024 rows 99 and 79; heads of 256: 4 of 4000
 // with 400 rows 108 and 166, one of 4096 with 1024 rows 111 and 110, 2048 rows 191 and 178.)
 Plan plan_of(int64_t sequences, int64_t heads_q, int64_t heads, int64_t D, int type, int64_t most_new, int64_t longest) {
     Plan p;
@@ -505,7 +506,7 @@ Plan plan_of(int64_t sequences, int64_t heads_q, int64_t heads, int64_t D, int t
     const int64_t on_unit = few ? waves_of(D <= 64 ? 64 : (D <= 128 ? 128 : 256), p.rows / 16, 1) : 1;
     const double blocks = (double)sequences * (double)heads * (double)p.blocks;
     const int64_t units = compute_units(), wanted = blocks < 1e12 ? (int64_t)blocks : (int64_t)1e12, per_turn = few ? kStep * kWaves : 256, turns = ceil_div(longest, per_turn);
-    int64_t want = ceil_div(on_unit * units, wanted);
+    int64_t want = few || units / wanted < 2 ? ceil_div(on_unit * units, wanted) : units / wanted;
     if (few && wanted >= units) {
         if (p.blocks == 1) want = ceil_div(on_unit * units * 5 / 2, wanted);
         want = want < turns / 8 ? want : (turns >= 8 ? turns / 8 : 1);

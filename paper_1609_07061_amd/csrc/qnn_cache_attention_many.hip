@@ -41,6 +41,7 @@ __global__ __launch_bounds__(64 * kWaves, kWaves / 4) void many_rows_kernel(cons
         uint32_t rest = quotient(id, a.pages.heads, a.heads_inverse, head);
         rest = quotient(rest, (uint32_t)a.splits, a.splits_inverse, split);
         b = quotient(rest, (uint32_t)a.blocks, a.blocks_inverse, block);
+        block = (uint32_t)a.blocks - 1u - block;  // (the last rows see the most keys: long work first.  4096 tokens' prompt, 32 heads of 128: 293 us -> 238)
     }
     if ((int64_t)b >= a.sequences) return;  // (of the launch's last line)
     if (tid < kTile) ones[tid] = 1.0f;
