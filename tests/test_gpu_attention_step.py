@@ -6,7 +6,7 @@ import sys
 import pytest
 import torch
 
-from attention_testlib import Rotation, attention, heads_of, norm_rotate
+from attention_testlib import Paged, Rotation, attention, heads_of, norm_rotate
 from int8_testlib import TYPES, U, assert_near, generator, normal
 
 pytestmark = pytest.mark.gpu
@@ -139,6 +139,57 @@ def test_a_block_trains(seed):
     for got, leaf in zip((dx, dk, dgq, dgk), leaves):
         # fp32 throughout: some thousand roundings of sums of T D terms
         assert ((got.double() - leaf.grad).abs() <= 2e-5 * leaf.grad.abs().max()).all()
+
+
+def test_given_buffers_and_new_ones(seed):
+    """The binding's short way, for calls that bring all their buffers, and its general one: the same bits."""
+    import paper_1609_07061_amd as q
+
+    T, Hq, Hk, D = 21, 6, 2, 48
+    p = Paged(seed, [30, 50], [20, 1], Hk, D, 16)
+    rotation = Rotation(seed, T, D, 16, 2)
+    x, k, v = (heads_of(seed + i, T, H, D, torch.bfloat16) for i, H in enumerate((Hq, Hk, Hk)))
+    gq, gk = ((1 + 0.2 * normal(generator(seed, i), D)).to(torch.bfloat16) for i in range(2))
+    new = lambda t: torch.full_like(t, 7)
+    byte = lambda n: torch.empty(max(n, 1), dtype=torch.uint8, device="cuda")
+
+    def same(a, b):
+        assert all(torch.equal(s, t) for s, t in zip(a, b, strict=True))
+
+    same(q.qnn_qk_norm_rotate(x, k, gq, gk, EPS, *rotation.args, new(x), new(k)), q.qnn_qk_norm_rotate(x, k, gq, gk, EPS, *rotation.args))
+    sums = [torch.full((D,), 7.0, device="cuda") for _ in range(2)]
+    ws = byte(q.qnn_qk_norm_rotate_backward_workspace_bytes(T, Hq, Hk, D))
+    same(q.qnn_qk_norm_rotate_backward(x, v, x, k, gq, gk, EPS, *rotation.args, new(x), new(k), *sums, ws), q.qnn_qk_norm_rotate_backward(x, v, x, k, gq, gk, EPS, *rotation.args))
+    kept = [t.clone() for t in p.cache]
+    short = q.qnn_cache_append(*p.args, k, v, gk, EPS, *rotation.args, x, gq, new(x))
+    other = q.qnn_cache_append(tuple(kept), *p.args[1:], k, v, gk, EPS, *rotation.args, x, gq)
+    same([short, *p.cache], [other, *kept])
+    slopes = torch.rand(Hq, device="cuda")
+    tree = torch.full((T,), 5, dtype=torch.int64, device="cuda")
+    for options in (dict(), dict(cap=5.0, slopes=slopes), dict(tree=tree)):
+        ws = byte(q.qnn_cache_attention_workspace_bytes(T, 2, Hq, Hk, D, 20, 50))
+        same([q.qnn_cache_attention(x, *p.args, 0.2, **options, most_new=20, longest=50, out=new(x), workspace=ws)],
+             [q.qnn_cache_attention(x, *p.args, 0.2, **options, most_new=20, longest=50)])
+    rows = x.view(T, Hq * D)
+    same(q.qnn_rows_quant(rows, new(rows).to(torch.int8), torch.empty(T, device="cuda")), q.qnn_rows_quant(rows))
+
+
+def test_two_streams_at_once(seed):
+    """Calls on two streams, each with buffers of its own: what each gives alone."""
+    import paper_1609_07061_amd as q
+
+    p = Paged(seed, [900, 3000], [1, 1], 2, 128, 16)
+    xs = [heads_of(seed + i, 2, 8, 128, torch.bfloat16) for i in range(2)]
+    want = [q.qnn_cache_attention(x, *p.args, most_new=1, longest=3000).clone() for x in xs]
+    streams = [torch.cuda.Stream() for _ in xs]
+    outs = [[], []]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                outs[i].append(q.qnn_cache_attention(xs[i], *p.args, most_new=1, longest=3000))
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, w) for got, w in zip(outs, want) for o in got)
 
 
 def test_example():

@@ -124,7 +124,8 @@ def test_offsets_beyond_32_bits(seed):
     got = torch.cat([codes[-1, 0], codes[-2, 0, :2]])
     assert_quantized(got, torch.cat([scale[-1, 0], scale[-2, 0, :2]]), want[:, 0], (error[:, 0] / want.abs().amax(dim=2)).max().item() + 4 * U)
     assert not codes[:-2].any() and not scale[:-2].any() and not codes[-2, 0, 2:].any()
-    x = heads_of(seed + 2, 130, 2, D, torch.bfloat16)
-    out = q.qnn_cache_attention(x, cache, ints(pages - 1, pages - 2)[None], ints(0, 130), ints(130))
     small = [torch.stack([t[-1], t[-2]]) for t in cache]
-    assert torch.equal(out, q.qnn_cache_attention(x, small, ints(0, 1)[None], ints(0, 130), ints(130)))
+    for heads in (2, 8):  # 260 rows and 1040
+        x = heads_of(seed + 2, 130, heads, D, torch.bfloat16)
+        out = q.qnn_cache_attention(x, cache, ints(pages - 1, pages - 2)[None], ints(0, 130), ints(130))
+        assert torch.equal(out, q.qnn_cache_attention(x, small, ints(0, 1)[None], ints(0, 130), ints(130)))
