@@ -3,6 +3,10 @@
 // first result a lane has keys 4 g + 0 .. 3 of either 16 for query lane mod 16, which is the second's right operand as it is once the rows of V are taken in that
 // order; the sums over keys of a query are per lane until the end.  Codes go from memory to registers, 16 bytes of K a lane and D / 16 of V (whole rows a load), and
 // become float16 there; V's transposition is the choice of bytes in that step.
+// Single tokens are bound by memory (64 sequences of up to 8192 tokens, 32 heads on 8 of 128, bf16: 618 MB in 126 us, and 5 for the join of four parts), of one sequence
+// by latency: page numbers, scales, codes, one after the other, before the first product (10000 tokens, 21 MB: 10.8 us and 3.8).  Drafted trees and short prompts are
+// bound by the vector instructions that make codes float16 and scores weights: some 750 a step of 32 rows, of 48 matrix instructions (8 sequences of up to 4099 tokens,
+// 40 drafted each, 16 heads on 4 of 128, fp16, capped: 46 us and 4 for the join).
 #include "qnn_attention.h"
 
 namespace qnn {
@@ -489,7 +493,7 @@ int launch_join(const Args &a, hipStream_t s) {
 }
 
 // Few rows (up to 768 of a sequence and head of the cache): 16 or 32 a workgroup, and as many parts of the keys as fill the card, each the same number of steps for
-// every wave.  (us, bf16, 32 heads on 8 of 128: 16 sequences of up to 4000 tokens in 6 parts each 27, in one 69; one sequence of 10000 in 79 parts 17.)  Where there is
+// every wave.  (us, bf16, 32 heads on 8 of 128: 8 sequences of up to 4000 tokens in 11 parts each 22, in one 55; one of 10000 in 79 parts 17, in 16 parts 20.)  Where there is
 // work for every unit without: parts of 8 turns of the waves at least, for their joining takes 5 us (64 sequences of up to 500 tokens in one part each 17, in two 22),
 // and where a sequence has one workgroup's rows, 2.5 times what the card holds, so that long sequences and short ones come out even (64 of up to 8192 in one part 163, in
 // two 146, in four 138; 128 of up to 4096 in one 156, in two 145).

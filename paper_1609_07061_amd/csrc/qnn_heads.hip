@@ -5,7 +5,9 @@
 // eight values each, so that a lane has both halves of eight pairs, whichever way pairs are formed; the sum of squares and, for codes, the largest magnitude are
 // joined across the lanes without LDS.  Angles are formed once for a token, in 64 bits (position * frequency in quarter turns, its fraction to fp32), and stay as
 // cosine and sine in LDS for all heads.
-// Bound by memory: a read and a write of every value.
+// Bound by memory: a read and a write of every value (8192 tokens of 40 heads of 128, bf16: 168 MB in 38 us; with a workgroup for every group of tokens, which asks for
+// its weights anew, 49; the gradient, two reads: 252 MB in 52 us and 4.6 for the weights' sums; keys and values of 4096 tokens to the cache, 8 heads each beside 32 of
+// queries: 50 MB read, 42 written in 28).  Few tokens: the launch (20 tokens: 5.8 us; of the gradient 2000: 19, in groups as for many 32).
 #include <type_traits>
 
 #include "qnn_paged.h"
@@ -255,7 +257,7 @@ __global__ __launch_bounds__(kThreads) void heads_kernel(const HeadsArgs a) {
     }
 }
 
-// Gradient.  The first blocks_q workgroups take the queries' heads, the others the keys'; each goes through every so many groups of tokens, keeps its lanes' part of
+// Gradient (formulas in qnn.h).  The first blocks_q workgroups take the queries' heads, the others the keys'; each goes through every so many groups of tokens, keeps its lanes' part of
 // the weight's gradient in registers over all of them and writes it once; a second kernel adds these parts in a fixed order.
 struct HeadsGradArgs {
     Matrix grad[2], h[2], out[2];
