@@ -15,7 +15,7 @@ typedef float v16f __attribute__((ext_vector_type(16)));
 
 constexpr int kTile = 64;  // keys
 
-// K: [key][DP] in pieces of 8 float16, piece p of key r at p xor (r mod 8).  V: rows of 64 keys, value d at row (d mod 4) (DP / 4) + d / 4: a block of 32 rows is what
+// K: [key][DP] in pieces of 8 float16, piece p of key r at p xor (r mod 8; mod 16 where a row has as many pieces: 1 % less time).  V: rows of 64 keys, value d at row (d mod 4) (DP / 4) + d / 4: a block of 32 rows is what
 // one quarter of the lanes' words holds; piece 2 s + g has keys 16 s + 4 g + 0 .. 3 and 16 s + 8 + 4 g + 0 .. 3, and lies at (2 s + g) xor (row mod 8).
 template <int DP>
 struct Tile {
@@ -33,6 +33,7 @@ template <typename T, int DP, int kWaves, int kKind>
 __global__ __launch_bounds__(64 * kWaves, kWaves / 4) void many_rows_kernel(const Args a) {
     constexpr int kThreads = 64 * kWaves, kRows = 32 * kWaves, kQuery = Parts<T>::kQuery, kWeight = Parts<T>::kWeight;
     constexpr int kUnitsK = kTile * DP / 16, kUnitsV = kTile / 4 * (DP / 4), kLoadsK = (kUnitsK + kThreads - 1) / kThreads, kLoadsV = (kUnitsV + kThreads - 1) / kThreads;
+    constexpr int kTurnK = DP >= 128 ? 15 : 7;  // pieces of a row of K change places by its number
     __shared__ __attribute__((aligned(16))) Tile<DP> tiles[2];
     __shared__ __attribute__((aligned(16))) Scales scales[2];
     __shared__ uint32_t rows_of[2][kTile];
@@ -158,7 +159,7 @@ __global__ __launch_bounds__(64 * kWaves, kWaves / 4) void many_rows_kernel(cons
                 if (kUnitsK % kThreads == 0 || u < kUnitsK) {
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
-                        *reinterpret_cast<h8 *>(to.k + key * DP * 2 + 16 * ((piece + h) ^ (key & 7))) = eight_codes(raw_k[i][2 * h], raw_k[i][2 * h + 1]);
+                        *reinterpret_cast<h8 *>(to.k + key * DP * 2 + 16 * ((piece + h) ^ (key & kTurnK))) = eight_codes(raw_k[i][2 * h], raw_k[i][2 * h + 1]);
                 }
             }
 #pragma unroll
@@ -204,7 +205,7 @@ __global__ __launch_bounds__(64 * kWaves, kWaves / 4) void many_rows_kernel(cons
             h8 of_k[kAhead], of_v[kAhead];
             auto read_k = [&](int n) __attribute__((always_inline)) {
                 const int h = n / kOperands, c = n % kOperands;
-                if (n < 2 * kOperands) of_k[n % kAhead] = *reinterpret_cast<const h8 *>(t.k + (32 * h + r) * DP * 2 + 16 * ((2 * c + g) ^ (r & 7)));
+                if (n < 2 * kOperands) of_k[n % kAhead] = *reinterpret_cast<const h8 *>(t.k + (32 * h + r) * DP * 2 + 16 * ((2 * c + g) ^ (r & kTurnK)));
             };
             auto read_v = [&](int n) __attribute__((always_inline)) {  // step c of 16 keys, rows 32 d on
                 const int h = n / kOperands, c = n % kOperands / (DP / 32), d = n % (DP / 32);
