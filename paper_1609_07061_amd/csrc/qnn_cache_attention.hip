@@ -77,11 +77,14 @@ struct Query {
     }
 };
 
-// (waves that a SIMD is to hold: what is in flight grows with them)
-constexpr int waves_of(int DP, int NB, int parts) { return DP == 64 ? (NB == 1 ? 4 : 2) : (DP == 128 && NB == 1 ? 3 : (parts == 2 ? 1 : 2)); }
+// Waves that a SIMD is to hold: what is in flight grows with them.  (Heads of 64, 32 rows: three, though 8 registers are spilled then, 62 us for two's 64, 16 sequences of up
+// to 3000 tokens with 40 drafted, bf16; 41 for 46, 4 sequences with 100 new tokens, fp16.  With a cap or a bias 18 would be.)
+constexpr int waves_of(int DP, int NB, int parts, bool more) {
+    return DP == 64 ? (NB == 1 ? 4 : (parts == 2 || more ? 2 : 3)) : (DP == 128 && NB == 1 ? 3 : (parts == 2 ? 1 : 2));
+}
 
 template <typename T, int DP, int NB, bool kMore>
-__global__ __launch_bounds__(64 * kWaves, waves_of(DP, NB, Parts<T>::kQuery)) void few_rows_kernel(const Args a) {
+__global__ __launch_bounds__(64 * kWaves, waves_of(DP, NB, Parts<T>::kQuery, kMore)) void few_rows_kernel(const Args a) {
     constexpr int kRows = 16 * NB, kPitch = DP + 4, kV = DP / 64, kQuery = Parts<T>::kQuery, kWeight = Parts<T>::kWeight;
     __shared__ Keys keys[kWaves][2];
     __shared__ float2 states[kWaves][kRows];
@@ -507,7 +510,7 @@ Plan plan_of(int64_t sequences, int64_t heads_q, int64_t heads, int64_t D, int t
     const bool few = rows <= 768 || !takes_many(D, type);
     p.rows = few ? (rows <= 16 || D > 128 ? 16 : 32) : many_rows(D);
     p.blocks = ceil_div(rows, p.rows);
-    const int64_t on_unit = few ? waves_of(D <= 64 ? 64 : (D <= 128 ? 128 : 256), p.rows / 16, 1) : 1;
+    const int64_t on_unit = few ? waves_of(D <= 64 ? 64 : (D <= 128 ? 128 : 256), p.rows / 16, 1, false) : 1;
     const double blocks = (double)sequences * (double)heads * (double)p.blocks;
     const int64_t units = compute_units(), wanted = blocks < 1e12 ? (int64_t)blocks : (int64_t)1e12, per_turn = few ? kStep * kWaves : 256, turns = ceil_div(longest, per_turn);
     int64_t want = few || units / wanted < 2 ? ceil_div(on_unit * units, wanted) : units / wanted;
