@@ -137,7 +137,7 @@ def test_a_block_trains(seed):
 
     mix(formula(leaves[0], leaves[2]), formula(leaves[1], leaves[3])).backward(up.double())
     for got, leaf in zip((dx, dk, dgq, dgk), leaves):
-        # fp32 throughout: some thousand roundings of sums of T D terms
+        # fp32 throughout, 335 U of the largest: values turned and turned back are off by some 30 U each, scores by 100, and what remains averages over 40 keys
         assert ((got.double() - leaf.grad).abs() <= 2e-5 * leaf.grad.abs().max()).all()
 
 
