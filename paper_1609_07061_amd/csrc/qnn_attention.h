@@ -50,6 +50,7 @@ struct Args {
     float scale, cap;
     int64_t tokens, sequences;
     int32_t D, heads_q, group, splits, blocks;  // blocks: of rows, for each sequence and head of the cache
+    int32_t short_rows;  // 0, or: sequences of at most this many rows are the kernel's for few, the others that for many
     uint32_t group_inverse, heads_inverse, heads_q_inverse, splits_inverse, blocks_inverse;
     float *part;   // [splits][tokens][heads_q][D]: sums, where splits > 1
     float2 *state;  // [splits][tokens][heads_q]: R, sum of 2^(t - R)

@@ -100,6 +100,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NB, Parts<T>::kQuery, kMo
     if ((int64_t)b >= a.sequences) return;  // (of the launch's last line)
     const Sequence s = sequence_at(a, b);
     const uint32_t n_rows = (uint32_t)s.fresh * (uint32_t)a.group;
+    if (a.short_rows > 0 && n_rows > (uint32_t)a.short_rows) return;
     for (uint32_t first = block * kRows; first < n_rows; first += (uint32_t)a.blocks * kRows) {
         uint32_t in_group;
         const uint32_t last = min(first + kRows, n_rows) - 1u;
@@ -527,6 +528,10 @@ bool plannable(int64_t tokens, int64_t sequences, int64_t heads_q, int64_t heads
 }
 // (numbers above what there can be do no more than these)
 int64_t at_most(int64_t x, int64_t limit) { return x < limit ? x : limit; }
+// From so many sequences on, those with up to 16 rows are left to the kernel for few where the call is the kernel's for many: single tokens beside a prompt.  (us with and
+// without, 32 heads on 8 of 128, bf16: 2048 of 8192 tokens and 63 sequences of up to 8192 with one 533 and 1417, 1024 tokens and 7 sequences of up to 8000 149 and 228,
+// 512 of 2000 and 7 of up to 4000 143 and 123, 8 sequences of 600 with 300 each 68.7 and 68.4.)
+constexpr int64_t kMixed = 8;
 
 template <typename T, int DP, bool kMore>
 int launch_few(const Args &a, int rows, dim3 grid, hipStream_t s) {
@@ -598,9 +603,20 @@ extern "C" int qnn_cache_attention(const qnn_paged_cache *cache, const void *q, 
     a.part = part, a.state = reinterpret_cast<float2 *>(part + p.splits * queries * D);
     hipStream_t s = static_cast<hipStream_t>(stream);
     const dim3 grid = rows::grid_of((int64_t)blocks);
-    const int rc = p.rows > 32
-                       ? attention::launch_many(a, type, grid, s)
-                       : rows::with_type(type, [&](auto tag) { return attention::launch_few<decltype(tag)>(a, p.rows, grid, s); });
+    const auto few = [&](const attention::Args &a, int rows, dim3 grid) {
+        return rows::with_type(type, [&](auto tag) { return attention::launch_few<decltype(tag)>(a, rows, grid, s); });
+    };
+    int rc;
+    if (p.rows > 32) {
+        a.short_rows = cache->sequences >= attention::kMixed ? 16 : 0;
+        rc = attention::launch_many(a, type, grid, s);
+        if (rc == QNN_OK && a.short_rows > 0) {
+            a.blocks = 1, a.blocks_inverse = inverse_of(1);
+            rc = few(a, 16, rows::grid_of(cache->sequences * cache->heads * p.splits));
+        }
+    } else {
+        rc = few(a, p.rows, grid);
+    }
     if (rc || p.splits == 1) return rc;
     return rows::with_type(type, [&](auto tag) { return attention::launch_join<decltype(tag)>(a, s); });
 }

@@ -81,6 +81,20 @@ def test_many_rows(seed, case, type, kind, with_tree):
     test_attention(seed, case, type, kind, with_tree)
 
 
+# single tokens beside prompts: sequences of up to 16 rows of a head of the cache have a kernel of their own
+MIXED = [([700, 300, 1, 64, 200, 900, 33, 120, 5], [300, 1, 1, 8, 0, 2, 33, 100, 5], 4, 2, 64, 16), ([260, 70, 40, 1, 999, 128, 17, 3], [250, 1, 16, 1, 1, 17, 4, 3], 3, 1, 256, 7),
+         ([2500, 60, 900, 900, 31, 32, 33, 2000, 1100], [200, 1, 1, 2, 2, 1, 1, 1, 1], 16, 2, 128, 64)]
+
+
+@pytest.mark.parametrize("case", MIXED)
+@pytest.mark.parametrize("type,kind", EACH)
+@pytest.mark.parametrize("with_tree", [False, True])
+def test_prompts_and_tokens(seed, case, type, kind, with_tree):
+    lengths, fresh, H, heads, D, page = case
+    assert (sum(fresh) + 3) * H // heads > 768 and len(fresh) >= 8
+    test_attention(seed, case, type, kind, with_tree)
+
+
 @pytest.mark.parametrize("type", ["f32", "bf16"])
 @pytest.mark.parametrize("lengths,fresh,H,heads,D,page", [([20000], [1], 8, 2, 128, 16), ([9000, 3, 4000], [1, 1, 1], 2, 1, 256, 64), ([3000, 2500], [64, 40], 8, 2, 64, 16),
                                                           ([5000], [700], 8, 2, 128, 64)])
