@@ -528,7 +528,7 @@ bool plannable(int64_t tokens, int64_t sequences, int64_t heads_q, int64_t heads
 }
 // (numbers above what there can be do no more than these)
 int64_t at_most(int64_t x, int64_t limit) { return x < limit ? x : limit; }
-// From so many sequences on, those with up to 16 rows are left to the kernel for few where the call is the kernel's for many: single tokens beside a prompt.  (us with and
+// From so many sequences on, those with up to 16 rows, or one token, are left to the kernel for few where the call is the kernel's for many: tokens beside a prompt.  (us with and
 // without, 32 heads on 8 of 128, bf16: 2048 of 8192 tokens and 63 sequences of up to 8192 with one 533 and 1417, 1024 tokens and 7 sequences of up to 8000 149 and 228,
 // 512 of 2000 and 7 of up to 4000 143 and 123, 8 sequences of 600 with 300 each 68.7 and 68.4.)
 constexpr int64_t kMixed = 8;
@@ -608,11 +608,12 @@ extern "C" int qnn_cache_attention(const qnn_paged_cache *cache, const void *q, 
     };
     int rc;
     if (p.rows > 32) {
-        a.short_rows = cache->sequences >= attention::kMixed ? 16 : 0;
+        a.short_rows = cache->sequences >= attention::kMixed && a.group <= 64 ? (a.group > 16 ? a.group : 16) : 0;
         rc = attention::launch_many(a, type, grid, s);
         if (rc == QNN_OK && a.short_rows > 0) {
-            a.blocks = 1, a.blocks_inverse = inverse_of(1);
-            rc = few(a, 16, rows::grid_of(cache->sequences * cache->heads * p.splits));
+            const int rows = a.short_rows <= 16 || D > 128 ? 16 : 32;
+            a.blocks = (int32_t)ceil_div(a.short_rows, rows), a.blocks_inverse = inverse_of(a.blocks);  // (at most 4, and those of many rows more)
+            rc = few(a, rows, rows::grid_of(cache->sequences * cache->heads * p.splits * a.blocks));
         }
     } else {
         rc = few(a, p.rows, grid);

@@ -83,7 +83,9 @@ def test_many_rows(seed, case, type, kind, with_tree):
 
 # single tokens beside prompts: sequences of up to 16 rows of a head of the cache have a kernel of their own
 MIXED = [([700, 300, 1, 64, 200, 900, 33, 120, 5], [300, 1, 1, 8, 0, 2, 33, 100, 5], 4, 2, 64, 16), ([260, 70, 40, 1, 999, 128, 17, 3], [250, 1, 16, 1, 1, 17, 4, 3], 3, 1, 256, 7),
-         ([2500, 60, 900, 900, 31, 32, 33, 2000, 1100], [200, 1, 1, 2, 2, 1, 1, 1, 1], 16, 2, 128, 64)]
+         ([2500, 60, 900, 900, 31, 32, 33, 2000, 1100], [200, 1, 1, 2, 2, 1, 1, 1, 1], 16, 2, 128, 64),
+         ([500, 40, 900, 1, 3, 70, 33, 20], [60, 1, 1, 1, 2, 1, 1, 1], 24, 1, 128, 16), ([90, 40, 600, 1, 3, 70, 33, 20], [20, 1, 1, 1, 2, 1, 1, 1], 64, 1, 48, 16),
+         ([90, 40, 600, 1, 3, 70, 33, 20], [20, 1, 1, 1, 2, 1, 1, 1], 80, 2, 208, 16)]
 
 
 @pytest.mark.parametrize("case", MIXED)
