@@ -9,6 +9,9 @@
 // R follows the largest of t_j + log2(b_j) seen, so that w_j is at most 2^15 and the largest about 2^8: small weights keep their digits down to 2^-22 of it, however
 // the scales b_j differ.  It moves only when a weight would pass 2^15: the sums are multiplied by a power then, and nothing else.  Sums that belong to different R
 // (of waves, of parts of the keys) are joined in a fixed order.
+// The sum below the line has the factors 2^(t_j - R) without b_j, which are large where b_j is small, and where it is 0 nothing is seen of them in w_j: log2(b_j) counts as
+// kLowest at least, so that they are at most 2^104 of the keys that R has followed, and R moves too when a lane's sum of a step passes 2^109.  (2^22 tokens of zeros in one
+// part of the keys stay within fp32.)
 #pragma once
 #include <type_traits>
 
@@ -25,7 +28,8 @@ typedef uint32_t v2u __attribute__((ext_vector_type(2)));
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.44269504f;
-constexpr float kLowest = -100.0f;  // log2 of the least scale of values that R follows (zeros have none)
+constexpr float kLowest = -96.0f;   // log2 of the least scale of values that R follows: what zeros count as
+constexpr float kOfSum = 0x1p-94f;  // weight that a sum of 2^(t - R) counts as, over the up to 16 keys that a lane has at a time: 2^109 moves R, and each is up to 2^104 then
 
 // A lane's number that the compiler cannot see through: what follows from it is worked out where it is needed.  (Worked out once before the loops, addresses take
 // some 100 registers, and the sums are spilled.)
@@ -36,6 +40,10 @@ __device__ __forceinline__ int opaque(int x) {
 
 // log2 of a scale of values, rounded up, for R to follow
 __device__ __forceinline__ float log_scale(float v) { return v != 0.0f ? fmaxf((float)__builtin_amdgcn_frexp_expf(v), kLowest) : kLowest; }
+
+// The root of what sums that belong to one R are multiplied by for another one.  (Sums of 2^(t - R) are up to 2^128 and may count where the factor itself is below the normal
+// numbers: they take the root twice.)
+__device__ __forceinline__ float root_of(float level, float top) { return level == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(0.5f * (level - top)); }
 
 struct Args {
     const void *q;

@@ -15,9 +15,6 @@ namespace {
 
 constexpr int kStep = 32, kWaves = 4;
 
-// What sums that belong to one R are multiplied by for another one
-__device__ __forceinline__ float factor_of(float level, float top) { return level == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(level - top); }
-
 // Keys of a step, as a wave needs them: by the lane in memory order, in LDS
 struct __attribute__((aligned(16))) Keys {
     uint32_t row[kStep];
@@ -247,6 +244,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NB, Parts<T>::kQuery, kMo
                         }
                 };
                 weigh();
+                largest = fmaxf(largest, sum * kOfSum);
                 if (__any(level[n] == -INFINITY || largest > 32768.0f)) {
                     float most = -INFINITY;
 #pragma unroll
@@ -261,9 +259,9 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NB, Parts<T>::kQuery, kMo
                     largest = fmaxf(largest, __shfl_xor(largest, 32));
                     // (whether a query's R moves depends on that query alone)
                     const bool moves = (level[n] == -INFINITY || largest > 32768.0f) && most > level[n];
-                    const float now = moves ? most - 8.0f : level[n], factor = level[n] == now ? 1.0f : __builtin_amdgcn_exp2f(level[n] - now);
+                    const float now = moves ? most - 8.0f : level[n], root = level[n] == now ? 1.0f : root_of(level[n], now), factor = root * root;
                     level[n] = now;
-                    total[n] *= factor;
+                    total[n] = total[n] * root * root;
 #pragma unroll
                     for (int d = 0; d < DP / 16; ++d) out[d][n] *= factor;
                     weigh();
@@ -350,7 +348,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NB, Parts<T>::kQuery, kMo
         auto put = [&](bool add) __attribute__((always_inline)) {
 #pragma unroll
             for (int n = 0; n < NB; ++n) {
-                const float f = factor_of(level[n], most_of(16 * n + r));
+                const float root = root_of(level[n], most_of(16 * n + r)), f = root * root;
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
 #pragma unroll
@@ -373,7 +371,10 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NB, Parts<T>::kQuery, kMo
             const float most = most_of(row);
             float sum = 0.0f, y[8];
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) sum += states[w][row].y * factor_of(states[w][row].x, most);
+            for (int w = 0; w < kWaves; ++w) {
+                const float root = root_of(states[w][row].x, most);
+                sum += states[w][row].y * root * root;
+            }
 #pragma unroll
             for (int e = 0; e < 8; ++e) y[e] = sums[0][row][d + e] + sums[1][row][d + e];
             if (a.splits == 1) {
@@ -432,9 +433,9 @@ __global__ __launch_bounds__(256) void join_few_kernel(const Args a) {
     for (int s = 0; s < kParts; ++s) top = fmaxf(top, state[s].x);
 #pragma unroll
     for (int s = 0; s < kParts; ++s) {
-        const float factor = s < a.splits ? factor_of(state[s].x, top) : 0.0f;
+        const float root = s < a.splits ? root_of(state[s].x, top) : 0.0f, factor = root * root;
         const bool none = s >= a.splits || state[s].y == 0.0f;
-        total = none ? total : __fmaf_rn(state[s].y, factor, total);
+        total = none ? total : __fmaf_rn(state[s].y * root, root, total);
 #pragma unroll
         for (int e = 0; e < 4; ++e) y[e] = none ? y[e] : __fmaf_rn(factor, part[s][e], y[e]);
     }
@@ -466,8 +467,9 @@ __global__ __launch_bounds__(256) void join_many_kernel(const Args a) {
     float factor[2], total = 0.0f;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        factor[i] = factor_of(state[i].x, top);
-        total = __fmaf_rn(state[i].y, factor[i], total);
+        const float root = root_of(state[i].x, top);
+        factor[i] = root * root;
+        total = __fmaf_rn(state[i].y * root, root, total);
         if (state[i].y == 0.0f) factor[i] = -1.0f;  // (nothing there)
     }
 #pragma unroll

@@ -302,6 +302,7 @@ __global__ __launch_bounds__(64 * kWaves, kWaves / 4) void many_rows_kernel(cons
             };
             // moves R where a weight would be too large, which is seldom, and takes the half's sum in
             auto settle = [&](int h) __attribute__((always_inline)) {
+                largest = fmaxf(largest, sum * kOfSum);
                 if (__any(level == -INFINITY || largest > 32768.0f)) {
                     asm volatile("" ::: "memory");
                     float most = -INFINITY;
@@ -314,9 +315,9 @@ __global__ __launch_bounds__(64 * kWaves, kWaves / 4) void many_rows_kernel(cons
                     most = fmaxf(most, __shfl_xor(most, 32)), largest = fmaxf(largest, __shfl_xor(largest, 32));
                     // (whether a query's R moves, and what it gets, depends on that query alone)
                     const bool moves = (level == -INFINITY || largest > 32768.0f) && most > level;
-                    const float now = moves ? most - 8.0f : level, factor = level == now ? 1.0f : __builtin_amdgcn_exp2f(level - now);
+                    const float now = moves ? most - 8.0f : level, root = level == now ? 1.0f : root_of(level, now), factor = root * root;
                     level = now;
-                    total *= factor;
+                    total = total * root * root;
 #pragma unroll
                     for (int d = 0; d < DP / 32; ++d) out[d] *= factor;
                     begin();
