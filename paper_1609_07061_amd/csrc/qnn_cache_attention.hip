@@ -80,8 +80,10 @@ constexpr int waves_of(int DP, int NB, int parts, bool more) {
     return DP == 64 ? (NB == 1 ? 4 : (parts == 2 || more ? 2 : 3)) : (DP == 128 && NB == 1 ? 3 : (parts == 2 ? 1 : 2));
 }
 
-template <typename T, int DP, int NB, bool kMore>
-__global__ __launch_bounds__(64 * kWaves, waves_of(DP, NB, Parts<T>::kQuery, kMore)) void few_rows_kernel(const Args a) {
+// kKind: 0 plain scores, 1 a bias by distance or a cap, 2 a cap that is close
+template <typename T, int DP, int NB, int kKind>
+__global__ __launch_bounds__(64 * kWaves, waves_of(DP, NB, Parts<T>::kQuery, kKind > 0)) void few_rows_kernel(const Args a) {
+    constexpr bool kMore = kKind > 0, kClose = kKind == 2;
     constexpr int kRows = 16 * NB, kPitch = DP + 4, kV = DP / 64, kQuery = Parts<T>::kQuery, kWeight = Parts<T>::kWeight;
     __shared__ Keys keys[kWaves][2];
     __shared__ float2 states[kWaves][kRows];
@@ -107,7 +109,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NB, Parts<T>::kQuery, kMo
         const int64_t steps = (end + (int64_t)kStep - 1) / kStep;
         const int32_t lo = (int32_t)(steps * split / a.splits), hi = (int32_t)(steps * (split + 1) / a.splits);
 
-        const Cap cap = kMore && a.cap > 0.0f ? cap_of(a) : Cap{};
+        const Cap cap = kClose || (kMore && !kAlwaysClose<T> && a.cap > 0.0f) ? cap_of<kClose>(a) : Cap{};
         Query<T, DP> query[NB];
         Sight sight[NB];
         v4f out[DP / 16][NB] = {};
@@ -210,7 +212,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NB, Parts<T>::kQuery, kMo
                         // (the scales first: a key that is not there has 0, and no product with it may overflow)
                         float x = dots[h][n][e] * (query[n].mult * k_scale[h][e]);
                         if constexpr (kMore) {
-                            if (a.cap > 0.0f) x = capped<kQuery == 2>(cap, x);
+                            if (kClose || (!kAlwaysClose<T> && a.cap > 0.0f)) x = capped<kClose>(cap, x);
                             if (a.slopes) x = __fmaf_rn(sight[n].slope, (float)(k.place[16 * h + 4 * g + e] - sight[n].place), x);
                         }
                         t[h][e] = x + bias[h][e];
@@ -316,7 +318,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NB, Parts<T>::kQuery, kMo
 #pragma unroll
             for (int n = 0; n < NB; ++n) {
                 query[n].make(a);
-                query[n].mult *= kMore && a.cap > 0.0f ? cap.inverse : kLog2e;
+                query[n].mult *= kClose || (kMore && !kAlwaysClose<T> && a.cap > 0.0f) ? cap.before : kLog2e;
             }
             int turn = 0;
             for (int32_t step = step0; step < hi; step += kWaves) {
@@ -535,17 +537,20 @@ int64_t at_most(int64_t x, int64_t limit) { return x < limit ? x : limit; }
 // 512 of 2000 and 7 of up to 4000 143 and 123, 8 sequences of 600 with 300 each 68.7 and 68.4.)
 constexpr int64_t kMixed = 8;
 
-template <typename T, int DP, bool kMore>
+template <typename T, int DP, int kKind>
 int launch_few(const Args &a, int rows, dim3 grid, hipStream_t s) {
-    if (DP > 128 || rows == 16) return QNN_LAUNCH("cache_attention", (few_rows_kernel<T, DP, 1, kMore>), grid, dim3(64 * kWaves), 0, s, a);
-    if constexpr (DP <= 128) return QNN_LAUNCH("cache_attention", (few_rows_kernel<T, DP, 2, kMore>), grid, dim3(64 * kWaves), 0, s, a);
+    if (DP > 128 || rows == 16) return QNN_LAUNCH("cache_attention", (few_rows_kernel<T, DP, 1, kKind>), grid, dim3(64 * kWaves), 0, s, a);
+    if constexpr (DP <= 128) return QNN_LAUNCH("cache_attention", (few_rows_kernel<T, DP, 2, kKind>), grid, dim3(64 * kWaves), 0, s, a);
+}
+template <typename T, int DP>
+int launch_few(const Args &a, int rows, dim3 grid, hipStream_t s) {
+    if (a.cap > (kAlwaysClose<T> ? 0.0f : kCloseFrom)) return launch_few<T, DP, 2>(a, rows, grid, s);
+    return a.cap > 0.0f || a.slopes ? launch_few<T, DP, 1>(a, rows, grid, s) : launch_few<T, DP, 0>(a, rows, grid, s);
 }
 template <typename T>
 int launch_few(const Args &a, int rows, dim3 grid, hipStream_t s) {
-    const bool more = a.cap > 0.0f || a.slopes;
-    if (a.D <= 64) return more ? launch_few<T, 64, true>(a, rows, grid, s) : launch_few<T, 64, false>(a, rows, grid, s);
-    if (a.D <= 128) return more ? launch_few<T, 128, true>(a, rows, grid, s) : launch_few<T, 128, false>(a, rows, grid, s);
-    return more ? launch_few<T, 256, true>(a, rows, grid, s) : launch_few<T, 256, false>(a, rows, grid, s);
+    if (a.D <= 64) return launch_few<T, 64>(a, rows, grid, s);
+    return a.D <= 128 ? launch_few<T, 128>(a, rows, grid, s) : launch_few<T, 256>(a, rows, grid, s);
 }
 
 }  // namespace

@@ -28,7 +28,7 @@ struct __attribute__((aligned(16))) Scales {
     int32_t all_there;
 };
 
-// kKind: 0 plain scores, 1 a bias by distance, 2 capped, with a bias or not
+// kKind: 0 plain scores, 1 a bias by distance, 2 capped, with a bias or not, 3 by a cap that is close
 template <typename T, int DP, int kWaves, int kKind>
 __global__ __launch_bounds__(64 * kWaves, kWaves / 4) void many_rows_kernel(const Args a) {
     constexpr int kThreads = 64 * kWaves, kRows = 32 * kWaves, kQuery = Parts<T>::kQuery, kWeight = Parts<T>::kWeight;
@@ -66,7 +66,7 @@ __global__ __launch_bounds__(64 * kWaves, kWaves / 4) void many_rows_kernel(cons
         // ---- the query: DP / 16 steps of 16 values, 8 g + 0 .. 7 of each in this lane
         h8 query[kQuery][DP / 16];
         float mult;
-        const Cap cap = kKind == 2 ? cap_of(a) : Cap{};
+        const Cap cap = kKind >= 2 ? cap_of<kKind == 3>(a) : Cap{};
         Sight sight;
         {
             T x[DP / 16][8];
@@ -84,7 +84,7 @@ __global__ __launch_bounds__(64 * kWaves, kWaves / 4) void many_rows_kernel(cons
             }
             top = max(top, (uint32_t)__shfl_xor((int)top, 32));
             const Scaling scaling(top);
-            mult = scaling.mult(a.scale) * (kKind == 2 ? cap.inverse : kLog2e);
+            mult = scaling.mult(a.scale) * (kKind >= 2 ? cap.before : kLog2e);
 #pragma unroll
             for (int c = 0; c < DP / 16; ++c)
 #pragma unroll
@@ -245,11 +245,11 @@ __global__ __launch_bounds__(64 * kWaves, kWaves / 4) void many_rows_kernel(cons
             // scores times log2(e), -infinity where a row does not see a key
             auto score = [&](int h) __attribute__((always_inline)) {
                 if constexpr (kKind > 0) scale(h);
-                if constexpr (kKind == 2) {
+                if constexpr (kKind >= 2) {
 #pragma unroll
-                    for (int x = 0; x < 16; ++x) dots[h][x] = capped<kQuery == 2>(cap, dots[h][x]);
+                    for (int x = 0; x < 16; ++x) dots[h][x] = capped<kKind == 3>(cap, dots[h][x]);
                 }
-                if (kKind == 1 || (kKind == 2 && a.slopes)) {
+                if (kKind == 1 || (kKind >= 2 && a.slopes)) {
                     const float place = (float)(sight.place - tile * kTile);  // (from the tile's beginning: whole numbers, exact)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
@@ -425,7 +425,8 @@ __global__ __launch_bounds__(64 * kWaves, kWaves / 4) void many_rows_kernel(cons
 
 template <typename T, int DP, int kWaves>
 int launch(const Args &a, dim3 grid, hipStream_t s) {
-    auto kernel = a.cap > 0.0f ? many_rows_kernel<T, DP, kWaves, 2> : (a.slopes ? many_rows_kernel<T, DP, kWaves, 1> : many_rows_kernel<T, DP, kWaves, 0>);
+    auto kernel = a.cap > 0.0f ? (a.cap > kCloseFrom ? many_rows_kernel<T, DP, kWaves, 3> : many_rows_kernel<T, DP, kWaves, kAlwaysClose<T> ? 3 : 2>)
+                               : (a.slopes ? many_rows_kernel<T, DP, kWaves, 1> : many_rows_kernel<T, DP, kWaves, 0>);
     return QNN_LAUNCH("cache_attention", kernel, grid, dim3(64 * kWaves), 0, s, a);
 }
 
