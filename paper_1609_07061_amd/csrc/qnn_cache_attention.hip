@@ -136,7 +136,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NB, Parts<T>::kQuery, kKi
             if (kMore && a.tree && x.place >= s.base && row != paged::kNoRow && x.place - s.base < s.fresh)
                 x.place = s.base - 1 + __popcll(a.tree[s.first + (x.place - s.base)]);
         };
-        auto note = [&](const Ahead &x, Keys &k) __attribute__((always_inline)) {
+        auto note = [&](const Ahead &x, Keys &k) __attribute__((always_inline)) -> bool {  // whether all are there
             const bool there = x.row != paged::kNoRow;
             if (lane < kStep) {
                 k.row[at] = there ? x.row : 0u;
@@ -148,6 +148,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NB, Parts<T>::kQuery, kKi
             __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
             __builtin_amdgcn_wave_barrier();
             __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+            return __all(there);
         };
         Codes<DP> c;
         auto fetch_k = [&](const Keys &k) __attribute__((always_inline)) {
@@ -191,16 +192,15 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NB, Parts<T>::kQuery, kKi
                                 dots[h][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes, query[n].part[p][i][f], dots[h][n], 0, 0, 0);
                     }
         };
-        auto use_v = [&](int32_t step, const Keys &k) __attribute__((always_inline)) {
+        auto use_v = [&](int32_t step, const Keys &k, bool all_there) __attribute__((always_inline)) {
             const int g = opaque(threadIdx.x & 63) >> 4;
-            v4f k_scale[2], v_scale[2], bias[2];
+            v4f k_scale[2], v_scale[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int from = 16 * h + 4 * g;
                 k_scale[h] = *reinterpret_cast<const v4f *>(&k.k_scale[from]), v_scale[h] = *reinterpret_cast<const v4f *>(&k.v_scale[from]);
-                bias[h] = *reinterpret_cast<const v4f *>(&k.bias[from]);
             }
-            const bool masked = (step + 1) * (int64_t)kStep > open;
+            const bool masked = (step + 1) * (int64_t)kStep > open || !all_there;
             h8 weights[NB][kWeight];
 #pragma unroll
             for (int n = 0; n < NB; ++n) {
@@ -209,19 +209,23 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NB, Parts<T>::kQuery, kKi
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        // (the scales first: a key that is not there has 0, and no product with it may overflow)
                         float x = dots[h][n][e] * (query[n].mult * k_scale[h][e]);
                         if constexpr (kMore) {
                             if (kClose || (!kAlwaysClose<T> && a.cap > 0.0f)) x = capped<kClose>(cap, x);
                             if (a.slopes) x = __fmaf_rn(sight[n].slope, (float)(k.place[16 * h + 4 * g + e] - sight[n].place), x);
                         }
-                        t[h][e] = x + bias[h][e];
+                        t[h][e] = x;
                     }
                 auto mask = [&](auto tree) __attribute__((always_inline)) {
 #pragma unroll
-                    for (int h = 0; h < 2; ++h)
+                    for (int h = 0; h < 2; ++h) {
+                        const v4f bias = *reinterpret_cast<const v4f *>(&k.bias[16 * h + 4 * g]);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) t[h][e] = sight[n].template sees<decltype(tree)::value>(s, step * kStep + 16 * h + 4 * g + e) ? t[h][e] : -INFINITY;
+                        for (int e = 0; e < 4; ++e) {
+                            const bool sees = sight[n].template sees<decltype(tree)::value>(s, step * kStep + 16 * h + 4 * g + e) & (bias[e] == 0.0f);
+                            t[h][e] = sees ? t[h][e] : -INFINITY;
+                        }
+                    }
                 };
                 if (masked) {
                     if (a.tree)
@@ -308,8 +312,9 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NB, Parts<T>::kQuery, kKi
             }
             scales(step0, row, ahead);
             row = find(step0 + kWaves);
+            bool all_there = true;
             if (step0 < hi) {
-                note(ahead, keys[wave][0]);
+                all_there = note(ahead, keys[wave][0]);
                 fetch_k(keys[wave][0]);
                 fetch_v(keys[wave][0]);
             }
@@ -323,9 +328,10 @@ __global__ __launch_bounds__(64 * kWaves, waves_of(DP, NB, Parts<T>::kQuery, kKi
             int turn = 0;
             for (int32_t step = step0; step < hi; step += kWaves) {
                 use_k();
-                note(ahead, keys[wave][turn ^ 1]);
+                const bool next_there = note(ahead, keys[wave][turn ^ 1]);
                 if (step + kWaves < hi) fetch_k(keys[wave][turn ^ 1]);
-                use_v(step, keys[wave][turn]);
+                use_v(step, keys[wave][turn], all_there);
+                all_there = next_there;
                 turn ^= 1;
                 if (step + kWaves < hi) fetch_v(keys[wave][turn]);
                 scales(step + 2 * kWaves, row, ahead);
