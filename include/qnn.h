@@ -396,13 +396,14 @@ typedef struct {
  *   n = h / sqrt(mean(h^2) + eps) * gamma   (gamma NULL: n = h),   then of every pair  y_a = n_a cos - n_b sin,  y_b = n_b cos + n_a sin.
  * q, k: DEVICE, value d of head h of token t at t * ld + h * step + d, of `type`; q_out, k_out likewise, and they may be q, k themselves (same strides).
  * heads_k may be 0 (k, k_out NULL).  gamma_q, gamma_k: DEVICE [D] of float32 or `type` (gamma_type), both or neither.  D a multiple of 16, at most 256.
- * What counts as not finite is as in qnn_rms_norm_quant: such a head is NaN or infinite. */
+ * What counts as not finite is as in qnn_rms_norm_quant: such a head is NaN or infinite.  A head of zeros is zeros, also where eps is 0. */
 int qnn_qk_norm_rotate(const void *q, int64_t ld_q, int64_t step_q, int64_t heads_q, const void *k, int64_t ld_k, int64_t step_k, int64_t heads_k, int type,
                        const void *gamma_q, const void *gamma_k, int gamma_type, float eps, const qnn_rotation *rotation, int64_t tokens, int64_t D, void *q_out,
                        int64_t ld_q_out, int64_t step_q_out, void *k_out, int64_t ld_k_out, int64_t step_k_out, void *stream);
 
 /* Its gradient.  With g = grad turned back by the same angles and r = 1 / sqrt(mean(h^2) + eps):
  *   out = r (gamma g - h r^2 mean(gamma g h)),   grad_gamma = sum over tokens and heads of g h r   (DEVICE float32 [D]);   gamma NULL: out = g.
+ * A head that the forward call counts as not finite, or one of zeros without eps, has no finite gradient: its part of out and all of grad_gamma are NaN or infinite.
  * q, k: what the forward call read.  out_q may be grad_q, out_k grad_k (same strides).  tokens >= 1 where there is a gamma.  workspace: DEVICE, 256-byte aligned,
  * qnn_qk_norm_rotate_backward_workspace_bytes(...) bytes (without gamma none).  Sums are formed in a fixed order. */
 int qnn_qk_norm_rotate_backward(const void *grad_q, int64_t ld_grad_q, int64_t step_grad_q, const void *grad_k, int64_t ld_grad_k, int64_t step_grad_k, const void *q,

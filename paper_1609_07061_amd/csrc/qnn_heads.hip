@@ -120,7 +120,8 @@ __device__ __forceinline__ void load_gamma(const void *gamma, bool is_f32, const
     load_either<false, T>(gamma, is_f32, Window(l.second, D), D, y);
 }
 
-// norm_factor of a head, from the sum of its squares: the root's reciprocal within a unit in the last place, without a root and a quotient
+// norm_factor of a head, from the sum of its squares: the root's reciprocal within a unit in the last place, without a root and a quotient.  Infinite for a head of zeros
+// without eps, as for one whose squares are below the normal numbers: heads_kernel tells them apart.
 __device__ __forceinline__ float head_factor(float total, float inverse_D, float eps) {
     const float mean = __fmaf_rn(total, inverse_D, eps);
     if (mean < 0x1p-126f) return __uint_as_float(0x7F800000u);
@@ -222,7 +223,13 @@ __global__ __launch_bounds__(kThreads) void heads_kernel(const HeadsArgs a) {
                     float sum = 0.0f;
 #pragma unroll
                     for (int i = 0; i < kVec; ++i) sum = __fmaf_rn(x[i], x[i], sum), sum = __fmaf_rn(y[i], y[i], sum);
-                    const float r = head_factor(sum_of_head<G>(sum), a.inverse_D, a.eps);
+                    float r = head_factor(sum_of_head<G>(sum), a.inverse_D, a.eps);
+                    if (magnitude(r) == 0x7F800000u) {  // (the same for all lanes of the head)
+                        uint32_t top = 0u;
+#pragma unroll
+                        for (int i = 0; i < kVec; ++i) top = max(top, max(magnitude(x[i]), magnitude(y[i])));
+                        if (most_of_head<G>(top) == 0u) r = 0.0f;
+                    }
 #pragma unroll
                     for (int i = 0; i < kVec; ++i) {
                         x[i] = x[i] * r * (q ? gamma[0][0][i] : gamma[1][0][i]);
