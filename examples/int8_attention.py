@@ -32,8 +32,7 @@ class Attention:
         self.codes, self.scale, self.h = new(T, width, dtype=torch.int8), new(T, dtype=torch.float32), new(T, width)
         self.rows, self.mixed, self.y = new(T, (heads + 2 * kv) * size), new(T, heads, size), new(T, width)
         self.mixed_codes, self.mixed_scale = new(T, heads * size, dtype=torch.int8), new(T, dtype=torch.float32)
-        # (fewer rows are split into more parts: the most that any number of tokens, shared among the sequences in any way, asks for)
-        need = max(q.qnn_cache_attention_workspace_bytes(t, sequences, heads, kv, size, n, longest) for t in range(1, T + 1) for n in range(-(-t // sequences), t + 1))
+        need = q.qnn_cache_attention_workspace_bytes(T, sequences, heads, kv, size, T, longest)  # (enough for fewer tokens, shared among the sequences in any way)
         self.workspace = new(max(need, 1), dtype=torch.uint8)
         self.longest = longest
 

@@ -428,7 +428,8 @@ int qnn_cache_append(const qnn_paged_cache *cache, const void *q, int64_t ld_q, 
  * place is the index in the sequence; with a tree that of a new token is n - m - 1 + (bits set in its mask).
  * q, out: DEVICE [tokens][heads_q][D] with strides as above, of `type`; slopes: DEVICE float32 [heads_q] or NULL; tree: DEVICE uint64 [tokens] or NULL.
  * most_new, longest: the most new tokens of a sequence and the longest sequence, as far as the host knows; they set how the work is split, so that results depend
- * on them in the last places, and any numbers >= 1 are right.  workspace: DEVICE, 256-byte aligned, qnn_cache_attention_workspace_bytes(...) bytes (0: none).
+ * on them in the last places, and any numbers >= 1 are right.  workspace: DEVICE, 256-byte aligned, qnn_cache_attention_workspace_bytes(...) bytes (0: none), which are enough for
+ * all calls with these heads of no more tokens and no longer sequences, whatever their numbers of sequences and new tokens.
  * A scale of the cache that is NaN makes every query NaN that sees it, and no other.  A query that is not finite gets NaN, if it sees anything.  Sums are formed in a
  * fixed order. */
 int qnn_cache_attention(const qnn_paged_cache *cache, const void *q, int64_t ld_q, int64_t step_q, int64_t heads_q, int type, float scale, float cap,

@@ -985,6 +985,7 @@ def qnn_cache_append(cache, table: torch.Tensor, starts: torch.Tensor, lengths: 
 
 
 def qnn_cache_attention_workspace_bytes(tokens: int, sequences: int, heads_q: int, heads: int, D: int, most_new: int, longest: int) -> int:
+    """Enough for all calls with these heads of no more tokens and no longer sequences, whatever their numbers of sequences and new tokens."""
     return int(_lib.qnn_cache_attention_workspace_bytes(tokens, sequences, heads_q, heads, D, most_new, longest))
 
 

@@ -536,6 +536,14 @@ bool plannable(int64_t tokens, int64_t sequences, int64_t heads_q, int64_t heads
     return tokens >= 1 && tokens <= 0x7FFFFFFF && sequences >= 1 && sequences <= 0x3FFFFFFF && heads >= 1 && heads_q >= 1 && heads_q % heads == 0 &&
            heads_q <= 65535 && D >= 16 && D <= paged::kMostD && most_new >= 1 && longest >= 1;
 }
+// Rows (queries and heads) times parts that a call has at most: what its workspace is for.  More tokens or longer sequences never have less, so that a workspace made for the most
+// serves all calls.  No plan for the tokens that sequences can have (sequences * most_new) comes to the second bound: two parts or more are made of fewer workgroups than 7.5 a unit
+// with 32 rows each, or than one a unit with 256, and there is at most one part more than that many workgroups in all give.  Calls of more tokens, nobody's for the most part, are
+// split into fewer.
+int64_t most_rows(int64_t rows, int64_t longest) {
+    const int64_t turns = ceil_div(longest, kStep * kWaves), parts = turns < kMostSplits ? turns : kMostSplits, most = 512 * (int64_t)compute_units();
+    return parts == 1 ? 0 : (rows * parts < most ? rows * parts : most);
+}
 // (numbers above what there can be do no more than these)
 int64_t at_most(int64_t x, int64_t limit) { return x < limit ? x : limit; }
 // From so many sequences on, those with up to 16 rows, or one token, are left to the kernel for few where the call is the kernel's for many: tokens beside a prompt.  (us with and
@@ -568,12 +576,7 @@ using namespace qnn;
 extern "C" size_t qnn_cache_attention_workspace_bytes(int64_t tokens, int64_t sequences, int64_t heads_q, int64_t heads, int64_t D, int64_t most_new,
                                                       int64_t longest) {
     if (!attention::plannable(tokens, sequences, heads_q, heads, D, most_new, longest)) return 0;
-    int64_t splits = 1;  // (enough for any type)
-    for (int type : {QNN_F32, QNN_BF16}) {
-        const attention::Plan p = attention::plan_of(sequences, heads_q, heads, D, type, attention::at_most(most_new, tokens), attention::at_most(longest, 0x7FFFFFFF));
-        if (p.splits > splits) splits = p.splits;
-    }
-    return splits == 1 ? 0 : (size_t)splits * (size_t)tokens * (size_t)heads_q * ((size_t)D * 4 + 8);
+    return (size_t)attention::most_rows(tokens * heads_q, attention::at_most(longest, 0x7FFFFFFF)) * ((size_t)D * 4 + 8);
 }
 
 extern "C" int qnn_cache_attention(const qnn_paged_cache *cache, const void *q, int64_t ld_q, int64_t step_q, int64_t heads_q, int type, float scale, float cap,
@@ -598,8 +601,10 @@ extern "C" int qnn_cache_attention(const qnn_paged_cache *cache, const void *q, 
     if (!rows::aligned_to(q, w) || !rows::aligned_to(out, w) || !rows::aligned_to(slopes, 4) || !rows::aligned_to(tree, 8))
         return fail(QNN_ERR_ALIGN, "%s: pointer not aligned to its type", what);
     most_new = attention::at_most(most_new, tokens), longest = attention::at_most(longest, 0x7FFFFFFF);
-    const attention::Plan p = attention::plan_of(cache->sequences, heads_q, cache->heads, D, type, most_new, longest);
-    const size_t need = qnn_cache_attention_workspace_bytes(tokens, cache->sequences, heads_q, cache->heads, D, most_new, longest);
+    attention::Plan p = attention::plan_of(cache->sequences, heads_q, cache->heads, D, type, most_new, longest);
+    const int64_t parts = attention::most_rows(tokens * heads_q, longest) / (tokens * heads_q);
+    p.splits = p.splits <= parts ? p.splits : (parts > 1 ? parts : 1);
+    const size_t need = p.splits == 1 ? 0 : qnn_cache_attention_workspace_bytes(tokens, cache->sequences, heads_q, cache->heads, D, most_new, longest);
     if (need > 0 && (!workspace || !rows::aligned_to(workspace, 256) || workspace_bytes < need))
         return fail(QNN_ERR_WORKSPACE, "%s: workspace NULL, misaligned or smaller than %zu bytes", what, need);
     const double blocks = (double)cache->sequences * (double)cache->heads * (double)p.blocks * (double)p.splits;
