@@ -405,7 +405,7 @@ int qnn_qk_norm_rotate(const void *q, int64_t ld_q, int64_t step_q, int64_t head
  *   out = r (gamma g - h r^2 mean(gamma g h)),   grad_gamma = sum over tokens and heads of g h r   (DEVICE float32 [D]);   gamma NULL: out = g.
  * A head that the forward call counts as not finite, or one of zeros without eps, has no finite gradient: its part of out and all of grad_gamma are NaN or infinite.
  * q, k: what the forward call read.  out_q may be grad_q, out_k grad_k (same strides).  tokens >= 1 where there is a gamma.  workspace: DEVICE, 256-byte aligned,
- * qnn_qk_norm_rotate_backward_workspace_bytes(...) bytes (without gamma none).  Sums are formed in a fixed order. */
+ * qnn_qk_norm_rotate_backward_workspace_bytes(...) bytes (without gamma none), which are enough for fewer tokens too.  Sums are formed in a fixed order. */
 int qnn_qk_norm_rotate_backward(const void *grad_q, int64_t ld_grad_q, int64_t step_grad_q, const void *grad_k, int64_t ld_grad_k, int64_t step_grad_k, const void *q,
                                 int64_t ld_q, int64_t step_q, int64_t heads_q, const void *k, int64_t ld_k, int64_t step_k, int64_t heads_k, int type,
                                 const void *gamma_q, const void *gamma_k, int gamma_type, float eps, const qnn_rotation *rotation, int64_t tokens, int64_t D,

@@ -355,14 +355,18 @@ constexpr int64_t kResident = 4, kMostBlocks = 1024;  // workgroups of heads_ker
 struct Split {
     int64_t q, k;
 };
-Split split_of(int64_t tokens, int64_t heads_q, int64_t heads_k, int64_t per_block) {
-    const int64_t groups = ceil_div(tokens, per_block);
+Split limits_of(int64_t heads_q, int64_t heads_k) {
     auto of = [&](int64_t heads) -> int64_t {
-        if (heads == 0) return 0;
-        const int64_t most = kMostBlocks * heads / (heads_q + heads_k), limit = most < 1 ? 1 : most;
-        return ceil_div(groups, ceil_div(groups, limit));
+        const int64_t most = kMostBlocks * heads / (heads_q + heads_k);
+        return heads == 0 ? 0 : (most < 1 ? 1 : most);
     };
     return {of(heads_q), of(heads_k)};
+}
+Split split_of(int64_t tokens, int64_t heads_q, int64_t heads_k, int64_t per_block) {
+    const int64_t groups = ceil_div(tokens, per_block);
+    const Split limits = limits_of(heads_q, heads_k);
+    auto of = [&](int64_t limit) -> int64_t { return limit == 0 ? 0 : ceil_div(groups, ceil_div(groups, limit)); };
+    return {of(limits.q), of(limits.k)};
 }
 // Tokens that a workgroup takes at a time: one while there are few, so that they spread over the card
 int tokens_per_block(int64_t tokens) { return tokens < 4 * 1024 ? 1 : kMostTokens; }
@@ -454,8 +458,9 @@ extern "C" int qnn_qk_norm_rotate(const void *q, int64_t ld_q, int64_t step_q, i
 
 extern "C" size_t qnn_qk_norm_rotate_backward_workspace_bytes(int64_t tokens, int64_t heads_q, int64_t heads_k, int64_t D) {
     if (tokens < 1 || tokens > 0x7FFFFFFF || heads_q < 0 || heads_k < 0 || heads_q > 65535 || heads_k > 65535 || heads_q + heads_k < 1 || D < 16 || D > paged::kMostD) return 0;
-    const Split s = split_of(tokens, heads_q, heads_k, tokens_per_group(tokens));
-    return (size_t)(s.q + s.k) * (size_t)D * 4;
+    // (more tokens may have fewer workgroups, but never need less)
+    const Split limits = limits_of(heads_q, heads_k);
+    return (size_t)((tokens < limits.q ? tokens : limits.q) + (tokens < limits.k ? tokens : limits.k)) * (size_t)D * 4;
 }
 
 extern "C" int qnn_qk_norm_rotate_backward(const void *grad_q, int64_t ld_grad_q, int64_t step_grad_q, const void *grad_k, int64_t ld_grad_k, int64_t step_grad_k,
