@@ -4,9 +4,10 @@
 // order; the sums over keys of a query are per lane until the end.  Codes go from memory to registers, 16 bytes of K a lane and D / 16 of V (whole rows a load), and
 // become float16 there; V's transposition is the choice of bytes in that step.
 // Single tokens are bound by memory (64 sequences of up to 8192 tokens, 32 heads on 8 of 128, bf16: 618 MB in 126 us, and 5 for the join of four parts), of one sequence
-// by latency: page numbers, scales, codes, one after the other, before the first product (10000 tokens, 21 MB: 10.8 us and 3.8).  Drafted trees and short prompts are
-// bound by the vector instructions that make codes float16 and scores weights: some 750 a step of 32 rows, of 48 matrix instructions (8 sequences of up to 4099 tokens,
-// 40 drafted each, 16 heads on 4 of 128, fp16, capped: 46 us and 4 for the join).
+// by latency: page numbers, scales, codes, one after the other, before the first product (10000 tokens, 21 MB: 11 us and 4).  Drafted trees and short prompts take some 750
+// vector instructions, which make codes float16 and scores weights, a step of 32 rows, and 48 matrix instructions; what bounds them is the longest sequences' workgroups, for all
+// sequences have the same number of parts (8 sequences of up to 4099 tokens, 40 drafted each, 16 heads on 4 of 128, fp16, capped: 44 us and 4.5 for the join, vector units
+// 39 % busy).
 #include "qnn_attention.h"
 
 namespace qnn {
@@ -74,8 +75,8 @@ struct Query {
     }
 };
 
-// Waves that a SIMD is to hold: what is in flight grows with them.  (Heads of 64, 32 rows: three, though 8 registers are spilled then, 62 us for two's 64, 16 sequences of up
-// to 3000 tokens with 40 drafted, bf16; 41 for 46, 4 sequences with 100 new tokens, fp16.  With a cap or a bias 18 would be.)
+// Waves that a SIMD is to hold: what is in flight grows with them.  (Heads of 64, 32 rows: three 62 us for two's 64, 16 sequences of up to 3000 tokens with 40 drafted, bf16; 41 for
+// 46, 4 sequences with 100 new tokens, fp16.  With a cap or a bias registers would be spilled.)
 constexpr int waves_of(int DP, int NB, int parts, bool more) {
     return DP == 64 ? (NB == 1 ? 4 : (parts == 2 || more ? 2 : 3)) : (DP == 128 && NB == 1 ? 3 : (parts == 2 ? 1 : 2));
 }
@@ -547,8 +548,9 @@ int64_t most_rows(int64_t rows, int64_t longest) {
 // (numbers above what there can be do no more than these)
 int64_t at_most(int64_t x, int64_t limit) { return x < limit ? x : limit; }
 // From so many sequences on, those with up to 16 rows, or one token, are left to the kernel for few where the call is the kernel's for many: tokens beside a prompt.  (us with and
-// without, 32 heads on 8 of 128, bf16: 2048 of 8192 tokens and 63 sequences of up to 8192 with one 533 and 1417, 1024 tokens and 7 sequences of up to 8000 149 and 228,
-// 512 of 2000 and 7 of up to 4000 143 and 123, 8 sequences of 600 with 300 each 68.7 and 68.4.)
+// without, 32 heads on 8 of 128, bf16: 2048 of 8192 tokens and one of each of 63 sequences of up to 8192 507 and 1454, 1024 of 4096 and 31 of up to 4096 250 and 403, and 15 of them 247 and
+// 279; with 7 sequences it goes either way: 512 of 2000 and 7 of up to 32768 594 and 916, a prompt of 1024 and 7 of up to 8000 174 and 231, but 1024 of 8000 and 7 of up to 8000 453
+// and 327, 512 of 2000 and 7 of up to 4000 155 and 122; 8 sequences of 600 with 300 each 74 and 73.)
 constexpr int64_t kMixed = 8;
 
 template <typename T, int DP, int kKind>

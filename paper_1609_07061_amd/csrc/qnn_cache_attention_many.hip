@@ -2,8 +2,8 @@
 // the workgroup brings from memory to registers two tiles ahead, makes float16 once for all waves and lays into LDS as the matrix instructions (32 x 32 x 16) take them.
 // S^T = K Q^T and O^T = V^T P^T: of the first result a lane has keys 8 a + 4 g + 0 .. 3 (a = 0 .. 3, g = lane / 32) of its query lane mod 32, which is the second's
 // right operand as it is, with the rows of V^T's operand in that order of keys.
-// Bound by what a wave's matrix instructions and vector ones take together and by the card's power: the last 2048 of 8192 tokens, 32 heads on 8 of 128, bf16, take 340 to
-// 390 us (0.62 to 0.71 Pop/s; 155 at the rate of a large matrix product), matrix cores 27 % of the time busy, vector ones 60 %; on codes that are all zero, with the same
+// Bound by what a wave's matrix instructions and vector ones take together and by the card's power: the last 2048 of 8192 tokens, 32 heads on 8 of 128, bf16, take 342 to
+// 390 us (0.62 to 0.70 Pop/s; 155 at the rate of a large matrix product), matrix cores 27 % of the time busy, vector ones 61 %; on codes that are all zero, with the same
 // instructions, 312.  A quarter more vector instructions (a bias by distance whose slopes are zero) cost 1 to 3 %.
 #include "qnn_attention.h"
 

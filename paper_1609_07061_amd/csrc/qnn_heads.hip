@@ -7,7 +7,7 @@
 // cosine and sine in LDS for all heads.
 // Bound by memory: a read and a write of every value (8192 tokens of 40 heads of 128, bf16: 168 MB in 38 us; with a workgroup for every group of tokens, which asks for
 // its weights anew, 49; the gradient, two reads: 252 MB in 52 us and 4.6 for the weights' sums; keys and values of 4096 tokens to the cache, 8 heads each beside 32 of
-// queries: 50 MB read, 42 written in 28).  Few tokens: the launch (20 tokens: 5.8 us; of the gradient 2000: 19, in groups as for many 32).
+// queries: 50 MB read, 42 written in 27, of which the look-ups before each workgroup's only group are some 8).  Few tokens: the launch (20 tokens: 5.8 us; of the gradient 2000: 19, in groups as for many 32).
 #include <type_traits>
 
 #include "qnn_paged.h"
