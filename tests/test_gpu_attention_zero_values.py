@@ -11,9 +11,9 @@ from int8_testlib import U, assert_near, generator, normal
 pytestmark = pytest.mark.gpu
 N, HEADS, GROUP, D = 1500, 2, 4, 64
 NAMES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
-# What a weight 2^(t - R) b in float16 is off by, half of its least step, for every token: R is at least t + log2(max(b, 2^-96)) - 7 of the one that this is largest for, so that a part
-# of 2^-25 2^7 2^-96 of a code is lost where tokens of zeros outweigh all others by as much as that.
-FLOOR = N * 127 * 2.0 ** (-25 + 7 - 96)
+# What a weight 2^(t - R) b in float16 is off by, half of its least step, for every token: R lies 7 or more below the largest t + log2(max(b, 2^-96)), and the sum below the line is at least
+# 2^(t - R) of that token, so that up to 2^-25 2^-7 2^-96 of a code is lost where tokens of zeros outweigh all others by as much as that.
+FLOOR = N * 127 * 2.0 ** (-25 - 7 - 96)
 WHICH = {"all": lambda i: i >= 0, "first": lambda i: i < N // 2, "last": lambda i: i >= N // 2, "steps": lambda i: i // 32 % 2 == 0, "tiles": lambda i: i // 64 % 2 == 1,
          "all but one": lambda i: i != 700}
 
